@@ -67,6 +67,9 @@ extern "C" {
 #define CKKS_OP_RESCALE 5
 #define CKKS_OP_PCMM_BSGS_DH 6
 #define CKKS_OP_HROT_SUM 7
+#define CKKS_OP_ROPE 8
+#define CKKS_OP_LINATTN_STEP 9  /* these two: ckks_linattn_workspace_bytes */
+#define CKKS_OP_LINATTN_CHUNK 10
 
 typedef struct ckks_ctx ckks_ctx;
 
@@ -294,6 +297,64 @@ int ckks_pmult(ckks_ctx* ctx, uint64_t* ct_out, const uint64_t* ct_in, const uin
                void* stream);
 int ckks_add(ckks_ctx* ctx, uint64_t* out, const uint64_t* a, const uint64_t* b, uint32_t npoly, uint32_t nlimbs,
              void* stream);
+
+/*
+ * Softmax-free attention on ciphertexts (extensions: the paper evaluates its attention with a polynomial softmax, Sec. 4.3; these
+ * are the parts of an attention that needs none). A lane is one head of one sequence; component i of a lane's vector sits in slot
+ * i * stride + lane, so that rotations by multiples of stride turn the components of all lanes at once.
+ *
+ * ckks_rope: rotary positions, a weighted sum of a ciphertext and R of its rotations with one ModDown. With P the product of the
+ * special primes and A(d; key) the two accumulators of a key switch of d before ModDown, in the extended basis,
+ *   ct_out[b] = ModDown( w_0 (.) (P c0, P c1) + sum_{r=1..R} w_r (.) ( A(sigma_r(c1); evks[r-1]) + (P sigma_r(c0), 0) ) ),
+ * i.e. w_0 (.) ct + sum_r w_r (.) HRot_r(ct) up to where ModDown rounds. w_0 holds the cosines (and ones for the components that do not
+ * turn), w_r the sines of the components whose partner is rotation r away; positions, layouts, scalings and the decays of
+ * linear attention are the tables' business (paper_2604_03425_amd.rope_tables).
+ *   pt_ext       device [npt][R + 1][nlimbs + K][N], evaluation domain: weights over q_0..q_{nlimbs-1}, p_0..p_{K-1} (the special
+ *                limbs of every w_0 are not read); ciphertext b of the batch uses set b / (B / npt), npt divides B
+ *   galois_elts, evks   host arrays of R entries (R = 0: a plain product with w_0)
+ * ct_in, ct_out: device [B][2][nlimbs][N]; ct_out may overlap neither ct_in nor pt_ext. Output scale = input scale times the
+ * weights' (no rescale). Workspace: CKKS_OP_ROPE.
+ */
+int ckks_rope(ckks_ctx* ctx, uint64_t* ct_out, const uint64_t* ct_in, uint32_t B, uint32_t nlimbs, const uint64_t* pt_ext,
+              uint32_t npt, const uint32_t* galois_elts, const uint64_t* const* evks, uint32_t R, void* ws, size_t ws_bytes,
+              void* stream);
+
+/*
+ * Linear attention with a decay for each head: o_t = q_t^T S_t, S_t = decay S_{t-1} + k_t v_t^T, for lanes of d = n1 * n2
+ * components (n1 * n2 * stride = N/2 slots makes every rotation cyclic within a lane, which is what the formulas below need to be
+ * this sum). The state is held as its d diagonals,
+ *   state[g][b] (slot i * stride + lane) = S[i + b][i - g n1],      device [n2][n1][B][2][nlimbs][N].
+ * Decays within a call are folded into q and k, which carry decay^(t+1) and decay^(-t-1) at token t = 0.. of the call (the weights
+ * of ckks_rope do that at no cost); `decay` (device [nlimbs][N], evaluation domain, or NULL for none) holds decay^tokens for every
+ * lane. With K[b] = HRot_{b stride}(k), Q[b] likewise, V[g] = HRot_{-g n1 stride}(v), and * a product in three components:
+ *   read(q, S, e) = ModDown( A(d2; evk_mult) + (P d0, P d1) + sum_{g>=1} ( A(sigma_g(y_g.c1); evk_giant[g-1]) + (P sigma_g(y_g.c0), 0) ) ),
+ *     d = e + sum_b Q[b] * S[0][b],  y_g = Relin(sum_b Q[b] * S[g][b]),  sigma_g of the rotation by g * n1 * stride.
+ * ckks_linattn_step, a token for each of B ciphertexts of lanes (the recurrent form):
+ *   M = S + Relin(K[b] * V[g]);  o = read(q, M, 0);  state_out = decay (.) M.
+ * ckks_linattn_chunk, `tokens` tokens at once (q, k, v, o_out: [tokens][B][2][nlimbs][N]):
+ *   o_t = read(q_t, S, sum_{s<=t} p_ts * v_s),  p_ts = sum2(sum1(Relin(q_t * k_s)));
+ *   state_out = decay (.) (S + Relin(sum_s K_s[b] * V_s[g]));
+ *   sum1(x) = ModDown(P x + sum_{b=1..n1-1} (A(sigma_b(c1); evk_baby[b-1]) + (P sigma_b(c0), 0))) and sum2 the same over the giant
+ *   steps: the scores of a lane end up in all of its slots.
+ * Without a state (state_in NULL: the start of a sequence) S is zero; read(q, 0, e) = Relin(e). state_out may be state_in.
+ * Scales: the state has the square of the inputs' scale, o its cube (times decay's for the state, where given); no rescale.
+ *   evk_mult    device, the relinearisation key; evk_baby, evk_giant as for ckks_pcmm_bsgs
+ *   evk_value   host array of n2-1 device pointers; evk_value[g-1] switches 5^(-g*n1*stride). Where n1*n2*stride = N/2 that is the
+ *               key of the giant step n2 - g.
+ * No output may overlap an input, but for state_out = state_in. Workspace: ckks_linattn_workspace_bytes (0 on a bad argument);
+ * tokens = 1 for a step. Limits: tokens, n1, n2 <= 4096, tokens * B <= 32767, n2 * tokens * B <= 65535.
+ */
+size_t ckks_linattn_workspace_bytes(const ckks_ctx* ctx, int op, uint32_t tokens, uint32_t B, uint32_t nlimbs, uint32_t n1,
+                                    uint32_t n2);
+int ckks_linattn_step(ckks_ctx* ctx, uint64_t* o_out, uint64_t* state_out, const uint64_t* q, const uint64_t* k,
+                      const uint64_t* v, const uint64_t* state_in, const uint64_t* decay, uint32_t B, uint32_t nlimbs,
+                      uint32_t n1, uint32_t n2, uint32_t stride, const uint64_t* evk_mult, const uint64_t* const* evk_baby,
+                      const uint64_t* const* evk_giant, const uint64_t* const* evk_value, void* ws, size_t ws_bytes, void* stream);
+int ckks_linattn_chunk(ckks_ctx* ctx, uint64_t* o_out, uint64_t* state_out, const uint64_t* q, const uint64_t* k,
+                       const uint64_t* v, const uint64_t* state_in, const uint64_t* decay, uint32_t tokens, uint32_t B,
+                       uint32_t nlimbs, uint32_t n1, uint32_t n2, uint32_t stride, const uint64_t* evk_mult,
+                       const uint64_t* const* evk_baby, const uint64_t* const* evk_giant, const uint64_t* const* evk_value,
+                       void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Measurement support (not part of the paper's operator set). While enabled, every kernel

@@ -217,6 +217,37 @@ class RefContext:
                                   C.c_uint32(R)))
         return out
 
+    def rope(self, ct, w, galois_elts, evks):
+        """w_0 ct + sum_r w_r HRot_{g_r}(ct) with one ModDown; w [npt][R + 1][nl + K][N], set b // (B / npt) for ciphertext b."""
+        ct, cp = _u64(ct)
+        w, wp = _u64(w)
+        B, two, nl, _ = ct.shape
+        npt, R = w.shape[0], len(galois_elts)
+        assert two == 2 and w.shape == (npt, R + 1, nl + self.np_, self.N) and len(evks) == R
+        keep = [_u64(k) for k in evks]
+        keys = (u64p * max(1, R))(*[k[1] for k in keep])
+        gs = (C.c_uint32 * max(1, R))(*[int(g) for g in galois_elts])
+        out = np.empty_like(ct)
+        _check(lib().ref_rope(self._h, out.ctypes.data_as(u64p), cp, C.c_uint32(B), C.c_uint32(nl), wp, C.c_uint32(npt), gs, keys,
+                              C.c_uint32(R)))
+        return out
+
+    def relin_rotated(self, d, evk, y, galois_elts, evks):
+        """Relin(d) plus the rotations of y [G][B][2][nl][N] with one ModDown."""
+        d, dp = _u64(d)
+        evk, ep = _u64(evk)
+        B, three, nl, _ = d.shape
+        G = len(galois_elts)
+        y, yp = _u64(y if G else np.zeros(1, dtype=np.uint64))
+        assert three == 3 and len(evks) == G and (not G or y.shape == (G, B, 2, nl, self.N))
+        keep = [_u64(k) for k in evks]
+        keys = (u64p * max(1, G))(*[k[1] for k in keep])
+        gs = (C.c_uint32 * max(1, G))(*[int(g) for g in galois_elts])
+        out = np.empty((B, 2, nl, self.N), dtype=np.uint64)
+        _check(lib().ref_relin_rotated(self._h, out.ctypes.data_as(u64p), dp, ep, yp, C.c_uint32(G), gs, keys, C.c_uint32(B),
+                                       C.c_uint32(nl)))
+        return out
+
     def tensor_acc(self, ct_a, ct_b, d_acc=None):
         """Un-relinearised product [B][3][nl][N], added to d_acc when given (late relinearisation, Sec. 5.2)."""
         ct_a, ap = _u64(ct_a)

@@ -758,6 +758,103 @@ int ref_hrot_sum(const RefCtx* c, u64* ct_out, const u64* ct_in, uint32_t B, uin
   return 0;
 }
 
+// Weighted sum of a ciphertext and R of its rotations with one rounding (rotary positions): with w [npt][R + 1][nlimbs + K][N] in
+// the extended basis (q_0..q_{nlimbs-1}, p_0..p_{K-1}), evaluation domain, and set b / (B / npt) for ciphertext b,
+//   T = w_0 (.) (P c0, P c1) + sum_r w_r (.) [ accumulators of the key switch of sigma_r(c1), plus P sigma_r(c0) ], out = ModDown(T).
+int ref_rope(const RefCtx* c, u64* ct_out, const u64* ct_in, uint32_t B, uint32_t nlimbs, const u64* w, uint32_t npt,
+             const uint32_t* galois, const u64* const* evks, uint32_t R) {
+  if (nlimbs == 0 || nlimbs > (uint32_t)c->nq || npt == 0 || B % npt) return fail("bad limb or set count");
+  const size_t N = c->N, pl = (size_t)nlimbs * N, sz = 2 * pl;
+  const int next = (int)nlimbs + c->np;
+  const size_t el = (size_t)next * N;
+  auto ext_mod = [&](int t) { return c->mod[t < (int)nlimbs ? t : c->nq + (t - (int)nlimbs)]; };
+  auto lifted = [&](u64 x, int t) {   // P x on the main primes
+    const u64 m = c->mod[t];
+    for (int k = 0; k < c->np; k++) x = mulm(x, c->mod[c->nq + k] % m, m);
+    return x;
+  };
+  parallel_for(B, [&](size_t bi) {
+    const u64* x = ct_in + bi * sz;
+    const u64* ws = w + (bi / (B / npt)) * (R + 1) * el;
+    std::vector<u64> T(2 * el, 0), r0(pl), r1(pl);
+    for (uint32_t r = 0; r <= R; r++) {
+      std::vector<u64> A(2 * el, 0);
+      if (r) {
+        for (uint32_t i = 0; i < nlimbs; i++) {
+          automorph_eval(c, &r0[(size_t)i * N], x + (size_t)i * N, i, galois[r - 1]);
+          automorph_eval(c, &r1[(size_t)i * N], x + pl + (size_t)i * N, i, galois[r - 1]);
+        }
+        A = keyswitch_accumulate(c, r1.data(), nlimbs, evks[r - 1]);
+      }
+      for (int comp = 0; comp < 2; comp++)
+        for (uint32_t i = 0; i < nlimbs; i++)
+          for (size_t n = 0; n < N; n++) {
+            if (r && comp) continue;
+            u64& a = A[(size_t)comp * el + (size_t)i * N + n];
+            const u64 v = r ? r0[(size_t)i * N + n] : x[(size_t)comp * pl + (size_t)i * N + n];
+            a = addm(a, lifted(v, (int)i), c->mod[i]);
+          }
+      for (int comp = 0; comp < 2; comp++)
+        for (int t = 0; t < next; t++)
+          for (size_t n = 0; n < N; n++) {
+            const u64 m = ext_mod(t);
+            const size_t k = (size_t)comp * el + (size_t)t * N + n;
+            T[k] = addm(T[k], mulm(A[k], ws[(size_t)r * el + (size_t)t * N + n], m), m);
+          }
+    }
+    moddown_pair(c, ct_out + bi * sz, T, nlimbs);
+  });
+  return 0;
+}
+
+// Relinearisation of d [B][3][nlimbs][N] plus G rotated ciphertexts y [G][B][2][nlimbs][N], with one rounding:
+//   T = accumulators of the key switch of d2 under evk, plus P (d0, d1)
+//     + sum_g [ accumulators of the key switch of sigma_g(y_g.c1) under evks[g], plus P sigma_g(y_g.c0) ],   out = ModDown(T).
+int ref_relin_rotated(const RefCtx* c, u64* ct_out, const u64* d, const u64* evk, const u64* y, uint32_t G, const uint32_t* galois,
+                      const u64* const* evks, uint32_t B, uint32_t nlimbs) {
+  if (nlimbs == 0 || nlimbs > (uint32_t)c->nq) return fail("bad limb count");
+  const size_t N = c->N, pl = (size_t)nlimbs * N;
+  const int next = (int)nlimbs + c->np;
+  const size_t el = (size_t)next * N;
+  auto ext_mod = [&](int t) { return c->mod[t < (int)nlimbs ? t : c->nq + (t - (int)nlimbs)]; };
+  parallel_for(B, [&](size_t bi) {
+    std::vector<u64> T(2 * el, 0), r0(pl), r1(pl);
+    auto add = [&](const std::vector<u64>& A) {
+      for (int comp = 0; comp < 2; comp++)
+        for (int t = 0; t < next; t++)
+          for (size_t n = 0; n < N; n++) {
+            const size_t k = (size_t)comp * el + (size_t)t * N + n;
+            T[k] = addm(T[k], A[k], ext_mod(t));
+          }
+    };
+    auto add_main = [&](int comp, const u64* x) {
+      for (uint32_t i = 0; i < nlimbs; i++)
+        for (size_t n = 0; n < N; n++) {
+          const u64 m = c->mod[i];
+          u64 v = x[(size_t)i * N + n];
+          for (int k = 0; k < c->np; k++) v = mulm(v, c->mod[c->nq + k] % m, m);
+          u64& a = T[(size_t)comp * el + (size_t)i * N + n];
+          a = addm(a, v, m);
+        }
+    };
+    const u64* db = d + bi * 3 * pl;
+    add(keyswitch_accumulate(c, db + 2 * pl, nlimbs, evk));
+    add_main(0, db);
+    add_main(1, db + pl);
+    for (uint32_t g = 0; g < G; g++) {
+      const u64* x = y + ((size_t)g * B + bi) * 2 * pl;
+      for (uint32_t i = 0; i < nlimbs; i++) {
+        automorph_eval(c, &r0[(size_t)i * N], x + (size_t)i * N, i, galois[g]);
+        automorph_eval(c, &r1[(size_t)i * N], x + pl + (size_t)i * N, i, galois[g]);
+      }
+      add(keyswitch_accumulate(c, r1.data(), nlimbs, evks[g]));
+      add_main(0, r0.data());
+    }
+    moddown_pair(c, ct_out + bi * 2 * pl, T, nlimbs);
+  });
+  return 0;
+}
+
 // BSGS matmul with the baby steps kept in the extended basis ("double hoisting": the hoisting the paper discusses
 // in Sec. 5.1 taken one step further; not the paper's own schedule, which rotates one at a time). With
 // P = p_0 ... p_{K-1} and the basis q_0..q_{nlimbs-1}, p_0..p_{K-1}:

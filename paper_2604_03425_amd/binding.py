@@ -12,6 +12,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libckks_mi355.so")
 
 OP_KEYSWITCH, OP_HROT, OP_HMULT_RELIN, OP_PCMM_BSGS, OP_RESCALE, OP_PCMM_BSGS_DH, OP_HROT_SUM = 1, 2, 3, 4, 5, 6, 7
+OP_ROPE, OP_LINATTN_STEP, OP_LINATTN_CHUNK = 8, 9, 10
 
 _SYMBOLS = ["ckks_last_error", "ckks_ctx_create", "ckks_ctx_destroy", "ckks_workspace_bytes", "ckks_ntt", "ckks_intt",
             "ckks_automorph", "ckks_keyswitch", "ckks_hrot", "ckks_hmult_relin", "ckks_pcmm_bsgs",
@@ -19,7 +20,8 @@ _SYMBOLS = ["ckks_last_error", "ckks_ctx_create", "ckks_ctx_destroy", "ckks_work
             "ckks_prof_reset", "ckks_prof_copy", "ckks_tune_set", "ckks_rescale", "ckks_pmult", "ckks_add",
             "ckks_hrot_hoisted", "ckks_pcmm_bsgs_hoisted", "ckks_hrot_multi", "ckks_hrot_add", "ckks_tensor_acc",
             "ckks_relin", "ckks_pcmm_bsgs_double_hoisted", "ckks_hrot_sum", "ckks_hrot_noalloc",
-            "ckks_noalloc_scratch_bytes"]
+            "ckks_noalloc_scratch_bytes", "ckks_rope", "ckks_linattn_workspace_bytes", "ckks_linattn_step",
+            "ckks_linattn_chunk"]
 
 
 class CkksError(RuntimeError):
@@ -73,6 +75,13 @@ def _load():
     lib.ckks_rescale.argtypes = [vp, u64p, u64p, C.c_uint32, C.c_uint32, vp, C.c_size_t, vp]
     lib.ckks_pmult.argtypes = [vp, u64p, u64p, u64p, C.c_uint32, C.c_uint32, vp]
     lib.ckks_add.argtypes = [vp, u64p, u64p, u64p, C.c_uint32, C.c_uint32, vp]
+    keys = C.POINTER(C.c_void_p)
+    lib.ckks_rope.argtypes = [vp, u64p, u64p, C.c_uint32, C.c_uint32, u64p, C.c_uint32, u32p, keys, C.c_uint32, vp, C.c_size_t, vp]
+    lib.ckks_linattn_workspace_bytes.restype = C.c_size_t
+    lib.ckks_linattn_workspace_bytes.argtypes = [vp, C.c_int] + [C.c_uint32] * 5
+    tail = [u64p, keys, keys, keys, vp, C.c_size_t, vp]
+    lib.ckks_linattn_step.argtypes = [vp] + [u64p] * 7 + [C.c_uint32] * 5 + tail
+    lib.ckks_linattn_chunk.argtypes = [vp] + [u64p] * 7 + [C.c_uint32] * 6 + tail
     lib.ckks_prof_enable.argtypes = [vp, C.c_int]
     lib.ckks_prof_copy.argtypes = [vp, vp, vp, C.c_size_t, vp]
     lib.ckks_tune_set.argtypes = [vp, C.c_int, C.c_int]
@@ -146,6 +155,12 @@ class Context:
 
     def workspace(self, op, batch, nlimbs, n1=0):
         n = ckks_workspace_bytes(self, op, batch, nlimbs, n1)
+        if n == 0:
+            raise CkksError(-2, "bad shape for workspace query")
+        return torch.empty(n // 8, dtype=torch.int64, device="cuda:%d" % self.device)
+
+    def linattn_workspace(self, op, tokens, batch, nlimbs, n1, n2):
+        n = ckks_linattn_workspace_bytes(self, op, tokens, batch, nlimbs, n1, n2)
         if n == 0:
             raise CkksError(-2, "bad shape for workspace query")
         return torch.empty(n // 8, dtype=torch.int64, device="cuda:%d" % self.device)
@@ -321,3 +336,50 @@ def ckks_pcmm_bsgs_hoisted(ctx, ct_out, ct_in, B, nlimbs, pt_diag, n1, n2, strid
 
 def ckks_pcmm_bsgs_double_hoisted(ctx, ct_out, ct_in, B, nlimbs, pt_ext, n1, n2, stride, evk_baby, evk_giant, ws):
     ckks_pcmm_bsgs(ctx, ct_out, ct_in, B, nlimbs, pt_ext, n1, n2, stride, evk_baby, evk_giant, ws, hoisted="double")
+
+
+def ckks_linattn_workspace_bytes(ctx, op, tokens, batch, nlimbs, n1, n2):
+    return int(_lib.ckks_linattn_workspace_bytes(ctx.handle, op, tokens, batch, nlimbs, n1, n2))
+
+
+def _keys(ctx, name, evks):
+    return (C.c_void_p * max(1, len(evks)))(*[_ptr(k, name, ctx, _key_elems(ctx)).value for k in evks])
+
+
+def ckks_rope(ctx, ct_out, ct_in, B, nlimbs, pt_ext, npt, galois_elts, evks, ws):
+    R = len(galois_elts)
+    if len(evks) != R:
+        raise ValueError("need one key per Galois element")
+    gs, _ = _ids(galois_elts)
+    e = B * 2 * nlimbs * ctx.N
+    _check(_lib.ckks_rope(ctx.handle, _ptr(ct_out, "ct_out", ctx, e), _ptr(ct_in, "ct_in", ctx, e), B, nlimbs,
+                          _ptr(pt_ext, "pt_ext", ctx, npt * (R + 1) * (nlimbs + ctx.np_) * ctx.N), npt, gs,
+                          _keys(ctx, "evk", evks), R, _ptr(ws, "ws", ctx), ws.numel() * 8, _stream()))
+
+
+def _linattn(ctx, o_out, state_out, q, k, v, state_in, decay, tokens, B, nlimbs, n1, n2, evk_mult, evk_baby, evk_giant, evk_value):
+    if len(evk_baby) != n1 - 1 or len(evk_giant) != n2 - 1 or len(evk_value) != n2 - 1:
+        raise ValueError("need n1-1 baby-step keys, n2-1 giant-step keys and n2-1 value keys")
+    e = tokens * B * 2 * nlimbs * ctx.N
+    s = n1 * n2 * B * 2 * nlimbs * ctx.N
+    tensors = [_ptr(o_out, "o_out", ctx, e), _ptr(state_out, "state_out", ctx, s), _ptr(q, "q", ctx, e), _ptr(k, "k", ctx, e),
+               _ptr(v, "v", ctx, e), None if state_in is None else _ptr(state_in, "state_in", ctx, s),
+               None if decay is None else _ptr(decay, "decay", ctx, nlimbs * ctx.N)]
+    return tensors, [_ptr(evk_mult, "evk_mult", ctx, _key_elems(ctx)), _keys(ctx, "evk_baby", evk_baby),
+                     _keys(ctx, "evk_giant", evk_giant), _keys(ctx, "evk_value", evk_value)]
+
+
+def ckks_linattn_step(ctx, o_out, state_out, q, k, v, state_in, decay, B, nlimbs, n1, n2, stride, evk_mult, evk_baby, evk_giant,
+                      evk_value, ws):
+    tensors, keys = _linattn(ctx, o_out, state_out, q, k, v, state_in, decay, 1, B, nlimbs, n1, n2, evk_mult, evk_baby, evk_giant,
+                             evk_value)
+    _check(_lib.ckks_linattn_step(ctx.handle, *tensors, B, nlimbs, n1, n2, stride, *keys, _ptr(ws, "ws", ctx), ws.numel() * 8,
+                                  _stream()))
+
+
+def ckks_linattn_chunk(ctx, o_out, state_out, q, k, v, state_in, decay, tokens, B, nlimbs, n1, n2, stride, evk_mult, evk_baby,
+                       evk_giant, evk_value, ws):
+    tensors, keys = _linattn(ctx, o_out, state_out, q, k, v, state_in, decay, tokens, B, nlimbs, n1, n2, evk_mult, evk_baby,
+                             evk_giant, evk_value)
+    _check(_lib.ckks_linattn_chunk(ctx.handle, *tensors, tokens, B, nlimbs, n1, n2, stride, *keys, _ptr(ws, "ws", ctx),
+                                   ws.numel() * 8, _stream()))

@@ -1,0 +1,512 @@
+// Host side of the calls for softmax-free attention: rotary positions (ckks_rope) and linear attention with decays
+// (ckks_linattn_step, ckks_linattn_chunk). Included at the end of ckks_mi355.hip, whose launch sequences it uses.
+#pragma once
+
+namespace {
+
+// Takes pieces of a workspace in order; without one it only counts.
+struct Carve {
+  char* base;
+  size_t used = 0;
+  char* bytes(size_t n) {
+    char* p = base ? base + used : nullptr;
+    used += align256(n);
+    return p;
+  }
+  u64* words(size_t n) { return (u64*)bytes(n * 8); }
+};
+
+u32 rotation_element(const ckks_ctx* c, u64 steps) {   // 5^steps mod 2N
+  const u64 two_n = 2 * (u64)c->N;
+  u64 g = 1, b = 5;
+  for (; steps; steps >>= 1) {
+    if (steps & 1) g = g * b % two_n;
+    b = b * b % two_n;
+  }
+  return (u32)g;
+}
+
+// Digits of B polynomials in the extended basis, evaluation domain, at L.ext of the key-switch workspace: (b, limb t) is at
+// d + b * d_stride + t * N. Doubles on the double-precision moduli of the two-pass rings, canonical residues elsewhere.
+int ext_digits(ckks_ctx* c, const LevelTables* lt, const u64* d, u64 d_stride, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
+  int rc;
+  if (two_pass(c)) {
+    FwdInnerArgs ia;
+    return hoist_front16(c, lt, d, d_stride, B, nlimbs, ws, st, ia);
+  }
+  const u32 N = c->N, next = lt->next, beta = lt->beta;
+  const KsLayout L = ks_layout(c, B, nlimbs);
+  u64 *dcoef = (u64*)(ws + L.dcoef), *ext = (u64*)(ws + L.ext);
+  if ((rc = launch_ntt(c, true, d, d_stride, dcoef, (u64)nlimbs * N, B, 0, nlimbs, identity_map(nlimbs), 0, 0, st))) return rc;
+  {
+    ModUpArgs a{dcoef, ext, c->d_mods, lt->up_inv, lt->up_mat, c->logN, nlimbs, c->nq, c->alpha, beta, next};
+    ProfScope ps(c, PK_MODUP, st);
+    launch_modup<false>(c, lt, a, beta, B, st);
+    HIP_TRY(hipGetLastError());
+  }
+  return launch_ntt(c, false, ext, (u64)next * N, ext, (u64)next * N, B * beta, 0, next, ext_map(c, nlimbs), beta, nlimbs, st);
+}
+
+// ModDown of both accumulators [B][2][next][N] (their special limbs are overwritten) to out [B][2][nlimbs][N].
+int ext_mod_down(ckks_ctx* c, const LevelTables* lt, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
+  int rc;
+  if (two_pass(c)) {
+    KsIo io{nullptr, 0, 0, out, {0, 0}, nullptr, 0};
+    return ks16_finish(c, lt, io, B, nlimbs, ws, st, acc);
+  }
+  const u32 N = c->N, next = lt->next, K = c->np;
+  u64* tq = (u64*)(ws + ks_layout(c, B, nlimbs).tq);
+  LimbMap pmap;
+  for (u32 k = 0; k < CKKS_MAX_SLOTS; k++) pmap.id[k] = (unsigned char)(k < K ? c->nq + k : 0);
+  if ((rc = launch_ntt(c, true, acc, (u64)next * N, acc, (u64)next * N, B * 2, nlimbs, K, pmap, 0, 0, st))) return rc;
+  {
+    ModDownArgs a{acc, tq, c->d_mods, lt->dn_inv, lt->dn_mat, c->logN, nlimbs, c->nq, K, next, nlimbs, c->nq};
+    ProfScope ps(c, PK_MODDOWN, st);
+    launch_moddown<false>(c, lt, a, B * 2, lt->narrow_dn, st);
+    HIP_TRY(hipGetLastError());
+  }
+  if ((rc = launch_ntt(c, false, tq, (u64)nlimbs * N, tq, (u64)nlimbs * N, B * 2, 0, nlimbs, identity_map(nlimbs), 0, 0, st)))
+    return rc;
+  FinalArgs a{acc, tq, out, c->d_mods, lt->pinv, c->logN, nlimbs, next, 0};
+  ProfScope ps(c, PK_FINAL, st);
+  hipLaunchKernelGGL(ks_final_kernel, dim3(N / 256, nlimbs, B * 2), dim3(256), 0, st, a);
+  HIP_TRY(hipGetLastError());
+  return CKKS_OK;
+}
+
+// Everything about rot_sum_kernel's arguments that the context and the level fix.
+RotSumArgs rot_sum_args(const ckks_ctx* c, const LevelTables* lt, u32 nlimbs, u64* acc, u64 d_stride) {
+  RotSumArgs a;
+  a.base = a.w = nullptr;
+  a.base_stride = 0;
+  a.acc = acc;
+  a.mods = c->d_mods;
+  a.d_stride = d_stride;
+  a.logN = c->logN;
+  a.nlimbs = nlimbs;
+  a.nq = c->nq;
+  a.nm = c->nm;
+  a.alpha = c->alpha;
+  a.beta = lt->beta;
+  a.next = lt->next;
+  a.nterms = a.w_first = a.w_terms = a.accumulate = 0;
+  a.per_set = 1;
+  return a;
+}
+int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st) {
+  const LimbMap emap = ext_map(c, a.nlimbs);
+  for (int kind = 0; kind < 3; kind++) {
+    u32 cnt = 0;
+    for (u32 s = 0; s < a.next; s++) {
+      const int k = !two_pass(c) ? 2 : host_class(c, c->mod[emap.id[s]]) == 0 ? 0 : 1;
+      if (k == kind) a.slots[cnt++] = (unsigned char)s;
+    }
+    if (!cnt) continue;
+    ProfScope ps(c, PK_ROT_SUM, st);
+    const dim3 grid(B, c->N / 256, cnt), block(256);
+    if (kind == 0) hipLaunchKernelGGL(rot_sum_kernel<0>, grid, block, 0, st, a);
+    else if (kind == 1) hipLaunchKernelGGL(rot_sum_kernel<1>, grid, block, 0, st, a);
+    else hipLaunchKernelGGL(rot_sum_kernel<2>, grid, block, 0, st, a);
+  }
+  HIP_TRY(hipGetLastError());
+  return CKKS_OK;
+}
+
+// acc = P w_0 ct + sum_r w_{r+1} (accumulators of the rotation of ct by galois[r]); ws: a key-switch workspace for B.
+int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, const u64* ct, u32 B, u32 nlimbs, const u32* galois,
+                     const u64* const* evks, u32 R, const u64* w, u32 per_set, u64* acc, char* ws, hipStream_t st) {
+  int rc;
+  const u64 pl = (u64)nlimbs * c->N;
+  if (R && (rc = ext_digits(c, lt, ct + pl, 2 * pl, B, nlimbs, ws, st))) return rc;
+  const u64* ext = (const u64*)(ws + ks_layout(c, B, nlimbs).ext);
+  RotSumArgs a = rot_sum_args(c, lt, nlimbs, acc, 2 * pl);
+  a.base = ct;
+  a.base_stride = 2 * pl;
+  a.w = w;
+  a.w_terms = R + 1;
+  a.per_set = per_set;
+  for (u32 r0 = 0; r0 == 0 || r0 < R; r0 += ROT_SUM_TERMS) {
+    a.nterms = std::min<u32>(ROT_SUM_TERMS, R - r0);
+    a.w_first = r0;
+    for (u32 r = 0; r < a.nterms; r++) a.term[r] = RotTerm{ext, ct + pl, ct, evks[r0 + r], galois[r0 + r]};
+    if ((rc = launch_rot_sum(c, a, B, st))) return rc;
+    a.base = nullptr;
+    a.accumulate = 1;
+  }
+  return CKKS_OK;
+}
+
+// ---- linear attention ----
+// Ciphertexts that one key switch of the calls below works on at a time: at least the B of a token. Enough to fill the chip
+// many times over; more would only take workspace.
+u32 linattn_slice(const ckks_ctx* c, u32 B) { return std::max<u32>(B, 64u << (c->logN < 16 ? 16 - c->logN : 0)); }
+
+struct LinAttn {
+  const ckks_ctx* cc;      // for sizes
+  ckks_ctx* c;
+  const LevelTables* lt;
+  u32 C, B, nlimbs, n1, n2;
+  u64 pl, ct;              // words of a polynomial, of a ciphertext
+  u32 slice, tokens;       // ciphertexts per key switch; tokens whose ciphertexts make at most that many
+  const u64 *mult_key;
+  const u64 *const *baby_keys, *const *giant_keys, *const *value_keys;
+  std::vector<u32> baby, giant, value;   // Galois elements
+  hipStream_t st;
+  // workspace
+  u64 *rot_a, *rot_b;      // rotations 1.. of keys or queries, and of values
+  u64 *d, *y, *p, *sums, *extra, *total;  // products in three components, ciphertexts, scores and their inner sums, the terms from
+                                          // inside the chunk, the read's sum in the extended basis
+  char* ks;
+  size_t ks_bytes;
+
+  void shape(const ckks_ctx* c_, u32 C_, u32 B_, u32 nlimbs_, u32 n1_, u32 n2_) {
+    cc = c_, C = C_, B = B_, nlimbs = nlimbs_, n1 = n1_, n2 = n2_;
+    pl = (u64)nlimbs * cc->N, ct = 2 * pl;
+    slice = linattn_slice(cc, B);
+    tokens = std::min<u32>(C, slice / B);
+  }
+  // pieces of the workspace of a step (scores = false) or of a chunk
+  size_t carve(char* ws, bool scores) {
+    Carve w{ws};
+    const u64 ext_ct = 2 * (u64)(nlimbs + cc->np) * cc->N;
+    const size_t group = (size_t)tokens * B;               // ciphertexts of the read's queries at a time
+    const size_t keyed = (size_t)C * B;
+    rot_a = w.words((n1 - 1) * keyed * ct);
+    rot_b = w.words((n2 - 1) * keyed * ct);
+    const size_t most = std::max<size_t>({(size_t)slice, group * n2, scores ? keyed : 0});
+    d = w.words(most * 3 * pl);
+    y = w.words(most * ct);
+    p = w.words(scores ? std::max<size_t>(slice, keyed) * ct : 0);
+    sums = w.words(scores ? slice * ct : 0);
+    extra = w.words(scores ? group * 3 * pl : 0);
+    total = w.words(group * ext_ct);
+    // a key switch of `slice` ciphertexts, the polynomials that rotations of rings without gathering kernels need, and the accumulators
+    // of hoisted rotations that share a pass over the digits
+    ks_bytes = ckks_workspace_bytes(cc, CKKS_OP_HROT, slice, nlimbs, 0) + hoisted_extra();
+    ks = w.bytes(ks_bytes);
+    return w.used;
+  }
+  u32 shared_rotations() const { return std::min<u32>(8, std::max(n1, n2) - 1); }
+  size_t hoisted_extra() const {
+    return two_pass(cc) ? (size_t)shared_rotations() * slice * 2 * (nlimbs + cc->np) * cc->N * 8 : 0;
+  }
+
+  // out[r][..] = rotations of n ciphertexts, one rotation out_stride words after another
+  int rotate(u64* out, u64 out_stride, const u64* in, u32 n, const std::vector<u32>& elements, const u64* const* keys) {
+    int rc;
+    const u32 R = (u32)elements.size();
+    const size_t need = ckks_workspace_bytes(c, CKKS_OP_HROT, slice, nlimbs, 0);
+    for (u32 i = 0; i < n && R; i += slice) {
+      const u32 nb = std::min(slice, n - i);
+      if (two_pass(c)) {
+        if ((rc = hrot_hoisted16(c, out + i * ct, out_stride, in + i * ct, nb, nlimbs, elements.data(), keys, R, ks, st, nullptr, 0,
+                                 false, (u64*)(ks + need), shared_rotations())))
+          return rc;
+        continue;
+      }
+      for (u32 r = 0; r < R; r++)
+        if ((rc = ckks_hrot(c, (uint64_t*)out + r * out_stride + i * ct, (const uint64_t*)in + i * ct, nb, nlimbs, elements[r],
+                            (const uint64_t*)keys[r], ks, ks_bytes, st)))
+          return rc;
+    }
+    return CKKS_OK;
+  }
+  int relin(u64* out, const u64* in, size_t n) {
+    int rc;
+    for (size_t i = 0; i < n; i += slice)
+      if ((rc = ckks_relin(c, (uint64_t*)out + i * ct, (const uint64_t*)in + i * 3 * pl, (u32)std::min<size_t>(slice, n - i), nlimbs,
+                           (const uint64_t*)mult_key, ks, ks_bytes, st)))
+        return rc;
+    return CKKS_OK;
+  }
+  int products(ProdSumArgs a, u32 first, u32 outputs) {
+    a.mods = c->d_mods;
+    a.logN = c->logN;
+    a.nlimbs = nlimbs;
+    a.B = B;
+    a.o_first = first;
+    ProfScope ps(c, PK_PROD_SUM, st);
+    hipLaunchKernelGGL(prod_sum_kernel, dim3(c->N / 256, nlimbs, outputs * B), dim3(256), 0, st, a);
+    HIP_TRY(hipGetLastError());
+    return CKKS_OK;
+  }
+
+  // state_out = state_in + Relin(sum_s K_s[b] * V_s[g]), then times decay. state_out may be state_in.
+  int update(u64* state_out, const u64* state_in, const u64* k, const u64* v, const u64* decay) {
+    int rc;
+    const u64 keyed = (u64)C * B;
+    if ((rc = rotate(rot_a, keyed * ct, k, C * B, baby, baby_keys))) return rc;
+    if ((rc = rotate(rot_b, keyed * ct, v, C * B, value, value_keys))) return rc;
+    ProdSumArgs a{};
+    a.x = ProdOperand{k, rot_a, {0, 0, keyed, B}, PROD_J};
+    a.y = ProdOperand{v, rot_b, {0, keyed, 0, B}, PROD_I};
+    a.nj = n1;
+    a.ns = C;
+    a.out = d;
+    a.add_comps = 2;
+    a.add_i = n2;
+    const u32 all = n1 * n2, per = slice / B;
+    for (u32 o = 0; o < all; o += per) {   // Relin(d) + S = Relin(d + (S, 0))
+      const u32 cnt = std::min(per, all - o);
+      a.add = state_in ? state_in + (u64)o * B * ct : nullptr;
+      if ((rc = products(a, o, cnt))) return rc;
+      if ((rc = relin(state_out + (u64)o * B * ct, d, (size_t)cnt * B))) return rc;
+    }
+    return decay ? multiply(state_out, decay) : CKKS_OK;
+  }
+  int multiply(u64* state, const u64* decay) {
+    int rc;
+    const u32 all = n1 * n2 * B;
+    for (u32 i = 0; i < all; i += 16384)
+      if ((rc = ckks_pmult(c, (uint64_t*)state + i * ct, (const uint64_t*)state + i * ct, (const uint64_t*)decay,
+                           std::min(16384u, all - i), nlimbs, st)))
+        return rc;
+    return CKKS_OK;
+  }
+
+  // o of tokens [t0, t0 + T), T <= tokens: see the header. extra (three components) holds these tokens' terms from inside the chunk.
+  int read(u64* o, const u64* q, u32 T, const u64* state, const u64* extra) {
+    int rc;
+    const u32 n = T * B;
+    const u64* d0 = extra;
+    if (state) {
+      if ((rc = rotate(rot_a, (u64)n * ct, q, n, baby, baby_keys))) return rc;
+      ProdSumArgs a{};
+      a.x = ProdOperand{q, rot_a, {0, 0, B, n}, PROD_S};
+      a.y = ProdOperand{state, nullptr, {0, (u64)n1 * B, 0, B}, PROD_NONE};
+      a.nj = T;
+      a.ns = n1;
+      a.out = d;
+      a.add = extra;
+      a.add_comps = 3;
+      a.add_i = 1;
+      if ((rc = products(a, 0, n2 * T))) return rc;
+      d0 = d;
+      if ((rc = relin(y, d + (u64)n * 3 * pl, (size_t)(n2 - 1) * n))) return rc;
+    }
+    // the sum of the first group's relinearisation and the others' rotations in the extended basis
+    if ((rc = ext_digits(c, lt, d0 + 2 * pl, 3 * pl, n, nlimbs, ks, st))) return rc;
+    RotSumArgs r = rot_sum_args(c, lt, nlimbs, total, 3 * pl);
+    r.base = d0;
+    r.base_stride = 3 * pl;
+    r.nterms = 1;
+    r.term[0] = RotTerm{(const u64*)(ks + ks_layout(c, n, nlimbs).ext), d0 + 2 * pl, nullptr, mult_key, 1};
+    if ((rc = launch_rot_sum(c, r, n, st))) return rc;
+    const u32 others = state ? n2 - 1 : 0, per = std::min<u32>(ROT_SUM_TERMS, slice / n);
+    for (u32 g0 = 0; g0 < others; g0 += per) {
+      const u32 cnt = std::min(per, others - g0);
+      const u64* yg = y + (u64)g0 * n * ct;
+      if ((rc = ext_digits(c, lt, yg + pl, ct, cnt * n, nlimbs, ks, st))) return rc;
+      const u64* ext = (const u64*)(ks + ks_layout(c, cnt * n, nlimbs).ext);
+      RotSumArgs s = rot_sum_args(c, lt, nlimbs, total, ct);
+      s.accumulate = 1;
+      s.nterms = cnt;
+      for (u32 g = 0; g < cnt; g++)
+        s.term[g] = RotTerm{ext + (u64)g * n * lt->beta * lt->next * c->N, yg + (u64)g * n * ct + pl, yg + (u64)g * n * ct,
+                            giant_keys[g0 + g], giant[g0 + g]};
+      if ((rc = launch_rot_sum(c, s, n, st))) return rc;
+    }
+    return ext_mod_down(c, lt, total, o, n, nlimbs, ks, st);
+  }
+
+  // out = in + its rotations by the elements, one ModDown for all of them; n <= slice ciphertexts
+  int sum_rotations(u64* out, const u64* in, u32 n, const std::vector<u32>& elements, const u64* const* keys) {
+    int rc;
+    u64* acc = (u64*)(ks + ks_layout(c, n, nlimbs).acc);
+    if ((rc = rotations_to_ext(c, lt, in, n, nlimbs, elements.data(), keys, (u32)elements.size(), nullptr, 1, acc, ks, st))) return rc;
+    return ext_mod_down(c, lt, acc, out, n, nlimbs, ks, st);
+  }
+
+  // d = sum_{s <= t} p_ts * v_s for tokens [t0, t0 + T)
+  int scored(u64* out, const u64* q, const u64* k, const u64* v, u32 t0, u32 T) {
+    int rc;
+    for (u32 t = t0; t < t0 + T;) {
+      // rows t .. u-1 of the triangle of pairs, whole rows that make at most a slice
+      u32 u = t + 1;
+      u64 pairs = t + 1;
+      while (u < t0 + T && (pairs + u + 1) * B <= std::max<u64>(slice, (u64)C * B)) {
+        u++;
+        pairs += u;
+      }
+      const u64 first = (u64)t * (t + 1) / 2;
+      ProdSumArgs a{};
+      a.x = ProdOperand{q, nullptr, {0, B, 0, 0}, PROD_NONE};
+      a.y = ProdOperand{k, nullptr, {0, 0, B, 0}, PROD_NONE};
+      a.nj = 1;
+      a.ns = 1;
+      a.tri_out = 1;
+      const u32 per = slice / B;
+      for (u64 i = 0; i < pairs; i += per) {
+        const u32 cnt = (u32)std::min<u64>(per, pairs - i);
+        a.out = d;
+        if ((rc = products(a, (u32)(first + i), cnt))) return rc;
+        u64* to = p + i * B * ct;
+        u64* stage = n1 > 1 || n2 > 1 ? y : to;
+        if ((rc = relin(stage, d, (size_t)cnt * B))) return rc;
+        if (n1 > 1) {
+          u64* next = n2 > 1 ? sums : to;
+          if ((rc = sum_rotations(next, stage, cnt * B, baby, baby_keys))) return rc;
+          stage = next;
+        }
+        if (n2 > 1 && (rc = sum_rotations(to, stage, cnt * B, giant, giant_keys))) return rc;
+      }
+      ProdSumArgs e{};
+      e.x = ProdOperand{p, nullptr, {0, 0, 0, B}, PROD_NONE};
+      e.y = ProdOperand{v, nullptr, {0, 0, 0, B}, PROD_NONE};
+      e.nj = 1;
+      e.tri_sum = 1;
+      e.tri_base = first;
+      e.out = out + (u64)(t - t0) * B * 3 * pl;
+      if ((rc = products(e, t, u - t))) return rc;
+      t = u;
+    }
+    return CKKS_OK;
+  }
+};
+
+int linattn_check(const ckks_ctx* c, u32 C, u32 B, u32 nlimbs, u32 n1, u32 n2) {
+  int rc = check_common(c, B, nlimbs);
+  if (rc) return rc;
+  if (C == 0 || n1 == 0 || n2 == 0) return fail(CKKS_ESHAPE, "tokens, n1 and n2 must be positive");
+  if (C > 4096 || n1 > 4096 || n2 > 4096 || (u64)C * B > 32767 || (u64)n1 * n2 * B > 32767 * 64ull || (u64)n2 * C * B > 65535 ||
+      (u64)linattn_slice(c, B) * std::max<u32>(2, c->dnum) > 65535)
+    return fail(CKKS_ESHAPE, "too many ciphertexts for one call");
+  return CKKS_OK;
+}
+
+struct LinAttnCall {
+  uint64_t *o_out, *state_out;
+  const uint64_t *q, *k, *v, *state_in, *decay;
+};
+int linattn_run(bool chunk, ckks_ctx* c, const LinAttnCall& io, u32 C, u32 B, u32 nlimbs, u32 n1, u32 n2, u32 stride,
+                const uint64_t* evk_mult, const uint64_t* const* evk_baby, const uint64_t* const* evk_giant,
+                const uint64_t* const* evk_value, void* ws, size_t ws_bytes, void* stream) {
+  int rc = linattn_check(c, C, B, nlimbs, n1, n2);
+  if (rc) return rc;
+  if (stride == 0) return fail(CKKS_ESHAPE, "stride must be positive");
+  if (!io.o_out || !io.state_out || !io.q || !io.k || !io.v || !evk_mult) return fail(CKKS_EINVAL, "null argument");
+  if ((n1 > 1 && !evk_baby) || (n2 > 1 && (!evk_giant || !evk_value))) return fail(CKKS_EINVAL, "null key array");
+  for (u32 b = 1; b < n1; b++)
+    if (!evk_baby[b - 1]) return fail(CKKS_EINVAL, "null baby-step key");
+  for (u32 g = 1; g < n2; g++)
+    if (!evk_giant[g - 1] || !evk_value[g - 1]) return fail(CKKS_EINVAL, "null giant-step or value key");
+  const size_t ct_bytes = (size_t)2 * nlimbs * c->N * 8, in_bytes = (size_t)C * B * ct_bytes, state_bytes = (size_t)n1 * n2 * B * ct_bytes;
+  for (const uint64_t* x : {io.q, io.k, io.v})
+    if (overlap(io.o_out, in_bytes, x, in_bytes) || overlap(io.state_out, state_bytes, x, in_bytes))
+      return fail(CKKS_EINVAL, "an output overlaps q, k or v");
+  if (overlap(io.o_out, in_bytes, io.state_out, state_bytes)) return fail(CKKS_EINVAL, "the outputs overlap each other");
+  if (io.state_in && (overlap(io.o_out, in_bytes, io.state_in, state_bytes) ||
+                      (io.state_in != io.state_out && overlap(io.state_out, state_bytes, io.state_in, state_bytes))))
+    return fail(CKKS_EINVAL, "state_in must be state_out itself or not overlap the outputs");
+  if (io.decay && (overlap(io.o_out, in_bytes, io.decay, ct_bytes / 2) || overlap(io.state_out, state_bytes, io.decay, ct_bytes / 2)))
+    return fail(CKKS_EINVAL, "an output overlaps decay");
+  LinAttn f;
+  f.shape(c, C, B, nlimbs, n1, n2);
+  f.c = c;
+  if (!ws || ((uintptr_t)ws & 255)) return fail(CKKS_EWORKSPACE, "workspace is null or not 256-byte aligned");
+  const size_t need = f.carve((char*)ws, chunk);
+  if (ws_bytes < need)
+    return fail(CKKS_EWORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes, got " + std::to_string(ws_bytes));
+  if ((rc = get_level(c, nlimbs, &f.lt))) return rc;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return fail(CKKS_EHIP, "cannot select the context's device");
+  f.st = (hipStream_t)stream;
+  f.mult_key = (const u64*)evk_mult;
+  f.baby_keys = (const u64* const*)evk_baby;
+  f.giant_keys = (const u64* const*)evk_giant;
+  f.value_keys = (const u64* const*)evk_value;
+  const u64 slots = c->N / 2;
+  for (u32 b = 1; b < n1; b++) f.baby.push_back(rotation_element(c, (u64)b * stride % slots));
+  for (u32 g = 1; g < n2; g++) {
+    const u64 steps = (u64)g * n1 % slots * stride % slots;
+    f.giant.push_back(rotation_element(c, steps));
+    f.value.push_back(rotation_element(c, slots - steps));
+  }
+  const u64 *q = (const u64*)io.q, *k = (const u64*)io.k, *v = (const u64*)io.v, *S = (const u64*)io.state_in, *decay = (const u64*)io.decay;
+  u64 *o = (u64*)io.o_out, *out = (u64*)io.state_out;
+  if (!chunk) {
+    if ((rc = f.update(out, S, k, v, nullptr))) return rc;
+    if ((rc = f.read(o, q, 1, out, nullptr))) return rc;
+    return decay ? f.multiply(out, decay) : CKKS_OK;
+  }
+  for (u32 t = 0; t < C; t += f.tokens) {   // all reads of the old state come before the update, which may overwrite it
+    const u32 T = std::min(f.tokens, C - t);
+    if ((rc = f.scored(f.extra, q, k, v, t, T))) return rc;
+    if ((rc = f.read(o + (u64)t * B * f.ct, q + (u64)t * B * f.ct, T, S, f.extra))) return rc;
+  }
+  return f.update(out, S, k, v, decay);
+}
+
+// Runs a call's body; what it may throw (memory for its host arrays) becomes an error code.
+template <class F>
+int guarded(F f) {
+  try {
+    return f();
+  } catch (const std::exception& e) {
+    return fail(CKKS_EINVAL, std::string("host error: ") + e.what());
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int ckks_rope(ckks_ctx* c, uint64_t* ct_out, const uint64_t* ct_in, uint32_t B, uint32_t nlimbs, const uint64_t* pt_ext, uint32_t npt,
+              const uint32_t* galois_elts, const uint64_t* const* evks, uint32_t R, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&]() -> int {
+    int rc = check_common(c, B, nlimbs);
+    if (rc) return rc;
+    if (!ct_out || !ct_in || !pt_ext || (R && (!galois_elts || !evks))) return fail(CKKS_EINVAL, "null argument");
+    if (npt == 0 || B % npt) return fail(CKKS_ESHAPE, "the batch must be a multiple of the number of weight sets");
+    for (u32 r = 0; r < R; r++) {
+      if (!evks[r]) return fail(CKKS_EINVAL, "null key");
+      if (!(galois_elts[r] & 1) || galois_elts[r] >= 2 * c->N) return fail(CKKS_EINVAL, "galois_elt must be odd and < 2N");
+    }
+    const LevelTables* lt;
+    if ((rc = get_level(c, nlimbs, &lt))) return rc;
+    if ((u64)B * std::max<u32>(2, lt->beta) > 65535) return fail(CKKS_ESHAPE, "batch too large for one call");
+    if ((rc = check_ws(c, CKKS_OP_ROPE, B, nlimbs, 0, ws, ws_bytes))) return rc;
+    const size_t ct_bytes = (size_t)B * 2 * nlimbs * c->N * 8;
+    const size_t pt_bytes = (size_t)npt * (R + (size_t)1) * lt->next * c->N * 8;
+    if (overlap(ct_out, ct_bytes, ct_in, ct_bytes) || overlap(ct_out, ct_bytes, pt_ext, pt_bytes))
+      return fail(CKKS_EINVAL, "ct_out overlaps an input");
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return fail(CKKS_EHIP, "cannot select the context's device");
+    hipStream_t st = (hipStream_t)stream;
+    u64* acc = (u64*)((char*)ws + ks_layout(c, B, nlimbs).acc);
+    if ((rc = rotations_to_ext(c, lt, (const u64*)ct_in, B, nlimbs, galois_elts, (const u64* const*)evks, R, (const u64*)pt_ext,
+                               B / npt, acc, (char*)ws, st)))
+      return rc;
+    return ext_mod_down(c, lt, acc, (u64*)ct_out, B, nlimbs, (char*)ws, st);
+  });
+}
+
+size_t ckks_linattn_workspace_bytes(const ckks_ctx* c, int op, uint32_t tokens, uint32_t B, uint32_t nlimbs, uint32_t n1, uint32_t n2) {
+  if ((op != CKKS_OP_LINATTN_STEP && op != CKKS_OP_LINATTN_CHUNK) || linattn_check(c, tokens, B, nlimbs, n1, n2)) return 0;
+  if (op == CKKS_OP_LINATTN_STEP && tokens != 1) return 0;
+  LinAttn f;
+  f.shape(c, tokens, B, nlimbs, n1, n2);
+  return f.carve(nullptr, op == CKKS_OP_LINATTN_CHUNK);
+}
+
+int ckks_linattn_step(ckks_ctx* c, uint64_t* o_out, uint64_t* state_out, const uint64_t* q, const uint64_t* k, const uint64_t* v,
+                      const uint64_t* state_in, const uint64_t* decay, uint32_t B, uint32_t nlimbs, uint32_t n1, uint32_t n2,
+                      uint32_t stride, const uint64_t* evk_mult, const uint64_t* const* evk_baby, const uint64_t* const* evk_giant,
+                      const uint64_t* const* evk_value, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&] {
+    return linattn_run(false, c, {o_out, state_out, q, k, v, state_in, decay}, 1, B, nlimbs, n1, n2, stride, evk_mult, evk_baby,
+                       evk_giant, evk_value, ws, ws_bytes, stream);
+  });
+}
+
+int ckks_linattn_chunk(ckks_ctx* c, uint64_t* o_out, uint64_t* state_out, const uint64_t* q, const uint64_t* k, const uint64_t* v,
+                       const uint64_t* state_in, const uint64_t* decay, uint32_t tokens, uint32_t B, uint32_t nlimbs, uint32_t n1,
+                       uint32_t n2, uint32_t stride, const uint64_t* evk_mult, const uint64_t* const* evk_baby,
+                       const uint64_t* const* evk_giant, const uint64_t* const* evk_value, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&] {
+    return linattn_run(true, c, {o_out, state_out, q, k, v, state_in, decay}, tokens, B, nlimbs, n1, n2, stride, evk_mult, evk_baby,
+                       evk_giant, evk_value, ws, ws_bytes, stream);
+  });
+}
+
+}  // extern "C"

@@ -15,6 +15,7 @@
 #include "ks12.hip.h"
 #include "ntt16_kernels.hip.h"
 #include "ntt_limb.hip.h"
+#include "attention.hip.h"
 
 typedef unsigned __int128 u128;
 
@@ -140,7 +141,7 @@ enum ProfKind {
   PK_FWD_ROWS, PK_FWD_BLOCKS = PK_FWD_ROWS + 3, PK_INV_BLOCKS = PK_FWD_BLOCKS + 3, PK_INV_ROWS = PK_INV_BLOCKS + 3,
   PK_FWD_FINAL = PK_INV_ROWS + 3,
   PK_AUTOMORPH = PK_FWD_FINAL + 3, PK_MODUP, PK_INNER, PK_INNER16, PK_INNER16_INT, PK_INNER_C, PK_INNER8, PK_INNER8_BIG, PK_BCONV_ROWS, PK_MODDOWN = PK_BCONV_ROWS + 3, PK_FINAL, PK_TENSOR, PK_PMACC, PK_PMACC_FP, PK_ADD,
-  PK_KS12_FRONT, PK_KS12_DIGITS, PK_KS12_SPECIAL, PK_KS12_FINAL, PK_CONV_ROWS, PK_COPY, PK_PMACC_STAGED, PK_PMACC_FP_STAGED, PK_COUNT
+  PK_KS12_FRONT, PK_KS12_DIGITS, PK_KS12_SPECIAL, PK_KS12_FINAL, PK_CONV_ROWS, PK_COPY, PK_PMACC_STAGED, PK_PMACC_FP_STAGED, PK_ROT_SUM, PK_PROD_SUM, PK_COUNT
 };
 static const char* const kProfNames[PK_COUNT] = {
     "ntt_fwd_pass", "ntt_inv_pass",
@@ -153,7 +154,7 @@ static const char* const kProfNames[PK_COUNT] = {
     "ntt16_bconv_rows_kernel<0>", "ntt16_bconv_rows_kernel<1>", "ntt16_bconv_rows_kernel<2>", "moddown_kernel", "ks_final_kernel", "tensor_kernel",
     "pmacc_int_kernel", "pmacc_fp_kernel", "addto_kernel",
     "ks12_front_kernel", "ks12_digits_kernel", "ks12_special_kernel", "ks12_final_kernel", "conv_rows_kernel", "copy",
-    "pmacc_int_staged_kernel", "pmacc_fp_staged_kernel"};
+    "pmacc_int_staged_kernel", "pmacc_fp_staged_kernel", "rot_sum_kernel", "prod_sum_kernel"};
 struct ProfRec {
   int kind;
   hipEvent_t start, stop;
@@ -1498,11 +1499,11 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
   return CKKS_OK;
 }
 
-// Shared front of the hoisted rotations: inverse transform, ModUp and forward transform of c1 of ct_in
-// ([B][2][nlimbs][N]) into the workspace, and the arguments of the streaming inner-product kernels that read them
+// Shared front of the hoisted rotations: inverse transform, ModUp and forward transform of B polynomials (limb-vector (b, t) at
+// d + b*d_stride + t*N) into the workspace, and the arguments of the streaming inner-product kernels that read them
 // (accumulators default to the workspace's own).
-static int hoist_front16(ckks_ctx* c, const LevelTables* lt, const u64* ct_in, u32 B, u32 nlimbs, char* ws, hipStream_t st,
-                         FwdInnerArgs& ia) {
+static int hoist_front16(ckks_ctx* c, const LevelTables* lt, const u64* d, u64 d_stride, u32 B, u32 nlimbs, char* ws,
+                         hipStream_t st, FwdInnerArgs& ia) {
   int rc;
   const u32 N = c->N, next = lt->next, beta = lt->beta;
   const u64 polyN = (u64)nlimbs * N;
@@ -1511,7 +1512,6 @@ static int hoist_front16(ckks_ctx* c, const LevelTables* lt, const u64* ct_in, u
   u64* ext = (u64*)(ws + L.ext);
   u64* acc = (u64*)(ws + L.acc);
   const LimbMap qmap = identity_map(nlimbs), emap = ext_map(c, nlimbs);
-  const u64* c1 = ct_in + polyN;
   NttOpts o1, of;
   o1.scale = lt->up_scale;
   of.blocks_only = conv_fits(c, 0, nlimbs, c->alpha);
@@ -1520,7 +1520,7 @@ static int hoist_front16(ckks_ctx* c, const LevelTables* lt, const u64* ct_in, u
     up = conv_up_job(c, lt, dcoef, ext, B, nlimbs);
     o1.blocks_only = !up.ready;
   }
-  if ((rc = launch_ntt(c, true, c1, 2 * polyN, dcoef, polyN, B, 0, nlimbs, qmap, 0, 0, st, o1))) return rc;
+  if ((rc = launch_ntt(c, true, d, d_stride, dcoef, polyN, B, 0, nlimbs, qmap, 0, 0, st, o1))) return rc;
   if (of.blocks_only) {
     if ((rc = launch_conv_rows(c, up, st))) return rc;
   } else {
@@ -1533,8 +1533,8 @@ static int hoist_front16(ckks_ctx* c, const LevelTables* lt, const u64* ct_in, u
   if ((rc = launch_ntt(c, false, ext, (u64)next * N, ext, (u64)next * N, B * beta, 0, next, emap, beta, nlimbs, st, of)))
     return rc;
   ia.ext = ext;
-  ia.d = c1;
-  ia.d_poly_stride = 2 * polyN;
+  ia.d = d;
+  ia.d_poly_stride = d_stride;
   ia.acc = acc;
   ia.tw = c->d_tw_fwd;
   ia.twfp = c->d_twfp_fwd;
@@ -1570,7 +1570,7 @@ int hrot_hoisted16(ckks_ctx* c, u64* out_base, u64 out_stride, const u64* ct_in,
   const LimbMap emap = ext_map(c, nlimbs);
   const u64* c1 = ct_in + polyN;
   FwdInnerArgs ia;
-  if ((rc = hoist_front16(c, lt, ct_in, B, nlimbs, ws, st, ia))) return rc;
+  if ((rc = hoist_front16(c, lt, c1, 2 * polyN, B, nlimbs, ws, st, ia))) return rc;
   if (acc_base) {
     ia.c0 = ct_in;
     ia.c0_poly_stride = 2 * polyN;
@@ -2109,6 +2109,7 @@ size_t ckks_workspace_bytes(const ckks_ctx* c, int op, uint32_t B, uint32_t nlim
       if (n1 == 0) return 0;
       // baby steps 1..n1-1, PMACC_TILE inner sums, rotated inner sum, HRot workspace
       return (size_t)(n1 - 1) * 2 * poly + (size_t)PMACC_TILE * 2 * poly + 2 * poly + ks + poly;
+    case CKKS_OP_ROPE: return ks;
     case CKKS_OP_HROT_SUM:
       // hoisted digits and ModDown scratch, plus the running sum in the extended basis
       return ks + poly + 2 * align256((size_t)B * (nlimbs + c->np) * c->N * 8);
@@ -2461,7 +2462,7 @@ int ckks_hrot_sum(ckks_ctx* c, uint64_t* ct_out, const uint64_t* ct_in, uint32_t
   char* hws = (char*)ws;
   u64* total = (u64*)(hws + ckks_workspace_bytes(c, CKKS_OP_HROT, B, nlimbs, 0));
   FwdInnerArgs ia;
-  if ((rc = hoist_front16(c, lt, (const u64*)ct_in, B, nlimbs, hws, st, ia))) return rc;
+  if ((rc = hoist_front16(c, lt, (const u64*)ct_in + (u64)nlimbs * N, 2 * (u64)nlimbs * N, B, nlimbs, hws, st, ia))) return rc;
   ia.acc = total;
   ia.c0 = (const u64*)ct_in;
   ia.c0_poly_stride = 2 * (u64)nlimbs * N;
@@ -2843,3 +2844,5 @@ int ckks_add(ckks_ctx* c, uint64_t* out, const uint64_t* a, const uint64_t* b, u
 }
 
 }  // extern "C"
+
+#include "attention_calls.hip.h"
