@@ -9,7 +9,8 @@
 //                 + sum_r w_r[t][n] ( sum_j D_rj[pi_r(n)] evk_r[j][c][id(t)][n] + [c = 0, main primes] P c0_r[b][t][pi_r(n)] ),
 // pi_r the evaluation-domain index map of term r. D_rj is digit j of the term's polynomial in the extended basis: d_r itself on
 // the limbs that the digit holds, the transformed conversions in ext_r elsewhere. Without weights every w is one. On integer
-// moduli of the two-pass rings acc carries the factor 2^-64 that ModDown's constants expect there.
+// moduli of the two-pass rings acc carries the factor 2^-64 that ModDown's constants expect there. A launch computes `outs` such
+// sums from nterms terms each, the accumulators one after another; base belongs to the first.
 struct RotTerm {
   const u64* ext;   // [B][beta][next][N]
   const u64* d;     // limb-vector (b, t) at d + b*d_stride + t*N
@@ -21,138 +22,312 @@ struct RotSumArgs {
   const u64* base;      // null: none; component c of ciphertext b at base + b*base_stride + c*nlimbs*N
   u64 base_stride;
   const u64* w;         // null: none; weight of term r of set s at w + ((s*w_terms + r + 1)*next + t)*N, of base at r = -1
-  u64* acc;             // [B][2][next][N]
+  u64* acc;             // [outs][B][2][next][N]
   const ModInfo* mods;
   u64 d_stride;
-  u32 logN, nlimbs, nq, nm, alpha, beta, next, nterms, w_first, w_terms, per_set, accumulate;
+  u32 logN, nlimbs, nq, nm, alpha, beta, next, B, nterms, w_first, w_terms, per_set, accumulate;
   unsigned char slots[128];
   RotTerm term[ROT_SUM_TERMS];
 };
 
-// KIND 0: doubles in ext (moduli < 2^50 of the two-pass rings); 1: residues, Montgomery factor in acc; 2: residues, none
-template <int KIND>
-__global__ void __launch_bounds__(256) rot_sum_kernel(RotSumArgs a) {
-  const size_t N = (size_t)1 << a.logN;
-  const u32 b = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x, t = a.slots[blockIdx.z];
+// Workgroup -> (what: ciphertexts or outputs, block of positions, limb), so that everything that reads the same positions of a limb
+// (key and weight slices, factors of many products) runs on one XCD, one after another, and finds them in its L2.
+__device__ __forceinline__ void attention_map(u32& what, u32& blk, u32& zi) {
+  const u32 lin = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z), units = gridDim.y * gridDim.z, whole = units & ~7u;
+  u32 unit;
+  if (lin < whole * gridDim.x) {
+    const u32 rest = lin >> 3;
+    what = rest % gridDim.x;
+    unit = (lin & 7) + 8 * (rest / gridDim.x);
+  } else {
+    const u32 rest = lin - whole * gridDim.x;
+    what = rest % gridDim.x;
+    unit = whole + rest / gridDim.x;
+  }
+  blk = unit % gridDim.y;
+  zi = unit / gridDim.y;
+}
+
+// Moduli below 2^50 on the two-pass rings: doubles in ext, sums in doubles (|.| < 2^53 = 8q throughout). A lane owns a position of
+// CB ciphertexts, which share the key words. grid = (outs * ceil(B / CB), N / 256, slots).
+template <int CB>
+__global__ void __launch_bounds__(256) rot_sum_fp_kernel(RotSumArgs a) {
+  const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, comp = (size_t)a.nm * N;
+  u32 what, blk, zi;
+  attention_map(what, blk, zi);
+  const u32 groups = (a.B + CB - 1) / CB, o = what / groups, b0 = (what % groups) * CB;
+  const u32 n = blk * 256 + threadIdx.x, t = a.slots[zi];
   const bool main_prime = t < a.nlimbs;
   const u32 id = main_prime ? t : t - a.nlimbs + a.nq;
   const ModInfo mi = a.mods[id];
-  const u64 m = mi.m;
-  const size_t pl = (size_t)a.nlimbs * N;
-  const u64* w = a.w ? a.w + (((size_t)(b / a.per_set) * a.w_terms + a.w_first) * a.next + t) * N + n : nullptr;
-  u64 s0 = 0, s1 = 0;
-  if (a.base && main_prime) {
-    const u64* x = a.base + (size_t)b * a.base_stride + (size_t)t * N + n;
-    const u64 pw = w ? mulmod(mi.pmod, *w, mi) : mi.pmod;
-    s0 = mulmod(x[0], pw, mi);
-    s1 = mulmod(x[pl], pw, mi);
+  const double q = mi.qd, qinv = mi.qinv, pm = u2d(mi.pmod);
+  u32 bb[CB];   // surplus places repeat the last ciphertext and store nothing
+  const u64* w[CB];
+  double s0[CB], s1[CB];
+#pragma unroll
+  for (int k = 0; k < CB; k++) {
+    bb[k] = min(b0 + k, a.B - 1);
+    w[k] = a.w ? a.w + (((size_t)(bb[k] / a.per_set) * a.w_terms + a.w_first) * a.next + t) * N + n : nullptr;
+    s0[k] = s1[k] = 0.0;
+    if (a.base && main_prime && o == 0) {
+      const u64* x = a.base + (size_t)bb[k] * a.base_stride + (size_t)t * N + n;
+      const double f = a.w ? fp_mulmod_var(pm, u2d(*w[k]), qinv, q) : pm;
+      s0[k] = fp_mulmod_var(u2d(x[0]), f, qinv, q);
+      s1[k] = fp_mulmod_var(u2d(x[pl]), f, qinv, q);
+    }
   }
+  const u32 jo = main_prime ? t / a.alpha : 0xFFFFFFFFu;   // the digit that holds limb t itself
   for (u32 r = 0; r < a.nterms; r++) {
-    const RotTerm& q = a.term[r];
-    const u32 k = galois_src_index(n, q.galois, a.logN);
-    Acc128 v0 = {0, 0}, v1 = {0, 0};
-    for (u32 j = 0; j < a.beta; j++) {
-      const u32 lo = j * a.alpha, hi = min(lo + a.alpha, a.nlimbs);
-      u64 x;
-      if (t >= lo && t < hi) {
-        x = q.d[(size_t)b * a.d_stride + (size_t)t * N + k];
+    const RotTerm& term = a.term[o * a.nterms + r];
+    const u32 m = galois_src_index(n, term.galois, a.logN);
+    const u64* e = term.evk + (size_t)id * N + n;
+    double v0[CB], v1[CB];
+#pragma unroll
+    for (int k = 0; k < CB; k++) {
+      v0[k] = v1[k] = 0.0;
+      if (term.c0 && main_prime) v0[k] = fp_mulmod_var(u2d(term.c0[(size_t)bb[k] * a.d_stride + (size_t)t * N + m]), pm, qinv, q);
+    }
+    for (u32 j = 0; j < a.beta; j++, e += 2 * comp) {
+      double x[CB];
+      if (j == jo) {
+#pragma unroll
+        for (int k = 0; k < CB; k++) x[k] = u2d(term.d[(size_t)bb[k] * a.d_stride + (size_t)t * N + m]);
       } else {
-        x = q.ext[(((size_t)b * a.beta + j) * a.next + t) * N + k];
-        if (KIND == 0) x = d2u_canon(__longlong_as_double((long long)x), mi.qd);
+#pragma unroll
+        for (int k = 0; k < CB; k++)
+          x[k] = __longlong_as_double((long long)term.ext[(((size_t)bb[k] * a.beta + j) * a.next + t) * N + m]);
       }
-      const u64* e = q.evk + ((size_t)j * 2 * a.nm + id) * N + n;
-      mac128(v0, x, e[0]);
-      mac128(v1, x, e[(size_t)a.nm * N]);
+      const double e0 = u2d(e[0]), e1 = u2d(e[comp]);
+#pragma unroll
+      for (int k = 0; k < CB; k++) {
+        v0[k] += fp_mulmod_var(x[k], e0, qinv, q);
+        v1[k] += fp_mulmod_var(x[k], e1, qinv, q);
+        if ((j & 3) == 3) v0[k] = fp_reduce(v0[k], qinv, q), v1[k] = fp_reduce(v1[k], qinv, q);   // at most 5 products below 0.9 q
+      }
     }
-    if (q.c0 && main_prime) mac128(v0, q.c0[(size_t)b * a.d_stride + (size_t)t * N + k], mi.pmod);
-    u64 r0 = reduce128(v0, mi), r1 = reduce128(v1, mi);
-    if (w) {
-      const u64 f = w[(size_t)(r + 1) * a.next * N];
-      r0 = mulmod(r0, f, mi);
-      r1 = mulmod(r1, f, mi);
+#pragma unroll
+    for (int k = 0; k < CB; k++) {
+      v0[k] = fp_reduce(v0[k], qinv, q);
+      v1[k] = fp_reduce(v1[k], qinv, q);
+      if (a.w) {
+        const double f = u2d(w[k][(size_t)(r + 1) * a.next * N]);
+        v0[k] = fp_mulmod_var(v0[k], f, qinv, q);
+        v1[k] = fp_mulmod_var(v1[k], f, qinv, q);
+      }
+      s0[k] = fp_reduce(s0[k] + v0[k], qinv, q);
+      s1[k] = fp_reduce(s1[k] + v1[k], qinv, q);
     }
-    s0 = addmod(s0, r0, m);
-    s1 = addmod(s1, r1, m);
   }
-  if (KIND == 1) {
-    s0 = csub(redc(Acc128{s0, 0}, m, mi.minv), m);
-    s1 = csub(redc(Acc128{s1, 0}, m, mi.minv), m);
+#pragma unroll
+  for (int k = 0; k < CB; k++) {
+    if (b0 + k >= a.B) break;
+    u64* to = a.acc + (((size_t)o * a.B + bb[k]) * 2 * a.next + t) * N + n;
+    if (a.accumulate) s0[k] += u2d(to[0]), s1[k] += u2d(to[(size_t)a.next * N]);
+    to[0] = d2u_canon(fp_reduce(s0[k], qinv, q), q);
+    to[(size_t)a.next * N] = d2u_canon(fp_reduce(s1[k], qinv, q), q);
   }
-  u64* o = a.acc + ((size_t)b * 2 * a.next + t) * N + n;
-  if (a.accumulate) {
-    s0 = addmod(s0, o[0], m);
-    s1 = addmod(s1, o[(size_t)a.next * N], m);
-  }
-  o[0] = s0;
-  o[(size_t)a.next * N] = s1;
 }
 
-// One operand of a sum of products: the ciphertext of output (i, j), term s. With `rotated` the index i, j or s that it names counts
-// the rotations of a ciphertext, the first of which (the ciphertext itself) lies at `first` and the others at `rest`, one
-// rotation after another.
-enum ProdIndex : u32 { PROD_NONE = 0, PROD_I = 1, PROD_J = 2, PROD_S = 3 };
+// All other moduli: residues in ext, Montgomery products, sums below 2m. PLAIN: acc without the factor 2^-64 (rings whose ModDown
+// takes none). Grid and lanes as above.
+template <int CB, bool PLAIN>
+__global__ void __launch_bounds__(256) rot_sum_int_kernel(RotSumArgs a) {
+  const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, comp = (size_t)a.nm * N;
+  u32 what, blk, zi;
+  attention_map(what, blk, zi);
+  const u32 groups = (a.B + CB - 1) / CB, o = what / groups, b0 = (what % groups) * CB;
+  const u32 n = blk * 256 + threadIdx.x, t = a.slots[zi];
+  const bool main_prime = t < a.nlimbs;
+  const u32 id = main_prime ? t : t - a.nlimbs + a.nq;
+  const ModInfo mi = a.mods[id];
+  const u64 q = mi.m, q2 = 2 * mi.m, r2 = a.w || PLAIN ? mont_r2(mi) : 0;
+  u32 bb[CB];
+  const u64* w[CB];
+  u64 s0[CB], s1[CB];
+#pragma unroll
+  for (int k = 0; k < CB; k++) {
+    bb[k] = min(b0 + k, a.B - 1);
+    w[k] = a.w ? a.w + (((size_t)(bb[k] / a.per_set) * a.w_terms + a.w_first) * a.next + t) * N + n : nullptr;
+    s0[k] = s1[k] = 0;
+    if (a.base && main_prime && o == 0) {
+      const u64* x = a.base + (size_t)bb[k] * a.base_stride + (size_t)t * N + n;
+      const u64 f = a.w ? mont_plain(*w[k], mi.pmod, r2, q, mi.minv) : mi.pmod;
+      s0[k] = mont_mul63(x[0], f, q, mi.minv);   // below 2m, with the factor 2^-64 like everything below
+      s1[k] = mont_mul63(x[pl], f, q, mi.minv);
+    }
+  }
+  const u32 jo = main_prime ? t / a.alpha : 0xFFFFFFFFu;
+  for (u32 r = 0; r < a.nterms; r++) {
+    const RotTerm& term = a.term[o * a.nterms + r];
+    const u32 m = galois_src_index(n, term.galois, a.logN);
+    const u64* e = term.evk + (size_t)id * N + n;
+    u64 v0[CB], v1[CB];
+#pragma unroll
+    for (int k = 0; k < CB; k++) {
+      v0[k] = v1[k] = 0;
+      if (term.c0 && main_prime) v0[k] = mont_mul63(term.c0[(size_t)bb[k] * a.d_stride + (size_t)t * N + m], mi.pmod, q, mi.minv);
+    }
+    for (u32 j = 0; j < a.beta; j++, e += 2 * comp) {
+      u64 x[CB];
+#pragma unroll
+      for (int k = 0; k < CB; k++)
+        x[k] = j == jo ? term.d[(size_t)bb[k] * a.d_stride + (size_t)t * N + m]
+                       : term.ext[(((size_t)bb[k] * a.beta + j) * a.next + t) * N + m];
+      const u64 e0 = e[0], e1 = e[comp];
+#pragma unroll
+      for (int k = 0; k < CB; k++) {
+        v0[k] = csub(v0[k] + mont_mul63(x[k], e0, q, mi.minv), q2);
+        v1[k] = csub(v1[k] + mont_mul63(x[k], e1, q, mi.minv), q2);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < CB; k++) {
+      if (a.w) {   // the weight times 2^64 makes up for this product's factor
+        const u64 f = csub(mont_mul63(w[k][(size_t)(r + 1) * a.next * N], r2, q, mi.minv), q);
+        v0[k] = mont_mul63(v0[k], f, q, mi.minv);
+        v1[k] = mont_mul63(v1[k], f, q, mi.minv);
+      }
+      s0[k] = csub(s0[k] + v0[k], q2);
+      s1[k] = csub(s1[k] + v1[k], q2);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < CB; k++) {
+    if (b0 + k >= a.B) break;
+    u64* to = a.acc + (((size_t)o * a.B + bb[k]) * 2 * a.next + t) * N + n;
+    if (PLAIN) s0[k] = mont_mul63(s0[k], r2, q, mi.minv), s1[k] = mont_mul63(s1[k], r2, q, mi.minv);
+    if (a.accumulate) s0[k] = csub(s0[k] + to[0], q2), s1[k] = csub(s1[k] + to[(size_t)a.next * N], q2);
+    to[0] = csub(s0[k], q);
+    to[(size_t)a.next * N] = csub(s1[k], q);
+  }
+}
+
+// An operand of a sum of products: the ciphertext for output index `idx` and term s. A rotated one counts by `idx` (1) or by s (2) the
+// rotations of a ciphertext, the first of which (the ciphertext itself) lies at `first` and the others at `rest`, one after another.
 struct ProdOperand {
   const u64 *first, *rest;
-  u64 step[4];   // in ciphertexts: [PROD_I], [PROD_J], [PROD_S] multiply the index; [0] is unused
+  u64 step, step_s;   // ciphertexts between two values of idx, of s
   u32 rotated;
 };
-// out[i][j][b] = sum_{s < ns} x(i, j, s)[b] * y(i, j, s)[b] in three components (+ add in the first two, or in all three)
+// out[i][j][b] = sum_{s < ns} x(j, s)[b] * y(i, s)[b] in three components (+ add in the first two, or in all three), for i0 <= i < i1 and
+// j0 <= j < j1. Products of moduli below 2^60 are kept as 128-bit sums, of those below 2^50 in doubles.
 struct ProdSumArgs {
   ProdOperand x, y;
   const u64* add;       // null: none; ciphertexts of add_comps components, in the order of the outputs
-  u64* out;             // [ni][nj][B][3][nlimbs][N]
+  const u64* fade;      // not null (nj = 1): every y is multiplied by it ([nlimbs][N]) where it lies, after it has been read
+  u64* out;             // [i1 - i0][j1 - j0][B][3][nlimbs][N]
   const ModInfo* mods;
-  u32 logN, nlimbs, B, nj, ns, add_comps, add_i;   // add_i: outputs with i below it have an addend
-  u32 o_first;          // the first output of the launch; out and add start at it
-  // triangles: outputs (i, j) with j <= i only, at i (i + 1) / 2 + j; or terms s <= i only, x's at i (i + 1) / 2 + s
+  u32 logN, nlimbs, B, i0, i1, j0, j1, ns, add_comps, add_i;   // add_i: outputs with i below it have an addend
+  // triangles: outputs j <= i only, pair (i, j) at place i (i + 1) / 2 + j, places tri_first .. tri_first + tri_out - 1; or terms s <= i
+  // only, y's at i (i + 1) / 2 + s - tri_first
   u32 tri_out, tri_sum;
-  u64 tri_base;         // the place in the triangle that x starts at
+  u64 tri_first;
+  unsigned char limbs[128];
 };
-__device__ __forceinline__ const u64* prod_operand(const ProdOperand& p, u32 i, u32 j, u32 s, u64 ct) {
-  const u32 r = p.rotated == PROD_I ? i : p.rotated == PROD_J ? j : p.rotated == PROD_S ? s : 0;
-  u64 at = p.step[PROD_I] * i + p.step[PROD_J] * j + p.step[PROD_S] * s;
-  if (p.rotated && r) return p.rest + (at - p.step[p.rotated]) * ct;
+__device__ __forceinline__ const u64* prod_operand(const ProdOperand& p, u32 idx, u32 s, u64 ct) {
+  const u64 at = p.step * idx + p.step_s * s;
+  if (p.rotated == 1 && idx) return p.rest + (at - p.step) * ct;
+  if (p.rotated == 2 && s) return p.rest + (at - p.step_s) * ct;
   return p.first + at * ct;
 }
 
-// grid = (N / 256, nlimbs, outputs * B)
+// Running sum of products of canonical residues of one modulus.
+template <bool FP>
+struct ProdAcc;
+template <>
+struct ProdAcc<true> {
+  double v = 0.0;
+  __device__ __forceinline__ void mac(u64 x, u64 y, const ModInfo& mi) { v += fp_mulmod_var(u2d(x), u2d(y), mi.qinv, mi.qd); }
+  __device__ __forceinline__ void fold(const ModInfo& mi) { v = fp_reduce(v, mi.qinv, mi.qd); }
+  __device__ __forceinline__ u64 value(const ModInfo& mi) const { return d2u_canon(fp_reduce(v, mi.qinv, mi.qd), mi.qd); }
+};
+template <>
+struct ProdAcc<false> {
+  Acc128 v = {0, 0};
+  __device__ __forceinline__ void mac(u64 x, u64 y, const ModInfo&) { mac128(v, x, y); }
+  __device__ __forceinline__ void fold(const ModInfo& mi) { v = Acc128{reduce128(v, mi), 0}; }
+  __device__ __forceinline__ u64 value(const ModInfo& mi) const { return reduce128(v, mi); }
+};
+template <bool FP>
+__device__ __forceinline__ u64 prod_mulmod(u64 x, u64 y, const ModInfo& mi) {
+  if (!FP) return mulmod(x, y, mi);
+  return d2u_canon(fp_mulmod_var(u2d(x), u2d(y), mi.qinv, mi.qd), mi.qd);
+}
+
+// A lane keeps one position of a tile of TI x TJ outputs, so that a word of x serves TI of them and a word of y TJ.
+// grid = (tiles * B, N / 256, limbs)
+template <bool FP, int TI, int TJ>
 __global__ void __launch_bounds__(256) prod_sum_kernel(ProdSumArgs a) {
   const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, ct = 2 * pl;
-  const u32 n = blockIdx.x * 256 + threadIdx.x, l = blockIdx.y, o = a.o_first + blockIdx.z / a.B, b = blockIdx.z % a.B;
-  u32 i = o / a.nj, j = o % a.nj;
+  u32 what, blk, zi;
+  attention_map(what, blk, zi);
+  const u32 n = blk * 256 + threadIdx.x, l = a.limbs[zi], b = what % a.B;
+  const u32 nj = a.j1 - a.j0, tj = (nj + TJ - 1) / TJ;
+  u32 tile = what / a.B, i = a.i0 + tile / tj * TI, j = a.j0 + tile % tj * TJ;
+  u64 place = (u64)(i - a.i0) * nj + (j - a.j0);   // of the tile's first output
   if (a.tri_out) {
+    const u64 pair = a.tri_first + tile;
     i = 0;
-    while ((i + 1) * (i + 2) / 2 <= o) i++;
-    j = o - i * (i + 1) / 2;
+    while ((u64)(i + 1) * (i + 2) / 2 <= pair) i++;
+    j = (u32)(pair - (u64)i * (i + 1) / 2);
+    place = tile;
   }
   const ModInfo mi = a.mods[l];
   const size_t at = (size_t)b * ct + (size_t)l * N + n;
-  Acc128 v0 = {0, 0}, v1 = {0, 0}, v2 = {0, 0};
+  ProdAcc<FP> v[TI][TJ][3];
   const u32 ns = a.tri_sum ? i + 1 : a.ns;
-  const u64 tri = a.tri_sum ? ((u64)i * (i + 1) / 2 - a.tri_base) * a.B * ct : 0;
+  const u64 tri = a.tri_sum ? ((u64)i * (i + 1) / 2 - a.tri_first) * a.B * ct : 0;
+  const u64 fade = a.fade ? a.fade[(size_t)l * N + n] : 0;
+  const u32 last_i = a.tri_out ? i : a.i1 - 1, last_j = a.tri_out ? j : a.j1 - 1;   // surplus places repeat the last output
   for (u32 s = 0; s < ns; s++) {
-    const u64* x = prod_operand(a.x, i, j, s, ct) + tri + at;
-    const u64* y = prod_operand(a.y, i, j, s, ct) + at;
-    const u64 x0 = x[0], x1 = x[pl], y0 = y[0], y1 = y[pl];
-    mac128(v0, x0, y0);
-    mac128(v1, x0, y1);
-    mac128(v1, x1, y0);
-    mac128(v2, x1, y1);
-    if ((s & 63) == 63) {   // at most 129 products below 2^120 in a sum
-      v0 = Acc128{reduce128(v0, mi), 0};
-      v1 = Acc128{reduce128(v1, mi), 0};
-      v2 = Acc128{reduce128(v2, mi), 0};
+    u64 x[TJ][2], y[TI][2];
+#pragma unroll
+    for (int f = 0; f < TJ; f++) {
+      const u64* p = prod_operand(a.x, min(j + f, last_j), s, ct) + at;
+      x[f][0] = p[0], x[f][1] = p[pl];
+    }
+#pragma unroll
+    for (int e = 0; e < TI; e++) {
+      const u64* p = prod_operand(a.y, min(i + e, last_i), s, ct) + tri + at;
+      y[e][0] = p[0], y[e][1] = p[pl];
+    }
+#pragma unroll
+    for (int e = 0; e < TI; e++) {
+      if (a.fade && i + e <= last_i) {
+        u64* p = const_cast<u64*>(prod_operand(a.y, i + e, s, ct)) + at;
+        p[0] = prod_mulmod<FP>(y[e][0], fade, mi), p[pl] = prod_mulmod<FP>(y[e][1], fade, mi);
+      }
+#pragma unroll
+      for (int f = 0; f < TJ; f++) {
+        v[e][f][0].mac(x[f][0], y[e][0], mi);
+        v[e][f][1].mac(x[f][0], y[e][1], mi);
+        v[e][f][1].mac(x[f][1], y[e][0], mi);
+        v[e][f][2].mac(x[f][1], y[e][1], mi);
+      }
+    }
+    // in doubles a sum takes 6 products below 0.9 q on top of a folded one, 128 bits take 130 products below 2^120
+    if (FP ? s % 3 == 2 : (s & 63) == 63) {
+#pragma unroll
+      for (int e = 0; e < TI; e++)
+#pragma unroll
+        for (int f = 0; f < TJ; f++)
+#pragma unroll
+          for (int c = 0; c < 3; c++) v[e][f][c].fold(mi);
     }
   }
-  u64 r0 = reduce128(v0, mi), r1 = reduce128(v1, mi), r2 = reduce128(v2, mi);
-  const size_t to = (size_t)blockIdx.z * 3 * pl + (size_t)l * N + n;
-  if (a.add && i < a.add_i) {
-    const u64* e = a.add + (size_t)blockIdx.z * a.add_comps * pl + (size_t)l * N + n;
-    r0 = addmod(r0, e[0], mi.m);
-    r1 = addmod(r1, e[pl], mi.m);
-    if (a.add_comps == 3) r2 = addmod(r2, e[2 * pl], mi.m);
-  }
-  a.out[to] = r0;
-  a.out[to + pl] = r1;
-  a.out[to + 2 * pl] = r2;
+#pragma unroll
+  for (int e = 0; e < TI; e++)
+#pragma unroll
+    for (int f = 0; f < TJ; f++) {
+      if (i + e > last_i || j + f > last_j) continue;
+      const size_t to = (place + (size_t)e * nj + f) * a.B + b;
+      u64* o = a.out + to * 3 * pl + (size_t)l * N + n;
+      const u64* g = a.add && i + e < a.add_i ? a.add + to * a.add_comps * pl + (size_t)l * N + n : nullptr;
+#pragma unroll
+      for (int c = 0; c < 3; c++) {
+        u64 r = v[e][f][c].value(mi);
+        if (g && (u32)c < a.add_comps) r = addmod(r, g[c * pl], mi.m);
+        o[c * pl] = r;
+      }
+    }
 }

@@ -93,7 +93,15 @@ RotSumArgs rot_sum_args(const ckks_ctx* c, const LevelTables* lt, u32 nlimbs, u6
   a.per_set = 1;
   return a;
 }
-int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st) {
+template <int CB>
+void launch_rot_sum_of(int kind, u32 outs, u32 slots, const RotSumArgs& a, hipStream_t st) {
+  const dim3 grid(outs * ((a.B + CB - 1) / CB), (1u << a.logN) / 256, slots), block(256);
+  if (kind == 0) hipLaunchKernelGGL(rot_sum_fp_kernel<CB>, grid, block, 0, st, a);
+  else if (kind == 1) hipLaunchKernelGGL((rot_sum_int_kernel<CB, false>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((rot_sum_int_kernel<CB, true>), grid, block, 0, st, a);
+}
+int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 outs = 1) {
+  a.B = B;
   const LimbMap emap = ext_map(c, a.nlimbs);
   for (int kind = 0; kind < 3; kind++) {
     u32 cnt = 0;
@@ -102,11 +110,10 @@ int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st) {
       if (k == kind) a.slots[cnt++] = (unsigned char)s;
     }
     if (!cnt) continue;
-    ProfScope ps(c, PK_ROT_SUM, st);
-    const dim3 grid(B, c->N / 256, cnt), block(256);
-    if (kind == 0) hipLaunchKernelGGL(rot_sum_kernel<0>, grid, block, 0, st, a);
-    else if (kind == 1) hipLaunchKernelGGL(rot_sum_kernel<1>, grid, block, 0, st, a);
-    else hipLaunchKernelGGL(rot_sum_kernel<2>, grid, block, 0, st, a);
+    ProfScope ps(c, kind ? PK_ROT_SUM_INT : PK_ROT_SUM, st);
+    if (B >= 3) launch_rot_sum_of<4>(kind, outs, cnt, a, st);
+    else if (B == 2) launch_rot_sum_of<2>(kind, outs, cnt, a, st);
+    else launch_rot_sum_of<1>(kind, outs, cnt, a, st);
   }
   HIP_TRY(hipGetLastError());
   return CKKS_OK;
@@ -156,7 +163,8 @@ struct LinAttn {
   u64 *rot_a, *rot_b;      // rotations 1.. of keys or queries, and of values
   u64 *d, *y, *p, *sums, *extra, *total;  // products in three components, ciphertexts, scores and their inner sums, the terms from
                                           // inside the chunk, the read's sum in the extended basis
-  char* ks;
+  u64* acc;                // accumulators of rotations, [slice][2][next][N]
+  char* ks;                // a key-switch workspace for `slice` ciphertexts
   size_t ks_bytes;
 
   void shape(const ckks_ctx* c_, u32 C_, u32 B_, u32 nlimbs_, u32 n1_, u32 n2_) {
@@ -180,34 +188,51 @@ struct LinAttn {
     sums = w.words(scores ? slice * ct : 0);
     extra = w.words(scores ? group * 3 * pl : 0);
     total = w.words(group * ext_ct);
-    // a key switch of `slice` ciphertexts, the polynomials that rotations of rings without gathering kernels need, and the accumulators
-    // of hoisted rotations that share a pass over the digits
-    ks_bytes = ckks_workspace_bytes(cc, CKKS_OP_HROT, slice, nlimbs, 0) + hoisted_extra();
+    acc = w.words(slice * ext_ct);
+    ks_bytes = ckks_workspace_bytes(cc, CKKS_OP_KEYSWITCH, slice, nlimbs, 0);
     ks = w.bytes(ks_bytes);
     return w.used;
   }
-  u32 shared_rotations() const { return std::min<u32>(8, std::max(n1, n2) - 1); }
-  size_t hoisted_extra() const {
-    return two_pass(cc) ? (size_t)shared_rotations() * slice * 2 * (nlimbs + cc->np) * cc->N * 8 : 0;
-  }
 
-  // out[r][..] = rotations of n ciphertexts, one rotation out_stride words after another
+  // out[r][..] = rotations of n ciphertexts, one rotation out_stride words after another. The digits are shared by all rotations of a
+  // ciphertext, and P sigma(c0) joins the accumulators, so that one ModDown serves all rotations of all ciphertexts at once
+  // (a ModDown of one ciphertext of 9 limbs at 2^16 takes 50 us, of seven 150).
   int rotate(u64* out, u64 out_stride, const u64* in, u32 n, const std::vector<u32>& elements, const u64* const* keys) {
     int rc;
     const u32 R = (u32)elements.size();
-    const size_t need = ckks_workspace_bytes(c, CKKS_OP_HROT, slice, nlimbs, 0);
-    for (u32 i = 0; i < n && R; i += slice) {
-      const u32 nb = std::min(slice, n - i);
-      if (two_pass(c)) {
-        if ((rc = hrot_hoisted16(c, out + i * ct, out_stride, in + i * ct, nb, nlimbs, elements.data(), keys, R, ks, st, nullptr, 0,
-                                 false, (u64*)(ks + need), shared_rotations())))
-          return rc;
-        continue;
+    if (!R) return CKKS_OK;
+    const u64 ext_ct = 2 * (u64)lt->next * c->N;
+    const u32 nb = std::min(n, std::max(1u, slice / R));
+    for (u32 i = 0; i < n; i += nb) {
+      const u32 cnt = std::min(nb, n - i), per = std::min<u32>(R, slice / cnt);
+      for (u32 r0 = 0; r0 < R; r0 += per) {
+        const u32 rots = std::min(per, R - r0);
+        if ((rc = rotations_apart(in + i * ct, cnt, elements.data() + r0, keys + r0, rots))) return rc;
+        if (out_stride == (u64)cnt * ct) {
+          if ((rc = ext_mod_down(c, lt, acc, out + r0 * out_stride, rots * cnt, nlimbs, ks, st))) return rc;
+          continue;
+        }
+        for (u32 r = 0; r < rots; r++)
+          if ((rc = ext_mod_down(c, lt, acc + (u64)r * cnt * ext_ct, out + (r0 + r) * out_stride + i * ct, cnt, nlimbs, ks, st)))
+            return rc;
       }
-      for (u32 r = 0; r < R; r++)
-        if ((rc = ckks_hrot(c, (uint64_t*)out + r * out_stride + i * ct, (const uint64_t*)in + i * ct, nb, nlimbs, elements[r],
-                            (const uint64_t*)keys[r], ks, ks_bytes, st)))
-          return rc;
+    }
+    return CKKS_OK;
+  }
+  // The accumulators of each rotation of n ciphertexts, at acc.
+  int rotations_apart(const u64* in, u32 n, const u32* elements, const u64* const* keys, u32 R) {
+    int rc;
+    const u64 ext_ct = 2 * (u64)lt->next * c->N;
+    if (two_pass(c))
+      return hrot_hoisted16(c, nullptr, 0, in, n, nlimbs, elements, keys, R, ks, st, acc, n * ext_ct);
+    if ((rc = ext_digits(c, lt, in + pl, ct, n, nlimbs, ks, st))) return rc;
+    const u64* ext = (const u64*)(ks + ks_layout(c, n, nlimbs).ext);
+    for (u32 r0 = 0; r0 < R; r0 += ROT_SUM_TERMS) {
+      RotSumArgs a = rot_sum_args(c, lt, nlimbs, acc + (u64)r0 * n * ext_ct, ct);
+      const u32 outs = std::min<u32>(ROT_SUM_TERMS, R - r0);
+      a.nterms = 1;
+      for (u32 r = 0; r < outs; r++) a.term[r] = RotTerm{ext, in + pl, in, keys[r0 + r], elements[r0 + r]};
+      if ((rc = launch_rot_sum(c, a, n, st, outs))) return rc;
     }
     return CKKS_OK;
   }
@@ -219,14 +244,29 @@ struct LinAttn {
         return rc;
     return CKKS_OK;
   }
-  int products(ProdSumArgs a, u32 first, u32 outputs) {
+  template <int TI, int TJ>
+  void launch_products(bool fp, u32 tiles, u32 cnt, const ProdSumArgs& a) {
+    const dim3 grid(tiles * B, c->N / 256, cnt), block(256);
+    if (fp) hipLaunchKernelGGL((prod_sum_kernel<true, TI, TJ>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((prod_sum_kernel<false, TI, TJ>), grid, block, 0, st, a);
+  }
+  int products(ProdSumArgs a) {
     a.mods = c->d_mods;
     a.logN = c->logN;
     a.nlimbs = nlimbs;
     a.B = B;
-    a.o_first = first;
-    ProfScope ps(c, PK_PROD_SUM, st);
-    hipLaunchKernelGGL(prod_sum_kernel, dim3(c->N / 256, nlimbs, outputs * B), dim3(256), 0, st, a);
+    for (int fp = 1; fp >= 0; fp--) {
+      u32 cnt = 0;
+      for (u32 l = 0; l < nlimbs; l++)
+        if ((c->logN <= 16 && host_class(c, c->mod[l]) == 0) == (fp == 1)) a.limbs[cnt++] = (unsigned char)l;
+      if (!cnt) continue;
+      ProfScope ps(c, PK_PROD_SUM, st);
+      const u32 ni = a.i1 - a.i0, nj = a.j1 - a.j0;
+      if (a.tri_out) launch_products<1, 1>(fp, a.tri_out, cnt, a);
+      else if (a.tri_sum || (ni == 1 && nj == 1)) launch_products<1, 1>(fp, ni * nj, cnt, a);
+      else if (nj == 1) launch_products<4, 1>(fp, (ni + 3) / 4, cnt, a);
+      else launch_products<2, 4>(fp, (ni + 1) / 2 * ((nj + 3) / 4), cnt, a);
+    }
     HIP_TRY(hipGetLastError());
     return CKKS_OK;
   }
@@ -238,20 +278,23 @@ struct LinAttn {
     if ((rc = rotate(rot_a, keyed * ct, k, C * B, baby, baby_keys))) return rc;
     if ((rc = rotate(rot_b, keyed * ct, v, C * B, value, value_keys))) return rc;
     ProdSumArgs a{};
-    a.x = ProdOperand{k, rot_a, {0, 0, keyed, B}, PROD_J};
-    a.y = ProdOperand{v, rot_b, {0, keyed, 0, B}, PROD_I};
-    a.nj = n1;
+    a.x = ProdOperand{k, rot_a, keyed, B, 1};
+    a.y = ProdOperand{v, rot_b, keyed, B, 1};
     a.ns = C;
     a.out = d;
     a.add_comps = 2;
     a.add_i = n2;
-    const u32 all = n1 * n2, per = slice / B;
-    for (u32 o = 0; o < all; o += per) {   // Relin(d) + S = Relin(d + (S, 0))
-      const u32 cnt = std::min(per, all - o);
-      a.add = state_in ? state_in + (u64)o * B * ct : nullptr;
-      if ((rc = products(a, o, cnt))) return rc;
-      if ((rc = relin(state_out + (u64)o * B * ct, d, (size_t)cnt * B))) return rc;
-    }
+    // whole rows of the state, as many as make a slice, or pieces of one row
+    const u32 rows = std::max(1u, slice / (n1 * B)), cols = std::min(n1, slice / B);
+    for (u32 g = 0; g < n2; g += rows)
+      for (u32 b = 0; b < n1; b += cols) {
+        a.i0 = g, a.i1 = std::min(n2, g + rows);
+        a.j0 = b, a.j1 = std::min(n1, b + cols);
+        const u64 at = ((u64)g * n1 + b) * B * ct;
+        a.add = state_in ? state_in + at : nullptr;   // Relin(d) + S = Relin(d + (S, 0))
+        if ((rc = products(a))) return rc;
+        if ((rc = relin(state_out + at, d, (size_t)(a.i1 - a.i0) * (a.j1 - a.j0) * B))) return rc;
+      }
     return decay ? multiply(state_out, decay) : CKKS_OK;
   }
   int multiply(u64* state, const u64* decay) {
@@ -264,23 +307,26 @@ struct LinAttn {
     return CKKS_OK;
   }
 
-  // o of tokens [t0, t0 + T), T <= tokens: see the header. extra (three components) holds these tokens' terms from inside the chunk.
-  int read(u64* o, const u64* q, u32 T, const u64* state, const u64* extra) {
+  // o of T <= tokens tokens: see the header. extra (three components) holds their terms from inside the chunk. fade (T = 1): the state is
+  // multiplied by it where it lies, once it has been read, which saves the product a pass of its own its read of the state.
+  int read(u64* o, const u64* q, u32 T, const u64* state, const u64* extra, const u64* fade = nullptr) {
     int rc;
     const u32 n = T * B;
     const u64* d0 = extra;
     if (state) {
       if ((rc = rotate(rot_a, (u64)n * ct, q, n, baby, baby_keys))) return rc;
       ProdSumArgs a{};
-      a.x = ProdOperand{q, rot_a, {0, 0, B, n}, PROD_S};
-      a.y = ProdOperand{state, nullptr, {0, (u64)n1 * B, 0, B}, PROD_NONE};
-      a.nj = T;
+      a.x = ProdOperand{q, rot_a, B, n, 2};
+      a.y = ProdOperand{state, nullptr, (u64)n1 * B, B, 0};
+      a.i1 = n2;
+      a.j1 = T;
       a.ns = n1;
+      a.fade = fade;
       a.out = d;
       a.add = extra;
       a.add_comps = 3;
       a.add_i = 1;
-      if ((rc = products(a, 0, n2 * T))) return rc;
+      if ((rc = products(a))) return rc;
       d0 = d;
       if ((rc = relin(y, d + (u64)n * 3 * pl, (size_t)(n2 - 1) * n))) return rc;
     }
@@ -330,16 +376,17 @@ struct LinAttn {
       }
       const u64 first = (u64)t * (t + 1) / 2;
       ProdSumArgs a{};
-      a.x = ProdOperand{q, nullptr, {0, B, 0, 0}, PROD_NONE};
-      a.y = ProdOperand{k, nullptr, {0, 0, B, 0}, PROD_NONE};
-      a.nj = 1;
+      a.x = ProdOperand{k, nullptr, B, 0, 0};
+      a.y = ProdOperand{q, nullptr, B, 0, 0};
+      a.j1 = a.i1 = 1;
       a.ns = 1;
-      a.tri_out = 1;
       const u32 per = slice / B;
       for (u64 i = 0; i < pairs; i += per) {
         const u32 cnt = (u32)std::min<u64>(per, pairs - i);
         a.out = d;
-        if ((rc = products(a, (u32)(first + i), cnt))) return rc;
+        a.tri_first = first + i;
+        a.tri_out = cnt;
+        if ((rc = products(a))) return rc;
         u64* to = p + i * B * ct;
         u64* stage = n1 > 1 || n2 > 1 ? y : to;
         if ((rc = relin(stage, d, (size_t)cnt * B))) return rc;
@@ -351,13 +398,15 @@ struct LinAttn {
         if (n2 > 1 && (rc = sum_rotations(to, stage, cnt * B, giant, giant_keys))) return rc;
       }
       ProdSumArgs e{};
-      e.x = ProdOperand{p, nullptr, {0, 0, 0, B}, PROD_NONE};
-      e.y = ProdOperand{v, nullptr, {0, 0, 0, B}, PROD_NONE};
-      e.nj = 1;
+      e.x = ProdOperand{v, nullptr, 0, B, 0};
+      e.y = ProdOperand{p, nullptr, 0, B, 0};
+      e.i0 = t;
+      e.i1 = u;
+      e.j1 = 1;
       e.tri_sum = 1;
-      e.tri_base = first;
+      e.tri_first = first;
       e.out = out + (u64)(t - t0) * B * 3 * pl;
-      if ((rc = products(e, t, u - t))) return rc;
+      if ((rc = products(e))) return rc;
       t = u;
     }
     return CKKS_OK;
@@ -426,8 +475,7 @@ int linattn_run(bool chunk, ckks_ctx* c, const LinAttnCall& io, u32 C, u32 B, u3
   u64 *o = (u64*)io.o_out, *out = (u64*)io.state_out;
   if (!chunk) {
     if ((rc = f.update(out, S, k, v, nullptr))) return rc;
-    if ((rc = f.read(o, q, 1, out, nullptr))) return rc;
-    return decay ? f.multiply(out, decay) : CKKS_OK;
+    return f.read(o, q, 1, out, nullptr, decay);
   }
   for (u32 t = 0; t < C; t += f.tokens) {   // all reads of the old state come before the update, which may overwrite it
     const u32 T = std::min(f.tokens, C - t);
