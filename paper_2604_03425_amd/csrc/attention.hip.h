@@ -331,3 +331,14 @@ __global__ void __launch_bounds__(256) prod_sum_kernel(ProdSumArgs a) {
       }
     }
 }
+
+// Up to three batches of ciphertexts one after another: out[k] = in[k] for k < gridDim.y, `words` 16-byte words each.
+struct GatherArgs {
+  const ulonglong2* in[3];
+  ulonglong2* out;
+  size_t words;
+};
+__global__ void __launch_bounds__(256) gather_kernel(GatherArgs a) {
+  const size_t i = blockIdx.x * (size_t)256 + threadIdx.x;
+  if (i < a.words) a.out[blockIdx.y * a.words + i] = a.in[blockIdx.y][i];
+}

@@ -30,10 +30,8 @@ u32 rotation_element(const ckks_ctx* c, u64 steps) {   // 5^steps mod 2N
 // d + b * d_stride + t * N. Doubles on the double-precision moduli of the two-pass rings, canonical residues elsewhere.
 int ext_digits(ckks_ctx* c, const LevelTables* lt, const u64* d, u64 d_stride, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
   int rc;
-  if (two_pass(c)) {
-    FwdInnerArgs ia;
-    return hoist_front16(c, lt, d, d_stride, B, nlimbs, ws, st, ia);
-  }
+  FwdInnerArgs unused;
+  if (two_pass(c)) return hoist_front16(c, lt, d, d_stride, B, nlimbs, ws, st, unused);
   const u32 N = c->N, next = lt->next, beta = lt->beta;
   const KsLayout L = ks_layout(c, B, nlimbs);
   u64 *dcoef = (u64*)(ws + L.dcoef), *ext = (u64*)(ws + L.ext);
@@ -146,7 +144,7 @@ int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, const u64* ct, u32 B, u
 // ---- linear attention ----
 // Ciphertexts that one key switch of the calls below works on at a time: at least the B of a token. Enough to fill the chip
 // many times over; more would only take workspace.
-u32 linattn_slice(const ckks_ctx* c, u32 B) { return std::max<u32>(B, 64u << (c->logN < 16 ? 16 - c->logN : 0)); }
+u32 linattn_slice(const ckks_ctx* c, u32 B) { return std::max<u32>(B, std::min(1024u, 128u << (c->logN < 16 ? 16 - c->logN : 0))); }
 
 struct LinAttn {
   const ckks_ctx* cc;      // for sizes
@@ -161,6 +159,8 @@ struct LinAttn {
   hipStream_t st;
   // workspace
   u64 *rot_a, *rot_b;      // rotations 1.. of keys or queries, and of values
+  const u64 *q_rest = nullptr, *k_rest = nullptr, *v_rest = nullptr;   // those of all three, where a call makes them at once
+  u32 turn_step = 0;       // ciphertexts from one rotation of a key to the next
   u64 *d, *y, *p, *sums, *extra, *total;  // products in three components, ciphertexts, scores and their inner sums, the terms from
                                           // inside the chunk, the read's sum in the extended basis
   u64* acc;                // accumulators of rotations, [slice][2][next][N]
@@ -179,9 +179,9 @@ struct LinAttn {
     const u64 ext_ct = 2 * (u64)(nlimbs + cc->np) * cc->N;
     const size_t group = (size_t)tokens * B;               // ciphertexts of the read's queries at a time
     const size_t keyed = (size_t)C * B;
-    rot_a = w.words((n1 - 1) * keyed * ct);
+    rot_a = w.words(std::max<size_t>((n1 - 1) * keyed, joint(true) || joint(false) ? slice : 0) * ct);
     rot_b = w.words((n2 - 1) * keyed * ct);
-    const size_t most = std::max<size_t>({(size_t)slice, group * n2, scores ? keyed : 0});
+    const size_t most = std::max<size_t>({(size_t)slice, group * n2, scores ? keyed : 0});   // (a call's inputs side by side too)
     d = w.words(most * 3 * pl);
     y = w.words(most * ct);
     p = w.words(scores ? std::max<size_t>(slice, keyed) * ct : 0);
@@ -205,9 +205,11 @@ struct LinAttn {
     const u32 nb = std::min(n, std::max(1u, slice / R));
     for (u32 i = 0; i < n; i += nb) {
       const u32 cnt = std::min(nb, n - i), per = std::min<u32>(R, slice / cnt);
-      for (u32 r0 = 0; r0 < R; r0 += per) {
+      const u64* ext = (const u64*)(ks + ks_layout(c, cnt, nlimbs).ext);
+      for (u32 r0 = 0; r0 < R; r0 += per) {   // (ModDown's scratch takes the digits' place, so a further pass converts again)
+        if ((rc = ext_digits(c, lt, in + i * ct + pl, ct, cnt, nlimbs, ks, st))) return rc;
         const u32 rots = std::min(per, R - r0);
-        if ((rc = rotations_apart(in + i * ct, cnt, elements.data() + r0, keys + r0, rots))) return rc;
+        if ((rc = rotations_apart(acc, ext, in + i * ct, cnt, elements.data() + r0, keys + r0, rots))) return rc;
         if (out_stride == (u64)cnt * ct) {
           if ((rc = ext_mod_down(c, lt, acc, out + r0 * out_stride, rots * cnt, nlimbs, ks, st))) return rc;
           continue;
@@ -219,21 +221,56 @@ struct LinAttn {
     }
     return CKKS_OK;
   }
-  // The accumulators of each rotation of n ciphertexts, at acc.
-  int rotations_apart(const u64* in, u32 n, const u32* elements, const u64* const* keys, u32 R) {
+  // The accumulators of each rotation of n ciphertexts `in`, whose digits are at `ext`, rotation by rotation.
+  int rotations_apart(u64* to, const u64* ext, const u64* in, u32 n, const u32* elements, const u64* const* keys, u32 R) {
     int rc;
-    const u64 ext_ct = 2 * (u64)lt->next * c->N;
-    if (two_pass(c))
-      return hrot_hoisted16(c, nullptr, 0, in, n, nlimbs, elements, keys, R, ks, st, acc, n * ext_ct);
-    if ((rc = ext_digits(c, lt, in + pl, ct, n, nlimbs, ks, st))) return rc;
-    const u64* ext = (const u64*)(ks + ks_layout(c, n, nlimbs).ext);
-    for (u32 r0 = 0; r0 < R; r0 += ROT_SUM_TERMS) {
-      RotSumArgs a = rot_sum_args(c, lt, nlimbs, acc + (u64)r0 * n * ext_ct, ct);
-      const u32 outs = std::min<u32>(ROT_SUM_TERMS, R - r0);
+    const u64 stride = n * 2 * (u64)lt->next * c->N;
+    const bool streamed = two_pass(c) && lt->beta <= INNER16_ROT_MAX_BETA;   // keeps the digits of a position for all rotations
+    const u32 most = streamed ? KS_MULTI_MAX : ROT_SUM_TERMS;
+    for (u32 r0 = 0; r0 < R; r0 += most) {
+      const u32 rots = std::min(most, R - r0);
+      if (streamed) {
+        FwdInnerArgs ia = hoisted_args(c, lt, in + pl, ct, ext, nlimbs);
+        ia.c0 = in;
+        ia.c0_poly_stride = ct;
+        if ((rc = launch_inner_rot(c, lt, ia, n, nlimbs, elements + r0, keys + r0, rots, to + r0 * stride, stride, st))) return rc;
+        continue;
+      }
+      RotSumArgs a = rot_sum_args(c, lt, nlimbs, to + r0 * stride, ct);
       a.nterms = 1;
-      for (u32 r = 0; r < outs; r++) a.term[r] = RotTerm{ext, in + pl, in, keys[r0 + r], elements[r0 + r]};
-      if ((rc = launch_rot_sum(c, a, n, st, outs))) return rc;
+      for (u32 r = 0; r < rots; r++) a.term[r] = RotTerm{ext, in + pl, in, keys[r0 + r], elements[r0 + r]};
+      if ((rc = launch_rot_sum(c, a, n, st, rots))) return rc;
     }
+    return CKKS_OK;
+  }
+  // All rotations of a call at once, where they are few: queries (if the state is read), keys and values side by side go through one
+  // decomposition and one ModDown, which takes a third of the launches.
+  bool joint(bool with_q) const {
+    const u64 baby_cts = (with_q ? 2 : 1) * (u64)(n1 - 1), all = (baby_cts + n2 - 1) * C * B;
+    return all && all <= slice && (with_q ? 3u : 2u) * (u64)C * B <= slice;
+  }
+  int rotate_all(const u64* q, const u64* k, const u64* v, bool with_q) {
+    int rc;
+    const u32 n = C * B, turned = (with_q ? 2 : 1) * n;   // ciphertexts that take the baby steps
+    const u64 ext_ct = 2 * (u64)lt->next * c->N;
+    GatherArgs g{{(const ulonglong2*)(with_q ? q : k), (const ulonglong2*)(with_q ? k : v), (const ulonglong2*)v}, (ulonglong2*)d, n * ct / 2};
+    {
+      ProfScope ps(c, PK_ADD, st);
+      hipLaunchKernelGGL(gather_kernel, dim3((unsigned)((g.words + 255) / 256), with_q ? 3 : 2), dim3(256), 0, st, g);
+      HIP_TRY(hipGetLastError());
+    }
+    if ((rc = ext_digits(c, lt, d + pl, ct, turned + n, nlimbs, ks, st))) return rc;
+    const u64* ext = (const u64*)(ks + ks_layout(c, turned + n, nlimbs).ext);
+    u64* to = acc;
+    if ((rc = rotations_apart(to, ext, d, turned, baby.data(), baby_keys, n1 - 1))) return rc;
+    to += (u64)(n1 - 1) * turned * ext_ct;
+    if ((rc = rotations_apart(to, ext + (u64)turned * lt->beta * lt->next * c->N, d + (u64)turned * ct, n, value.data(), value_keys, n2 - 1)))
+      return rc;
+    if ((rc = ext_mod_down(c, lt, acc, rot_a, (n1 - 1) * turned + (n2 - 1) * n, nlimbs, ks, st))) return rc;
+    q_rest = rot_a;
+    k_rest = rot_a + (with_q ? n * ct : 0);
+    v_rest = rot_a + (u64)(n1 - 1) * turned * ct;
+    turn_step = turned;
     return CKKS_OK;
   }
   int relin(u64* out, const u64* in, size_t n) {
@@ -275,11 +312,13 @@ struct LinAttn {
   int update(u64* state_out, const u64* state_in, const u64* k, const u64* v, const u64* decay) {
     int rc;
     const u64 keyed = (u64)C * B;
-    if ((rc = rotate(rot_a, keyed * ct, k, C * B, baby, baby_keys))) return rc;
-    if ((rc = rotate(rot_b, keyed * ct, v, C * B, value, value_keys))) return rc;
+    if (!k_rest) {
+      if ((rc = rotate(rot_a, keyed * ct, k, C * B, baby, baby_keys))) return rc;
+      if ((rc = rotate(rot_b, keyed * ct, v, C * B, value, value_keys))) return rc;
+    }
     ProdSumArgs a{};
-    a.x = ProdOperand{k, rot_a, keyed, B, 1};
-    a.y = ProdOperand{v, rot_b, keyed, B, 1};
+    a.x = ProdOperand{k, k_rest ? k_rest : rot_a, k_rest ? turn_step : keyed, B, 1};
+    a.y = ProdOperand{v, k_rest ? v_rest : rot_b, keyed, B, 1};
     a.ns = C;
     a.out = d;
     a.add_comps = 2;
@@ -314,9 +353,9 @@ struct LinAttn {
     const u32 n = T * B;
     const u64* d0 = extra;
     if (state) {
-      if ((rc = rotate(rot_a, (u64)n * ct, q, n, baby, baby_keys))) return rc;
+      if (!q_rest && (rc = rotate(rot_a, (u64)n * ct, q, n, baby, baby_keys))) return rc;
       ProdSumArgs a{};
-      a.x = ProdOperand{q, rot_a, B, n, 2};
+      a.x = ProdOperand{q, q_rest ? q_rest : rot_a, B, q_rest ? turn_step : n, 2};
       a.y = ProdOperand{state, nullptr, (u64)n1 * B, B, 0};
       a.i1 = n2;
       a.j1 = T;
@@ -473,6 +512,8 @@ int linattn_run(bool chunk, ckks_ctx* c, const LinAttnCall& io, u32 C, u32 B, u3
   }
   const u64 *q = (const u64*)io.q, *k = (const u64*)io.k, *v = (const u64*)io.v, *S = (const u64*)io.state_in, *decay = (const u64*)io.decay;
   u64 *o = (u64*)io.o_out, *out = (u64*)io.state_out;
+  const bool with_q = !chunk || S;
+  if (f.joint(with_q) && (rc = f.rotate_all(q, k, v, with_q))) return rc;
   if (!chunk) {
     if ((rc = f.update(out, S, k, v, nullptr))) return rc;
     return f.read(o, q, 1, out, nullptr, decay);

@@ -1499,6 +1499,26 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
   return CKKS_OK;
 }
 
+// Arguments of the streaming inner-product kernels for hoisted digits (all but the accumulators).
+static FwdInnerArgs hoisted_args(const ckks_ctx* c, const LevelTables* lt, const u64* d, u64 d_stride, const u64* ext, u32 nlimbs) {
+  FwdInnerArgs ia;
+  ia.ext = ext;
+  ia.d = d;
+  ia.d_poly_stride = d_stride;
+  ia.tw = c->d_tw_fwd;
+  ia.twfp = c->d_twfp_fwd;
+  ia.mods = c->d_mods;
+  ia.logN = c->logN;
+  ia.nlimbs = nlimbs;
+  ia.nq = c->nq;
+  ia.nm = c->nm;
+  ia.alpha = c->alpha;
+  ia.beta = lt->beta;
+  ia.next = lt->next;
+  ia.map_mode = map_mode_inner(c, true);
+  return ia;
+}
+
 // Shared front of the hoisted rotations: inverse transform, ModUp and forward transform of B polynomials (limb-vector (b, t) at
 // d + b*d_stride + t*N) into the workspace, and the arguments of the streaming inner-product kernels that read them
 // (accumulators default to the workspace's own).
@@ -1510,7 +1530,6 @@ static int hoist_front16(ckks_ctx* c, const LevelTables* lt, const u64* d, u64 d
   KsLayout L = ks_layout(c, B, nlimbs);
   u64* dcoef = (u64*)(ws + L.dcoef);
   u64* ext = (u64*)(ws + L.ext);
-  u64* acc = (u64*)(ws + L.acc);
   const LimbMap qmap = identity_map(nlimbs), emap = ext_map(c, nlimbs);
   NttOpts o1, of;
   o1.scale = lt->up_scale;
@@ -1532,21 +1551,42 @@ static int hoist_front16(ckks_ctx* c, const LevelTables* lt, const u64* d, u64 d
   of.raw_out = true;  // reduced doubles on double-precision moduli, canonical residues elsewhere
   if ((rc = launch_ntt(c, false, ext, (u64)next * N, ext, (u64)next * N, B * beta, 0, next, emap, beta, nlimbs, st, of)))
     return rc;
-  ia.ext = ext;
-  ia.d = d;
-  ia.d_poly_stride = d_stride;
-  ia.acc = acc;
-  ia.tw = c->d_tw_fwd;
-  ia.twfp = c->d_twfp_fwd;
-  ia.mods = c->d_mods;
-  ia.logN = c->logN;
-  ia.nlimbs = nlimbs;
-  ia.nq = c->nq;
-  ia.nm = c->nm;
-  ia.alpha = c->alpha;
-  ia.beta = beta;
-  ia.next = next;
-  ia.map_mode = map_mode_inner(c, true);
+  ia = hoisted_args(c, lt, d, d_stride, ext, nlimbs);
+  ia.acc = (u64*)(ws + L.acc);
+  return CKKS_OK;
+}
+
+// Several rotations per pass over the hoisted digits that ia describes (nr <= KS_MULTI_MAX, at most INNER16_ROT_MAX_BETA digits):
+// accumulators of rotation r to dst + r * stride.
+static int launch_inner_rot(const ckks_ctx* c, const LevelTables* lt, FwdInnerArgs ia, u32 B, u32 nlimbs, const u32* galois,
+                            const u64* const* evks, u32 nr, u64* dst, u64 stride, hipStream_t st) {
+  const u32 N = c->N, next = lt->next, beta = lt->beta;
+  const LimbMap emap = ext_map(c, nlimbs);
+  ia.acc = dst;
+  ia.acc_rot_stride = stride;
+  ia.nrot = nr;
+  for (u32 r = 0; r < nr; r++) {
+    ia.galois_pc[r] = inv_mod_pow2(galois[r], c->logN + 1);
+    ia.evk_pc[r] = evks[r];
+  }
+  for (int fp = 1; fp >= 0; fp--) {
+    FwdInnerArgs a = ia;
+    u32 cnt = 0;
+    for (u32 s_ = 0; s_ < next; s_++)
+      if ((host_class(c, c->mod[emap.id[s_]]) == 0) == (fp == 1)) a.slots[cnt++] = (unsigned char)s_;
+    if (!cnt) continue;
+    ProfScope ps(c, fp ? PK_INNER16 : PK_INNER16_INT, st);
+    const u32 cb = fp ? INNER16_ROT_CB_FP : INNER16_ROT_CB;
+    const dim3 grid((B + cb - 1) / cb, N / 256, cnt);
+    if (fp && beta == 1) hipLaunchKernelGGL((inner16_rot_fp_kernel<1, true>), grid, dim3(256), 0, st, a, B);
+    else if (fp && beta == 2) hipLaunchKernelGGL((inner16_rot_fp_kernel<2, true>), grid, dim3(256), 0, st, a, B);
+    else if (fp && beta == 3) hipLaunchKernelGGL((inner16_rot_fp_kernel<3, true>), grid, dim3(256), 0, st, a, B);
+    else if (fp && beta == 4) hipLaunchKernelGGL((inner16_rot_fp_kernel<4, true>), grid, dim3(256), 0, st, a, B);
+    else if (fp) hipLaunchKernelGGL((inner16_rot_fp_kernel<INNER16_ROT_MAX_BETA, false>), grid, dim3(256), 0, st, a, B);
+    else if (beta <= 4) hipLaunchKernelGGL(inner16_rot_int_kernel<4>, grid, dim3(256), 0, st, a, B);
+    else hipLaunchKernelGGL(inner16_rot_int_kernel<INNER16_ROT_MAX_BETA>, grid, dim3(256), 0, st, a, B);
+  }
+  HIP_TRY(hipGetLastError());
   return CKKS_OK;
 }
 
@@ -1576,35 +1616,8 @@ int hrot_hoisted16(ckks_ctx* c, u64* out_base, u64 out_stride, const u64* ct_in,
     ia.c0_poly_stride = 2 * polyN;
     ia.accumulate = acc_add ? 1u : 0u;
   }
-  // several rotations per pass over the digits (at most KS_MULTI_MAX): accumulators of rotations r0 .. r0+nr-1 to
-  // dst + k * stride
   auto launch_rot = [&](u32 r0, u32 nr, u64* dst, u64 stride) -> int {
-      ia.acc = dst;
-      ia.acc_rot_stride = stride;
-      ia.nrot = nr;
-      for (u32 r = 0; r < nr; r++) {
-        ia.galois_pc[r] = inv_mod_pow2(galois[r0 + r], c->logN + 1);
-        ia.evk_pc[r] = evks[r0 + r];
-      }
-      for (int fp = 1; fp >= 0; fp--) {
-        FwdInnerArgs a = ia;
-        u32 cnt = 0;
-        for (u32 s_ = 0; s_ < next; s_++)
-          if ((host_class(c, c->mod[emap.id[s_]]) == 0) == (fp == 1)) a.slots[cnt++] = (unsigned char)s_;
-        if (!cnt) continue;
-        ProfScope ps(c, fp ? PK_INNER16 : PK_INNER16_INT, st);
-        const u32 cb = fp ? INNER16_ROT_CB_FP : INNER16_ROT_CB;
-        const dim3 grid((B + cb - 1) / cb, N / 256, cnt);
-        if (fp && beta == 1) hipLaunchKernelGGL((inner16_rot_fp_kernel<1, true>), grid, dim3(256), 0, st, a, B);
-        else if (fp && beta == 2) hipLaunchKernelGGL((inner16_rot_fp_kernel<2, true>), grid, dim3(256), 0, st, a, B);
-        else if (fp && beta == 3) hipLaunchKernelGGL((inner16_rot_fp_kernel<3, true>), grid, dim3(256), 0, st, a, B);
-        else if (fp && beta == 4) hipLaunchKernelGGL((inner16_rot_fp_kernel<4, true>), grid, dim3(256), 0, st, a, B);
-        else if (fp) hipLaunchKernelGGL((inner16_rot_fp_kernel<INNER16_ROT_MAX_BETA, false>), grid, dim3(256), 0, st, a, B);
-        else if (beta <= 4) hipLaunchKernelGGL(inner16_rot_int_kernel<4>, grid, dim3(256), 0, st, a, B);
-        else hipLaunchKernelGGL(inner16_rot_int_kernel<INNER16_ROT_MAX_BETA>, grid, dim3(256), 0, st, a, B);
-      }
-      HIP_TRY(hipGetLastError());
-      return CKKS_OK;
+    return launch_inner_rot(c, lt, ia, B, nlimbs, galois + r0, evks + r0, nr, dst, stride, st);
   };
   if (acc_base && !acc_add && beta <= INNER16_ROT_MAX_BETA) {
     for (u32 r0 = 0; r0 < R; r0 += KS_MULTI_MAX) {

@@ -135,6 +135,13 @@ def test_work_in_slices():
     _run("chunk", "ring16", 2, 40, 3, 2, 1, True, False, check=[0, 39])
 
 
+def test_work_in_more_slices():
+    """Several slices at each place: rows of the state that make one and a half, pieces of a row, tokens one slice after another."""
+    _run("step", "ring16", 2, 24, 1, 3, 3, True, True, check=[0, 23])
+    _run("step", "ring16", 1, 100, 1, 2, 1, True, False, check=[0, 99])
+    _run("chunk", "ring16", 1, 50, 3, 2, 1, True, True, check=[0, 49])
+
+
 def test_a_chunk_of_one_token_and_a_longer_one_agree():
     """Outputs depend on no later token."""
     import paper_2604_03425_amd as ck
