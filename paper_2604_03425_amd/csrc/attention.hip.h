@@ -1,7 +1,7 @@
 // Kernels of softmax-free attention on ciphertexts: weighted sums of rotations in the extended basis (rotary positions, slot
 // sums, the giant steps of a state's read) and sums of ciphertext products (scores, the state's update and read).
 #pragma once
-#include "modarith.hip.h"
+#include "ntt16_kernels.hip.h"
 
 #define ROT_SUM_TERMS 32   // terms per launch (they travel in the kernel's arguments)
 
@@ -202,13 +202,6 @@ __global__ void __launch_bounds__(256) rot_sum_int_kernel(RotSumArgs a) {
   }
 }
 
-// An operand of a sum of products: the ciphertext for output index `idx` and term s. A rotated one counts by `idx` (1) or by s (2) the
-// rotations of a ciphertext, the first of which (the ciphertext itself) lies at `first` and the others at `rest`, one after another.
-struct ProdOperand {
-  const u64 *first, *rest;
-  u64 step, step_s;   // ciphertexts between two values of idx, of s
-  u32 rotated;
-};
 // out[i][j][b] = sum_{s < ns} x(j, s)[b] * y(i, s)[b] in three components (+ add in the first two, or in all three), for i0 <= i < i1 and
 // j0 <= j < j1. Products of moduli below 2^60 are kept as 128-bit sums, of those below 2^50 in doubles.
 struct ProdSumArgs {
@@ -224,13 +217,6 @@ struct ProdSumArgs {
   u64 tri_first;
   unsigned char limbs[128];
 };
-__device__ __forceinline__ const u64* prod_operand(const ProdOperand& p, u32 idx, u32 s, u64 ct) {
-  const u64 at = p.step * idx + p.step_s * s;
-  if (p.rotated == 1 && idx) return p.rest + (at - p.step) * ct;
-  if (p.rotated == 2 && s) return p.rest + (at - p.step_s) * ct;
-  return p.first + at * ct;
-}
-
 // Running sum of products of canonical residues of one modulus.
 template <bool FP>
 struct ProdAcc;
@@ -254,9 +240,10 @@ __device__ __forceinline__ u64 prod_mulmod(u64 x, u64 y, const ModInfo& mi) {
   return d2u_canon(fp_mulmod_var(u2d(x), u2d(y), mi.qinv, mi.qd), mi.qd);
 }
 
-// A lane keeps one position of a tile of TI x TJ outputs, so that a word of x serves TI of them and a word of y TJ.
+// A lane keeps one position of a tile of TI x TJ outputs, so that a word of x serves TI of them and a word of y TJ. FIRST = 2: only the
+// third component of every product, [i1 - i0][j1 - j0][B][nlimbs][N].
 // grid = (tiles * B, N / 256, limbs)
-template <bool FP, int TI, int TJ>
+template <bool FP, int TI, int TJ, int FIRST>
 __global__ void __launch_bounds__(256) prod_sum_kernel(ProdSumArgs a) {
   const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, ct = 2 * pl;
   u32 what, blk, zi;
@@ -274,7 +261,8 @@ __global__ void __launch_bounds__(256) prod_sum_kernel(ProdSumArgs a) {
   }
   const ModInfo mi = a.mods[l];
   const size_t at = (size_t)b * ct + (size_t)l * N + n;
-  ProdAcc<FP> v[TI][TJ][3];
+  constexpr int NC = 3 - FIRST;
+  ProdAcc<FP> v[TI][TJ][NC];
   const u32 ns = a.tri_sum ? i + 1 : a.ns;
   const u64 tri = a.tri_sum ? ((u64)i * (i + 1) / 2 - a.tri_first) * a.B * ct : 0;
   const u64 fade = a.fade ? a.fade[(size_t)l * N + n] : 0;
@@ -299,10 +287,12 @@ __global__ void __launch_bounds__(256) prod_sum_kernel(ProdSumArgs a) {
       }
 #pragma unroll
       for (int f = 0; f < TJ; f++) {
-        v[e][f][0].mac(x[f][0], y[e][0], mi);
-        v[e][f][1].mac(x[f][0], y[e][1], mi);
-        v[e][f][1].mac(x[f][1], y[e][0], mi);
-        v[e][f][2].mac(x[f][1], y[e][1], mi);
+        if (FIRST == 0) {
+          v[e][f][0].mac(x[f][0], y[e][0], mi);
+          v[e][f][1 % NC].mac(x[f][0], y[e][1], mi);
+          v[e][f][1 % NC].mac(x[f][1], y[e][0], mi);
+        }
+        v[e][f][NC - 1].mac(x[f][1], y[e][1], mi);
       }
     }
     // in doubles a sum takes 6 products below 0.9 q on top of a folded one, 128 bits take 130 products below 2^120
@@ -312,7 +302,7 @@ __global__ void __launch_bounds__(256) prod_sum_kernel(ProdSumArgs a) {
 #pragma unroll
         for (int f = 0; f < TJ; f++)
 #pragma unroll
-          for (int c = 0; c < 3; c++) v[e][f][c].fold(mi);
+          for (int c = 0; c < NC; c++) v[e][f][c].fold(mi);
     }
   }
 #pragma unroll
@@ -321,12 +311,12 @@ __global__ void __launch_bounds__(256) prod_sum_kernel(ProdSumArgs a) {
     for (int f = 0; f < TJ; f++) {
       if (i + e > last_i || j + f > last_j) continue;
       const size_t to = (place + (size_t)e * nj + f) * a.B + b;
-      u64* o = a.out + to * 3 * pl + (size_t)l * N + n;
+      u64* o = a.out + to * NC * pl + (size_t)l * N + n;
       const u64* g = a.add && i + e < a.add_i ? a.add + to * a.add_comps * pl + (size_t)l * N + n : nullptr;
 #pragma unroll
-      for (int c = 0; c < 3; c++) {
+      for (int c = 0; c < NC; c++) {
         u64 r = v[e][f][c].value(mi);
-        if (g && (u32)c < a.add_comps) r = addmod(r, g[c * pl], mi.m);
+        if (FIRST == 0 && g && (u32)c < a.add_comps) r = addmod(r, g[c * pl], mi.m);
         o[c * pl] = r;
       }
     }

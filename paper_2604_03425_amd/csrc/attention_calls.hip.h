@@ -281,13 +281,13 @@ struct LinAttn {
         return rc;
     return CKKS_OK;
   }
-  template <int TI, int TJ>
+  template <int TI, int TJ, int FIRST = 0>
   void launch_products(bool fp, u32 tiles, u32 cnt, const ProdSumArgs& a) {
     const dim3 grid(tiles * B, c->N / 256, cnt), block(256);
-    if (fp) hipLaunchKernelGGL((prod_sum_kernel<true, TI, TJ>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((prod_sum_kernel<false, TI, TJ>), grid, block, 0, st, a);
+    if (fp) hipLaunchKernelGGL((prod_sum_kernel<true, TI, TJ, FIRST>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((prod_sum_kernel<false, TI, TJ, FIRST>), grid, block, 0, st, a);
   }
-  int products(ProdSumArgs a) {
+  int products(ProdSumArgs a, bool third_only = false) {
     a.mods = c->d_mods;
     a.logN = c->logN;
     a.nlimbs = nlimbs;
@@ -299,7 +299,8 @@ struct LinAttn {
       if (!cnt) continue;
       ProfScope ps(c, PK_PROD_SUM, st);
       const u32 ni = a.i1 - a.i0, nj = a.j1 - a.j0;
-      if (a.tri_out) launch_products<1, 1>(fp, a.tri_out, cnt, a);
+      if (third_only) launch_products<2, 4, 2>(fp, (ni + 1) / 2 * ((nj + 3) / 4), cnt, a);
+      else if (a.tri_out) launch_products<1, 1>(fp, a.tri_out, cnt, a);
       else if (a.tri_sum || (ni == 1 && nj == 1)) launch_products<1, 1>(fp, ni * nj, cnt, a);
       else if (nj == 1) launch_products<4, 1>(fp, (ni + 3) / 4, cnt, a);
       else launch_products<2, 4>(fp, (ni + 1) / 2 * ((nj + 3) / 4), cnt, a);
@@ -330,6 +331,22 @@ struct LinAttn {
         a.i0 = g, a.i1 = std::min(n2, g + rows);
         a.j0 = b, a.j1 = std::min(n1, b + cols);
         const u64 at = ((u64)g * n1 + b) * B * ct;
+        if (C == 1 && two_pass(c) && c->tune[3] != 1) {
+          // the key switch forms the first two terms of the products where it assembles its result, with the state's addend
+          if ((rc = products(a, true))) return rc;
+          const u32 cnt = (a.i1 - a.i0) * (a.j1 - a.j0) * B;
+          KsIo io{d, pl, 0, state_out + at, {state_in ? 1u : 0u, state_in ? 1u : 0u}, nullptr, 0};
+          io.add2 = state_in ? state_in + at : nullptr;
+          io.more = KS_MAPPED;
+          io.more_args.B = B;
+          io.more_args.i0 = a.i0;
+          io.more_args.j0 = a.j0;
+          io.more_args.nj = a.j1 - a.j0;
+          io.more_args.x = a.x;
+          io.more_args.y = a.y;
+          if ((rc = keyswitch_impl(c, io, cnt, nlimbs, mult_key, ks, st))) return rc;
+          continue;
+        }
         a.add = state_in ? state_in + at : nullptr;   // Relin(d) + S = Relin(d + (S, 0))
         if ((rc = products(a))) return rc;
         if ((rc = relin(state_out + at, d, (size_t)(a.i1 - a.i0) * (a.j1 - a.j0) * B))) return rc;
@@ -562,6 +579,16 @@ int ckks_rope(ckks_ctx* c, uint64_t* ct_out, const uint64_t* ct_in, uint32_t B, 
     DeviceGuard guard(c->device);
     if (!guard.ok) return fail(CKKS_EHIP, "cannot select the context's device");
     hipStream_t st = (hipStream_t)stream;
+    const u64* in = (const u64*)ct_in;
+    if (R == 1 && two_pass(c) && c->tune[3] != 1) {
+      // one rotation: the weights join the fused kernels of a key switch, whose digits never reach memory in the evaluation domain
+      const u64 pl = (u64)nlimbs * c->N;
+      KsIo io{in + pl, 2 * pl, galois_elts[0], (u64*)ct_out, {0, 0}, in, galois_elts[0]};
+      io.more = KS_WEIGHTED;
+      io.more_args.w = (const u64*)pt_ext;
+      io.more_args.per_set = B / npt;
+      return keyswitch_impl(c, io, B, nlimbs, (const u64*)evks[0], (char*)ws, st);
+    }
     u64* acc = (u64*)((char*)ws + ks_layout(c, B, nlimbs).acc);
     if ((rc = rotations_to_ext(c, lt, (const u64*)ct_in, B, nlimbs, galois_elts, (const u64* const*)evks, R, (const u64*)pt_ext,
                                B / npt, acc, (char*)ws, st)))

@@ -945,6 +945,8 @@ struct KsIo {
   // ciphertexts [B][2][nlimbs][N], whose other two product terms are the addends
   const u64 *prod_a = nullptr, *prod_b = nullptr;
   bool steps = false;          // ring 2^12: one kernel per step (whole_limb said no)
+  int more = KS_PLAIN;         // two-pass rings with knob 3 at its default: KS_WEIGHTED or KS_MAPPED with these arguments
+  KsMore more_args = {};
 };
 
 // Base conversion fused with the first forward pass (ntt16_bconv_rows_kernel): one launch per modulus class among
@@ -1248,14 +1250,30 @@ int ks16_finish(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B, u32 n
   return ks16_assemble(c, lt, io, B, nlimbs, acc, tq, st);
 }
 
-void launch_inner_c(const ckks_ctx* c, u32 B, u32 nslots, const FwdInnerArgs& a, hipStream_t st) {
+template <int MORE>
+void launch_inner_c_of(const ckks_ctx* c, u32 B, u32 nslots, const FwdInnerArgs& a, hipStream_t st) {
   const dim3 grid(B * 2, pass_tiles(c), nslots), block(NTT16_THREADS);
   switch (c->logN) {
-    case 13: hipLaunchKernelGGL(ntt16_fwd_blocks_inner_c_kernel<13>, grid, block, 0, st, a); break;
-    case 14: hipLaunchKernelGGL(ntt16_fwd_blocks_inner_c_kernel<14>, grid, block, 0, st, a); break;
-    case 15: hipLaunchKernelGGL(ntt16_fwd_blocks_inner_c_kernel<15>, grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL(ntt16_fwd_blocks_inner_c_kernel<16>, grid, block, 0, st, a); break;
+    case 13: hipLaunchKernelGGL((ntt16_fwd_blocks_inner_c_kernel<13, MORE>), grid, block, 0, st, a); break;
+    case 14: hipLaunchKernelGGL((ntt16_fwd_blocks_inner_c_kernel<14, MORE>), grid, block, 0, st, a); break;
+    case 15: hipLaunchKernelGGL((ntt16_fwd_blocks_inner_c_kernel<15, MORE>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((ntt16_fwd_blocks_inner_c_kernel<16, MORE>), grid, block, 0, st, a); break;
   }
+}
+void launch_inner_c(const ckks_ctx* c, u32 B, u32 nslots, const FwdInnerArgs& a, hipStream_t st, int more = KS_PLAIN) {
+  if (more == KS_WEIGHTED) launch_inner_c_of<KS_WEIGHTED>(c, B, nslots, a, st);
+  else if (more == KS_MAPPED) launch_inner_c_of<KS_MAPPED>(c, B, nslots, a, st);
+  else launch_inner_c_of<KS_PLAIN>(c, B, nslots, a, st);
+}
+// FIN and MORE of the integer-class kernel; only the special limbs' sums are weighted before they are stored.
+template <int CLS>
+void launch_inner8_of(dim3 grid, const FwdInnerArgs& a, bool fin, int more, hipStream_t st) {
+  const dim3 block(256);
+  if (more == KS_WEIGHTED && fin) hipLaunchKernelGGL((ntt16_fwd_blocks_inner8_kernel<CLS, true, KS_WEIGHTED>), grid, block, 0, st, a);
+  else if (more == KS_WEIGHTED) hipLaunchKernelGGL((ntt16_fwd_blocks_inner8_kernel<CLS, false, KS_WEIGHTED>), grid, block, 0, st, a);
+  else if (more == KS_MAPPED && fin) hipLaunchKernelGGL((ntt16_fwd_blocks_inner8_kernel<CLS, true, KS_MAPPED>), grid, block, 0, st, a);
+  else if (fin) hipLaunchKernelGGL((ntt16_fwd_blocks_inner8_kernel<CLS, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((ntt16_fwd_blocks_inner8_kernel<CLS, false>), grid, block, 0, st, a);
 }
 
 // Whether the integer-class main limbs store their sums beside the special limbs' (step 3) and are assembled from there, instead of
@@ -1307,7 +1325,7 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
   const LimbMap qmap = identity_map(nlimbs), emap = ext_map(c, nlimbs);
   if (io.galois_pc && B > KS_MULTI_MAX) return fail(CKKS_ESHAPE, "internal: per-ciphertext keys for too many ciphertexts");
   const bool fused_fp = c->tune[3] != 1;
-  if (acc_add && !fused_fp) return fail(CKKS_EINVAL, "internal: accumulation needs the default inner kernels");
+  if ((acc_add || io.more != KS_PLAIN) && !fused_fp) return fail(CKKS_EINVAL, "internal: this needs the default inner kernels");
   auto ext_class = [&](u32 s) { return host_class(c, c->mod[emap.id[s]]); };
   bool any_fp = false, any_int = false, special_fp = false;
   for (u32 s_ = 0; s_ < next; s_++) {
@@ -1409,6 +1427,7 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
   ia.map_mode = map_mode_inner(c, io.galois_pc == nullptr);
   ia.galois = io.d_galois;
   ia.ext_galois = 0;
+  ia.more = io.more_args;
   if (io.galois_pc) {
     ia.multi = 1;
     for (u32 i = 0; i < B; i++) ia.galois_pc[i] = io.galois_pc[i], ia.evk_pc[i] = io.evk_pc[i];
@@ -1429,14 +1448,12 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
         if (ext_class(s_) == cls && (s_ >= nlimbs ? special : main_slots)) a.slots[cnt++] = (unsigned char)s_;
       if (!cnt) continue;
       ProfScope ps(c, PK_INNER8 + cls - 1, st);
-      const dim3 grid(B, N / 2048, cnt), block(256);
-      if (fin && cls == 1) hipLaunchKernelGGL((ntt16_fwd_blocks_inner8_kernel<1, true>), grid, block, 0, st, a);
-      else if (fin) hipLaunchKernelGGL((ntt16_fwd_blocks_inner8_kernel<2, true>), grid, block, 0, st, a);
-      else if (cls == 1) hipLaunchKernelGGL((ntt16_fwd_blocks_inner8_kernel<1, false>), grid, block, 0, st, a);
-      else hipLaunchKernelGGL((ntt16_fwd_blocks_inner8_kernel<2, false>), grid, block, 0, st, a);
+      const dim3 grid(B, N / 2048, cnt);
+      if (cls == 1) launch_inner8_of<1>(grid, a, fin, io.more, st);
+      else launch_inner8_of<2>(grid, a, fin, io.more, st);
     }
   };
-  const bool stored = fused_fp && !acc_add && !io.prod_a && int_sums_stored(c, B, nlimbs, false);
+  const bool stored = fused_fp && !acc_add && !io.prod_a && io.more == KS_PLAIN && int_sums_stored(c, B, nlimbs, false);
   launch_inner8(ia, true, acc_add || !fused_fp || stored, false);
   HIP_TRY(hipGetLastError());
   // double-precision slots whose accumulators are needed in memory: the special ones always (ModDown reads them),
@@ -1449,7 +1466,7 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
     if (!cnt) return CKKS_OK;
     if (fused_fp) {
       ProfScope ps(c, PK_INNER_C, s);
-      launch_inner_c(c, B, cnt, a, s);
+      launch_inner_c(c, B, cnt, a, s, io.more);
     } else {
       // plain block pass of every converted double-precision slot (own limbs are skipped), then a streaming product
       NttOpts o;
@@ -1491,7 +1508,7 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
     if (ext_class(s_) == 0) a.slots[cnt++] = (unsigned char)s_;
   if (cnt) {
     ProfScope ps(c, PK_INNER_C, st);
-    launch_inner_c(c, B, cnt, a, st);
+    launch_inner_c(c, B, cnt, a, st, io.more);
   }
   if (stored) return ks16_assemble(c, lt, io, B, nlimbs, acc, tq, st, true);
   launch_inner8(a, false, true, true);

@@ -364,6 +364,37 @@ __global__ void __launch_bounds__(NTT16_THREADS) ntt16_bconv_rows_kernel(BconvRo
 // the evaluation domain). Output canonical. On integer-class moduli the products go through a Montgomery
 // reduction, so acc carries a factor 2^-64 there, which the later stages absorb into their constants; on
 // double-precision moduli acc is the plain sum.
+// An operand of products of ciphertexts: the ciphertext for output index `idx` and term s. A rotated one counts by `idx` (1) or by s (2)
+// the rotations of a ciphertext, the first of which (the ciphertext itself) lies at `first` and the others at `rest`, one after another.
+struct ProdOperand {
+  const u64 *first, *rest;
+  u64 step, step_s;   // ciphertexts between two values of idx, of s
+  u32 rotated;
+};
+__device__ __forceinline__ const u64* prod_operand(const ProdOperand& p, u32 idx, u32 s, u64 ct) {
+  const u64 at = p.step * idx + p.step_s * s;
+  if (p.rotated == 1 && idx) return p.rest + (at - p.step) * ct;
+  if (p.rotated == 2 && s) return p.rest + (at - p.step_s) * ct;
+  return p.first + at * ct;
+}
+// What a key switch can do beside the plain one (MORE of the fused kernels; KS_PLAIN leaves no trace of it in them):
+// KS_WEIGHTED: out = (w_1 acc - correction) / P + w_0 add_src + [c = 0] w_1 sigma(add_src), the weighted sum of a ciphertext and one
+//   rotation; w_r of set s at w + (s*2 + r)*next*N over the extended basis, ciphertext b takes set b / per_set;
+// KS_MAPPED: the first two terms of the product x(j) * y(i) are added, for output b = ((i - i0)*nj + j - j0)*B + lanes' ciphertext,
+//   and fin_add2 where a component's mode says so. d holds the third.
+enum { KS_PLAIN = 0, KS_WEIGHTED = 1, KS_MAPPED = 2 };
+struct KsMore {
+  const u64* w;
+  u32 per_set;
+  u32 B, i0, j0, nj;
+  ProdOperand x, y;
+};
+__device__ __forceinline__ void ks_mapped(const KsMore& m, u32 b, size_t ct, const u64*& x, const u64*& y) {
+  const u32 o = b / m.B, lanes = b % m.B;
+  x = uniform_ptr(prod_operand(m.x, m.j0 + o % m.nj, 0, ct) + lanes * ct);
+  y = uniform_ptr(prod_operand(m.y, m.i0 + o / m.nj, 0, ct) + lanes * ct);
+}
+
 struct FwdInnerArgs {
   const u64* ext;   // [B][beta][next][N], after the row pass
   const u64* d;     // eval domain, limb-vector (b, t) at d + b*d_poly_stride + t*N; read through the Galois map if galois != 0
@@ -404,6 +435,7 @@ struct FwdInnerArgs {
   // the same kernels: != null switches the product of the second components of two ciphertexts ([B][2][nlimbs][N] each; d is
   // not read) and adds the other two terms of the product to the result (fin_mode0 == fin_mode1 == 4)
   const u64 *prod_a = nullptr, *prod_b = nullptr;
+  KsMore more = {};
 };
 // b is the same for the whole workgroup; saying so keeps the table look-ups on the scalar unit and their results
 // in scalar registers.
@@ -437,7 +469,7 @@ typedef __attribute__((address_space(1))) const void* global_void_ptr;
 typedef const __attribute__((address_space(1))) u64* global_u64_ptr;
 typedef u64 global_u64x2 __attribute__((ext_vector_type(2)));
 #define INNER_C_EX_WORDS (16 * 272)
-template <int LOGN>   // compile-time ring: with a run-time shift the kernel spills
+template <int LOGN, int MORE>   // compile-time ring: with a run-time shift the kernel spills
 __device__ __forceinline__ void fwd_inner_c_body_fp(const FwdInnerArgs& a, u32 bc, u32 tile, u32 t, u32 id, const ModInfo& mi,
                                                     u32* ex, double* img, double* twl) {
   const u32 b = bc >> 1, c = bc & 1;
@@ -540,6 +572,62 @@ __device__ __forceinline__ void fwd_inner_c_body_fp(const FwdInnerArgs& a, u32 b
     }
     jn = jnext;
   }
+  const u64* w0 = nullptr;
+  if (MORE == KS_WEIGHTED) {
+    w0 = uniform_ptr(a.more.w + ((size_t)(b / a.more.per_set) * 2 * a.next + t) * N);
+    const u64* w1 = w0 + a.next * N + lane_pos();
+#pragma unroll
+    for (int i = 0; i < 16; i++) acc[i] = fp_mulmod_var(fp_reduce(acc[i], qinv, q), u2d(w1[i * 16]), qinv, q);
+  }
+  if (MORE != KS_PLAIN && a.fin_tq) {
+    const u32 pos = lane_pos();
+    const double2 pv = ((const double2*)a.fin_pinv)[t];
+    u64* o = a.fin_out + ((size_t)bc * a.nlimbs + t) * N + pos;
+    const size_t pl = (size_t)a.nlimbs * N;
+    if (MORE == KS_WEIGHTED) {
+      const u64* as = a.fin_add_src + ((size_t)bc * a.nlimbs + t) * N;
+      take(x);
+      ntt16_fwd_blocks_fp_words<true>(x, tw, q, qinv, tile, R, ex, twl, [] {}, [&] {
+#pragma unroll
+        for (int i = 0; i < 16; i++) e[i] = w0[pos + i * 16];
+      });
+#pragma unroll
+      for (int i = 0; i < 16; i++)
+        x[i] = fp_mulmod_const(fp_reduce(acc[i], qinv, q) - x[i], pv.x, pv.y, q) + fp_mulmod_var(u2d(as[pos + i * 16]), u2d(e[i]), qinv, q);
+      if (c == 0) {
+        const u64* w1 = w0 + a.next * N;
+#pragma unroll
+        for (int i = 0; i < 16; i++)
+          x[i] += fp_mulmod_var(u2d(as[galois_src_index(pos + i * 16, a.fin_galois, LOGN)]), u2d(w1[pos + i * 16]), qinv, q);
+      }
+    } else {
+      const u64 *px, *py;
+      ks_mapped(a.more, b, 2 * pl, px, py);
+      const u32 mode = c ? a.fin_mode1 : a.fin_mode0;
+      const size_t at = (size_t)t * N + pos;
+      take(x);
+      ntt16_fwd_blocks_fp_words<true>(x, tw, q, qinv, tile, R, ex, twl, [] {}, [&] {
+#pragma unroll
+        for (int i = 0; i < 16; i++) e[i] = px[at + i * 16];
+      });
+#pragma unroll
+      for (int i = 0; i < 16; i++)
+        x[i] = fp_mulmod_const(fp_reduce(acc[i], qinv, q) - x[i], pv.x, pv.y, q) +
+               fp_mulmod_var(u2d(e[i]), u2d(py[at + (c ? pl : 0) + i * 16]), qinv, q);
+      if (c) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) x[i] += fp_mulmod_var(u2d(px[at + pl + i * 16]), u2d(py[at + i * 16]), qinv, q);
+      }
+      if (mode & 1) {
+        const u64* a2 = a.fin_add2 + ((size_t)bc * a.nlimbs + t) * N + pos;
+#pragma unroll
+        for (int i = 0; i < 16; i++) x[i] += u2d(a2[i * 16]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i++) o[i * 16] = d2u_canon(fp_reduce(x[i], qinv, q), q);
+    return;
+  }
   if (a.fin_tq) {
     const u32 mode = c ? a.fin_mode1 : a.fin_mode0;
     const u32 gf = a.multi ? g : a.fin_galois;
@@ -607,7 +695,7 @@ __device__ __forceinline__ void fwd_inner_c_body_fp(const FwdInnerArgs& a, u32 b
 #pragma unroll
   for (int i = 0; i < 16; i++) o[i * 16] = d2u_canon(fp_reduce(acc[i], qinv, q), q);
 }
-template <int LOGN>
+template <int LOGN, int MORE = KS_PLAIN>
 __global__ void __launch_bounds__(NTT16_THREADS) __attribute__((amdgpu_waves_per_eu(3, 3)))
 ntt16_fwd_blocks_inner_c_kernel(FwdInnerArgs a) {
   // separate arrays, so that the compiler knows the transposes never touch the image a prefetch is landing in
@@ -619,7 +707,7 @@ ntt16_fwd_blocks_inner_c_kernel(FwdInnerArgs a) {
   const u32 t = a.slots[zi];
   const u32 id = t < a.nlimbs ? t : t - a.nlimbs + a.nq;
   const ModInfo mi = a.mods[id];
-  fwd_inner_c_body_fp<LOGN>(a, bc, tile, t, id, mi, ex, img, twl);
+  fwd_inner_c_body_fp<LOGN, MORE>(a, bc, tile, t, id, mi, ex, img, twl);
 }
 
 // Integer-class moduli (the special primes): both key components per workgroup, 8 values per lane: a workgroup takes
@@ -640,7 +728,7 @@ __device__ __forceinline__ void inner8_load(u64 (&v)[8], const u64* p) {
     v[2 * k + 1] = w.y;
   }
 }
-template <int CLS, bool FIN>
+template <int CLS, bool FIN, int MORE = KS_PLAIN>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3)))
 ntt16_fwd_blocks_inner8_kernel(FwdInnerArgs a) {
   constexpr bool BIG = CLS == 2;
@@ -716,7 +804,7 @@ ntt16_fwd_blocks_inner8_kernel(FwdInnerArgs a) {
   u32 jn = jo == 0 ? 1u : 0u;   // next converted digit
   auto tq_limb = [&](u32 c) { return a.fin_tq + (((size_t)b * 2 + c) * a.nlimbs + t) * N; };
   auto prod_limb = [&](const u64* p, u32 c) { return p + (((size_t)b * 2 + c) * a.nlimbs + t) * N + posC; };
-  const u64 r2 = FIN && a.prod_a ? mont_r2(mi) : 0;
+  const u64 r2 = MORE != KS_PLAIN || (FIN && a.prod_a) ? mont_r2(mi) : 0;
   if (jn < beta) request(ext_limb(jn));
   else if (FIN) request(tq_limb(0));
   if (jo != 0xFFFFFFFFu) {   // the own digit first: its loads are in flight together with the first prefetch
@@ -756,6 +844,18 @@ ntt16_fwd_blocks_inner8_kernel(FwdInnerArgs a) {
     multiply();
     jn = jnext;
   }
+  const u64* w0 = nullptr;
+  if (MORE == KS_WEIGHTED) {   // the weight times 2^64 makes up for this product's factor
+    w0 = uniform_ptr(a.more.w + ((size_t)(b / a.more.per_set) * 2 * a.next + t) * N);
+    const u64* w1 = w0 + a.next * N + posC;
+#pragma unroll
+    for (int k = 0; k < 8; k++) {
+      const u64 f = csub(mont_mul63(w1[k], r2, q, mi.minv), q);
+      acc0[k] = mont_mul63(acc0[k], f, q, mi.minv);
+      acc1[k] = mont_mul63(acc1[k], f, q, mi.minv);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
   if (FIN) {
     const ulonglong2 pv = a.fin_pinv[t];
     const u32 gf = a.multi ? g : a.fin_galois;
@@ -767,6 +867,7 @@ ntt16_fwd_blocks_inner8_kernel(FwdInnerArgs a) {
       u64 ev[8];
       take();
       ntt256_fwd_blocks_int8<BIG>(x, tw, q, h, 1u << (a.logN - 8), l, smb, [&] {
+        if (MORE != KS_PLAIN) return;
         if (mode & 1) inner8_load(ev, a.fin_add2 + ((a.fin_add2_three ? (size_t)b * 3 + c : (size_t)b * 2 + c) * a.nlimbs + t) * N + posC);
         else if (mode == 4) inner8_load(ev, prod_limb(a.prod_a, 0));
         else if (mode == 2) {
@@ -782,7 +883,39 @@ ntt16_fwd_blocks_inner8_kernel(FwdInnerArgs a) {
         if (BIG) x[k] = csub_neg(x[k], 8 * q);
         x[k] = shoup(acc[k] + above - x[k], pv.x, pv.y, q);
       }
-      if (mode == 4) {   // d0 = a0 b0, d1 = a0 b1 + a1 b0; ev holds a0
+      if (MORE == KS_WEIGHTED) {
+        u64 f[8];
+        inner8_load(ev, as + posC);
+        inner8_load(f, w0 + posC);
+#pragma unroll
+        for (int k = 0; k < 8; k++) x[k] = addmod(x[k], mont_plain(ev[k], f[k], r2, q, mi.minv), q);
+        if (c == 0) {
+          inner8_load(f, w0 + a.next * N + posC);
+#pragma unroll
+          for (int k = 0; k < 8; k++)
+            x[k] = addmod(x[k], mont_plain(as[galois_src_index(posC + k, a.fin_galois, a.logN)], f[k], r2, q, mi.minv), q);
+        }
+      } else if (MORE == KS_MAPPED) {
+        const u64 *px, *py;
+        const size_t pl = (size_t)a.nlimbs * N, at = (size_t)t * N + posC;
+        ks_mapped(a.more, b, 2 * pl, px, py);
+        u64 f[8];
+        inner8_load(ev, px + at);
+        inner8_load(f, py + at + (c ? pl : 0));
+#pragma unroll
+        for (int k = 0; k < 8; k++) x[k] = addmod(x[k], mont_plain(ev[k], f[k], r2, q, mi.minv), q);
+        if (c) {
+          inner8_load(ev, px + at + pl);
+          inner8_load(f, py + at);
+#pragma unroll
+          for (int k = 0; k < 8; k++) x[k] = addmod(x[k], mont_plain(ev[k], f[k], r2, q, mi.minv), q);
+        }
+        if (mode & 1) {
+          inner8_load(ev, a.fin_add2 + (((size_t)b * 2 + c) * a.nlimbs + t) * N + posC);
+#pragma unroll
+          for (int k = 0; k < 8; k++) x[k] = addmod(x[k], ev[k], q);
+        }
+      } else if (mode == 4) {   // d0 = a0 b0, d1 = a0 b1 + a1 b0; ev holds a0
         u64 f[8];
         inner8_load(f, prod_limb(a.prod_b, c));
 #pragma unroll

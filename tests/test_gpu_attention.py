@@ -45,7 +45,11 @@ def contexts(name):
     return _contexts[name]
 
 
-@pytest.mark.parametrize("name,nl,B,npt,R", [
+ONE_ROTATION = [("ring13", 3, 4, 2, 1), ("ring13_int", 4, 3, 1, 1), ("ring13_mixed", 5, 4, 4, 1), ("ring13_mixed", 4, 3, 1, 1),
+                ("ring13_fp", 3, 4, 2, 1), ("ring14_wide", 10, 3, 3, 1), ("ring15", 4, 2, 1, 1), ("ring16", 1, 6, 2, 1)]
+
+
+@pytest.mark.parametrize("name,nl,B,npt,R", ONE_ROTATION + [
     ("ring10", 4, 1, 1, 1), ("ring10", 1, 3, 1, 2), ("ring10", 3, 2, 2, 33), ("ring10", 2, 2, 1, 65), ("ring11", 2, 4, 2, 2),
     ("ring12", 5, 8, 1, 1), ("ring12", 3, 3, 3, 2), ("ring13", 4, 5, 1, 2), ("ring13", 2, 1, 1, 0), ("ring13_int", 5, 2, 1, 2),
     ("ring13_int", 3, 6, 3, 1), ("ring13_mixed", 5, 3, 3, 2), ("ring13_mixed", 3, 1, 1, 34), ("ring13_fp", 4, 4, 2, 2),
