@@ -25,7 +25,7 @@ struct RotSumArgs {
   u64* acc;             // [outs][B][2][next][N]
   const ModInfo* mods;
   u64 d_stride;
-  u32 logN, nlimbs, nq, nm, alpha, beta, next, B, nterms, w_first, w_terms, per_set, accumulate;
+  u32 logN, nlimbs, nq, nm, alpha, beta, next, B, nterms, w_first, w_terms, per_set, accumulate, nfp, doubles;   // doubles: ext holds doubles on moduli < 2^50
   unsigned char slots[128];
   RotTerm term[ROT_SUM_TERMS];
 };
@@ -48,13 +48,15 @@ __device__ __forceinline__ void attention_map(u32& what, u32& blk, u32& zi) {
   zi = unit / gridDim.y;
 }
 
-// Moduli below 2^50 on the two-pass rings: doubles in ext, sums in doubles (|.| < 2^53 = 8q throughout). A lane owns a position of
-// CB ciphertexts, which share the key words. grid = (outs * ceil(B / CB), N / 256, slots).
+// Moduli below 2^50 where ext holds doubles (rings 2^12 .. 2^16): sums in doubles (|.| < 2^53 = 8q throughout). A lane owns a position of
+// CB ciphertexts, which share the key words. What bounds it is memory, the last-level cache's share included: two rotations of 16
+// ciphertexts of 20 limbs, 4 digits, move 2.4 GB in 477 us. CB = 2: with 4 there are fewer waves to hide the gathers (512 us), with 1
+// every ciphertext fetches the keys again (590). With all digits of a term requested ahead, which costs registers, 513 and 550.
+// By (ciphertexts, limb) on an XCD instead, which finds more digits and fewer key words in its L2, 504.
+// grid = (outs * ceil(B / CB), N / 256, slots).
 template <int CB>
-__global__ void __launch_bounds__(256) rot_sum_fp_kernel(RotSumArgs a) {
+__device__ __forceinline__ void rot_sum_fp(const RotSumArgs& a, u32 what, u32 blk, u32 zi) {
   const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, comp = (size_t)a.nm * N;
-  u32 what, blk, zi;
-  attention_map(what, blk, zi);
   const u32 groups = (a.B + CB - 1) / CB, o = what / groups, b0 = (what % groups) * CB;
   const u32 n = blk * 256 + threadIdx.x, t = a.slots[zi];
   const bool main_prime = t < a.nlimbs;
@@ -67,11 +69,11 @@ __global__ void __launch_bounds__(256) rot_sum_fp_kernel(RotSumArgs a) {
 #pragma unroll
   for (int k = 0; k < CB; k++) {
     bb[k] = min(b0 + k, a.B - 1);
-    w[k] = a.w ? a.w + (((size_t)(bb[k] / a.per_set) * a.w_terms + a.w_first) * a.next + t) * N + n : nullptr;
+    w[k] = a.w ? a.w + (((size_t)(bb[k] / a.per_set) * a.w_terms + a.w_first) * a.next + t) * N : nullptr;
     s0[k] = s1[k] = 0.0;
     if (a.base && main_prime && o == 0) {
       const u64* x = a.base + (size_t)bb[k] * a.base_stride + (size_t)t * N + n;
-      const double f = a.w ? fp_mulmod_var(pm, u2d(*w[k]), qinv, q) : pm;
+      const double f = a.w ? fp_mulmod_var(pm, u2d(w[k][n]), qinv, q) : pm;
       s0[k] = fp_mulmod_var(u2d(x[0]), f, qinv, q);
       s1[k] = fp_mulmod_var(u2d(x[pl]), f, qinv, q);
     }
@@ -80,37 +82,43 @@ __global__ void __launch_bounds__(256) rot_sum_fp_kernel(RotSumArgs a) {
   for (u32 r = 0; r < a.nterms; r++) {
     const RotTerm& term = a.term[o * a.nterms + r];
     const u32 m = galois_src_index(n, term.galois, a.logN);
-    const u64* e = term.evk + (size_t)id * N + n;
+    const u64* e = uniform_ptr(term.evk) + (size_t)id * N;
+    const u64 *ext = uniform_ptr(term.ext), *d = uniform_ptr(term.d), *c0 = term.c0 ? uniform_ptr(term.c0) : nullptr;
+    u64 cw[CB], ww[CB];
+#pragma unroll
+    for (int k = 0; k < CB; k++) {
+      cw[k] = c0 && main_prime ? uniform_load(c0 + (size_t)bb[k] * a.d_stride + (size_t)t * N, m * 8) : 0;
+      ww[k] = a.w ? uniform_load(w[k] + (size_t)(r + 1) * a.next * N, n * 8) : 0;
+    }
     double v0[CB], v1[CB];
 #pragma unroll
-    for (int k = 0; k < CB; k++) {
-      v0[k] = v1[k] = 0.0;
-      if (term.c0 && main_prime) v0[k] = fp_mulmod_var(u2d(term.c0[(size_t)bb[k] * a.d_stride + (size_t)t * N + m]), pm, qinv, q);
-    }
+    for (int k = 0; k < CB; k++) v0[k] = v1[k] = 0.0;
     for (u32 j = 0; j < a.beta; j++, e += 2 * comp) {
-      double x[CB];
-      if (j == jo) {
+      const bool own = j == jo;   // uniform: where the digit's words start, and how far its ciphertexts are apart
+      const u64* x = own ? d + (size_t)t * N : ext + ((size_t)j * a.next + t) * N;
+      const size_t apart = own ? (size_t)a.d_stride : (size_t)a.beta * a.next * N;
+      u64 xr[CB];
 #pragma unroll
-        for (int k = 0; k < CB; k++) x[k] = u2d(term.d[(size_t)bb[k] * a.d_stride + (size_t)t * N + m]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < CB; k++)
-          x[k] = __longlong_as_double((long long)term.ext[(((size_t)bb[k] * a.beta + j) * a.next + t) * N + m]);
-      }
-      const double e0 = u2d(e[0]), e1 = u2d(e[comp]);
+      for (int k = 0; k < CB; k++) xr[k] = uniform_load(x + bb[k] * apart, m * 8);
+      const double e0 = u2d(uniform_load(e, n * 8)), e1 = u2d(uniform_load(e + comp, n * 8));
+      // residues become doubles by setting the exponent and taking 2^52 away, doubles stay what they are
+      const u64 bias = own ? 0x4330000000000000ull : 0ull;
+      const double less = __longlong_as_double((long long)bias);
 #pragma unroll
       for (int k = 0; k < CB; k++) {
-        v0[k] += fp_mulmod_var(x[k], e0, qinv, q);
-        v1[k] += fp_mulmod_var(x[k], e1, qinv, q);
-        if ((j & 3) == 3) v0[k] = fp_reduce(v0[k], qinv, q), v1[k] = fp_reduce(v1[k], qinv, q);   // at most 5 products below 0.9 q
+        const double v = __longlong_as_double((long long)(xr[k] | bias)) - less;
+        v0[k] += fp_mulmod_var(v, e0, qinv, q);
+        v1[k] += fp_mulmod_var(v, e1, qinv, q);
+        if ((j & 3) == 3) v0[k] = fp_reduce(v0[k], qinv, q), v1[k] = fp_reduce(v1[k], qinv, q);   // 4 products below 0.9 q, a folded sum
       }
     }
 #pragma unroll
     for (int k = 0; k < CB; k++) {
+      if (c0 && main_prime) v0[k] += fp_mulmod_var(u2d(cw[k]), pm, qinv, q);
       v0[k] = fp_reduce(v0[k], qinv, q);
       v1[k] = fp_reduce(v1[k], qinv, q);
       if (a.w) {
-        const double f = u2d(w[k][(size_t)(r + 1) * a.next * N]);
+        const double f = u2d(ww[k]);
         v0[k] = fp_mulmod_var(v0[k], f, qinv, q);
         v1[k] = fp_mulmod_var(v1[k], f, qinv, q);
       }
@@ -131,10 +139,8 @@ __global__ void __launch_bounds__(256) rot_sum_fp_kernel(RotSumArgs a) {
 // All other moduli: residues in ext, Montgomery products, sums below 2m. PLAIN: acc without the factor 2^-64 (rings whose ModDown
 // takes none). Grid and lanes as above.
 template <int CB, bool PLAIN>
-__global__ void __launch_bounds__(256) rot_sum_int_kernel(RotSumArgs a) {
+__device__ __forceinline__ void rot_sum_int(const RotSumArgs& a, u32 what, u32 blk, u32 zi) {
   const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, comp = (size_t)a.nm * N;
-  u32 what, blk, zi;
-  attention_map(what, blk, zi);
   const u32 groups = (a.B + CB - 1) / CB, o = what / groups, b0 = (what % groups) * CB;
   const u32 n = blk * 256 + threadIdx.x, t = a.slots[zi];
   const bool main_prime = t < a.nlimbs;
@@ -200,6 +206,16 @@ __global__ void __launch_bounds__(256) rot_sum_int_kernel(RotSumArgs a) {
     to[0] = csub(s0[k], q);
     to[(size_t)a.next * N] = csub(s1[k], q);
   }
+}
+
+// KIND 0: double-precision slots; 1: integer ones; 2: every slot, PLAIN; 3: slots of both kinds in one launch, the first nfp of them
+// double-precision ones (ring 2^12, where a launch more costs more than the registers of the other kind)
+template <int KIND, int CB>
+__global__ void __launch_bounds__(256) rot_sum_kernel(RotSumArgs a) {
+  u32 what, blk, zi;
+  attention_map(what, blk, zi);
+  if (KIND == 0 || (KIND == 3 && zi < a.nfp)) rot_sum_fp<CB>(a, what, blk, zi);
+  else rot_sum_int<CB, KIND == 2>(a, what, blk, zi);
 }
 
 // out[i][j][b] = sum_{s < ns} x(j, s)[b] * y(i, s)[b] in three components (+ add in the first two, or in all three), for i0 <= i < i1 and

@@ -26,12 +26,23 @@ u32 rotation_element(const ckks_ctx* c, u64 steps) {   // 5^steps mod 2N
   return (u32)g;
 }
 
+// Ring 2^12 has its kernels that hold whole limbs (`whole`: whole_limb's rule, once a call, since the forms below differ) or goes one
+// kernel per step like the rings without any: rotary positions of 8 ciphertexts of 4 limbs 38 us that way, by steps 44; 256 of 12 limbs
+// in 3 digits 1012 and 880.
 // Digits of B polynomials in the extended basis, evaluation domain, at L.ext of the key-switch workspace: (b, limb t) is at
-// d + b * d_stride + t * N. Doubles on the double-precision moduli of the two-pass rings, canonical residues elsewhere.
-int ext_digits(ckks_ctx* c, const LevelTables* lt, const u64* d, u64 d_stride, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
+// d + b * d_stride + t * N. Doubles on the double-precision moduli of the two-pass rings and of whole limbs, canonical residues elsewhere.
+int ext_digits(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* d, u64 d_stride, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
   int rc;
   FwdInnerArgs unused;
   if (two_pass(c)) return hoist_front16(c, lt, d, d_stride, B, nlimbs, ws, st, unused);
+  if (whole) {
+    Ks12Args a = ks12_args(c, lt, B, nlimbs, ws);
+    a.d = d;
+    a.d_stride = d_stride;
+    launch_ks12_digits(c, lt, B, nlimbs, a, st);
+    HIP_TRY(hipGetLastError());
+    return CKKS_OK;
+  }
   const u32 N = c->N, next = lt->next, beta = lt->beta;
   const KsLayout L = ks_layout(c, B, nlimbs);
   u64 *dcoef = (u64*)(ws + L.dcoef), *ext = (u64*)(ws + L.ext);
@@ -46,11 +57,26 @@ int ext_digits(ckks_ctx* c, const LevelTables* lt, const u64* d, u64 d_stride, u
 }
 
 // ModDown of both accumulators [B][2][next][N] (their special limbs are overwritten) to out [B][2][nlimbs][N].
-int ext_mod_down(ckks_ctx* c, const LevelTables* lt, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
+int ext_mod_down(ckks_ctx* c, const LevelTables* lt, bool whole, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
   int rc;
   if (two_pass(c)) {
     KsIo io{nullptr, 0, 0, out, {0, 0}, nullptr, 0};
     return ks16_finish(c, lt, io, B, nlimbs, ws, st, acc);
+  }
+  if (whole) {
+    Ks12Args a = ks12_args(c, lt, B, nlimbs, ws);
+    a.sums = a.acc = acc;
+    a.out = out;
+    const dim3 block(WL_THREADS), grid(2 * B, nlimbs);
+    {
+      ProfScope ps(c, PK_KS12_SPECIAL, st);
+      hipLaunchKernelGGL(ks12_special_sums_kernel, dim3(2 * B, c->np), block, 0, st, a);
+    }
+    ProfScope ps(c, PK_KS12_FINAL, st);
+    if (lt->narrow_dn) hipLaunchKernelGGL(ks12_final_sums_kernel<true>, grid, block, 0, st, a);
+    else hipLaunchKernelGGL(ks12_final_sums_kernel<false>, grid, block, 0, st, a);
+    HIP_TRY(hipGetLastError());
+    return CKKS_OK;
   }
   const u32 N = c->N, next = lt->next, K = c->np;
   u64* tq = (u64*)(ws + ks_layout(c, B, nlimbs).tq);
@@ -73,7 +99,7 @@ int ext_mod_down(ckks_ctx* c, const LevelTables* lt, u64* acc, u64* out, u32 B, 
 }
 
 // Everything about rot_sum_kernel's arguments that the context and the level fix.
-RotSumArgs rot_sum_args(const ckks_ctx* c, const LevelTables* lt, u32 nlimbs, u64* acc, u64 d_stride) {
+RotSumArgs rot_sum_args(const ckks_ctx* c, const LevelTables* lt, bool whole, u32 nlimbs, u64* acc, u64 d_stride) {
   RotSumArgs a;
   a.base = a.w = nullptr;
   a.base_stride = 0;
@@ -89,42 +115,56 @@ RotSumArgs rot_sum_args(const ckks_ctx* c, const LevelTables* lt, u32 nlimbs, u6
   a.next = lt->next;
   a.nterms = a.w_first = a.w_terms = a.accumulate = 0;
   a.per_set = 1;
+  a.doubles = two_pass(c) || whole;
   return a;
 }
-template <int CB>
-void launch_rot_sum_of(int kind, u32 outs, u32 slots, const RotSumArgs& a, hipStream_t st) {
-  const dim3 grid(outs * ((a.B + CB - 1) / CB), (1u << a.logN) / 256, slots), block(256);
-  if (kind == 0) hipLaunchKernelGGL(rot_sum_fp_kernel<CB>, grid, block, 0, st, a);
-  else if (kind == 1) hipLaunchKernelGGL((rot_sum_int_kernel<CB, false>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((rot_sum_int_kernel<CB, true>), grid, block, 0, st, a);
+template <int KIND>
+void launch_rot_sum_of(u32 outs, u32 slots, const RotSumArgs& a, hipStream_t st) {
+  const dim3 block(256);
+  if (a.B > 1) hipLaunchKernelGGL((rot_sum_kernel<KIND, 2>), dim3(outs * ((a.B + 1) / 2), (1u << a.logN) / 256, slots), block, 0, st, a);
+  else hipLaunchKernelGGL((rot_sum_kernel<KIND, 1>), dim3(outs, (1u << a.logN) / 256, slots), block, 0, st, a);
 }
 int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 outs = 1) {
   a.B = B;
   const LimbMap emap = ext_map(c, a.nlimbs);
-  for (int kind = 0; kind < 3; kind++) {
-    u32 cnt = 0;
-    for (u32 s = 0; s < a.next; s++) {
-      const int k = !two_pass(c) ? 2 : host_class(c, c->mod[emap.id[s]]) == 0 ? 0 : 1;
-      if (k == kind) a.slots[cnt++] = (unsigned char)s;
-    }
-    if (!cnt) continue;
-    ProfScope ps(c, kind ? PK_ROT_SUM_INT : PK_ROT_SUM, st);
-    if (B >= 3) launch_rot_sum_of<4>(kind, outs, cnt, a, st);
-    else if (B == 2) launch_rot_sum_of<2>(kind, outs, cnt, a, st);
-    else launch_rot_sum_of<1>(kind, outs, cnt, a, st);
+  unsigned char slots[128];
+  u32 cnt = 0;
+  for (int fp = 1; fp >= 0; fp--) {   // double-precision slots first
+    for (u32 s = 0; s < a.next; s++)
+      if ((a.doubles && host_class(c, c->mod[emap.id[s]]) == 0) == (fp == 1)) slots[cnt++] = (unsigned char)s;
+    if (fp) a.nfp = cnt;
+  }
+  auto take = [&](u32 first, u32 n) { std::copy(slots + first, slots + first + n, a.slots); };
+  if (!two_pass(c)) {
+    ProfScope ps(c, PK_ROT_SUM_INT, st);
+    take(0, cnt);
+    if (a.doubles) launch_rot_sum_of<3>(outs, cnt, a, st);
+    else launch_rot_sum_of<2>(outs, cnt, a, st);
+    HIP_TRY(hipGetLastError());
+    return CKKS_OK;
+  }
+  if (a.nfp) {
+    ProfScope ps(c, PK_ROT_SUM, st);
+    take(0, a.nfp);
+    launch_rot_sum_of<0>(outs, a.nfp, a, st);
+  }
+  if (cnt > a.nfp) {
+    ProfScope ps(c, PK_ROT_SUM_INT, st);
+    take(a.nfp, cnt - a.nfp);
+    launch_rot_sum_of<1>(outs, cnt - a.nfp, a, st);
   }
   HIP_TRY(hipGetLastError());
   return CKKS_OK;
 }
 
 // acc = P w_0 ct + sum_r w_{r+1} (accumulators of the rotation of ct by galois[r]); ws: a key-switch workspace for B.
-int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, const u64* ct, u32 B, u32 nlimbs, const u32* galois,
+int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* ct, u32 B, u32 nlimbs, const u32* galois,
                      const u64* const* evks, u32 R, const u64* w, u32 per_set, u64* acc, char* ws, hipStream_t st) {
   int rc;
   const u64 pl = (u64)nlimbs * c->N;
-  if (R && (rc = ext_digits(c, lt, ct + pl, 2 * pl, B, nlimbs, ws, st))) return rc;
+  if (R && (rc = ext_digits(c, lt, whole, ct + pl, 2 * pl, B, nlimbs, ws, st))) return rc;
   const u64* ext = (const u64*)(ws + ks_layout(c, B, nlimbs).ext);
-  RotSumArgs a = rot_sum_args(c, lt, nlimbs, acc, 2 * pl);
+  RotSumArgs a = rot_sum_args(c, lt, whole, nlimbs, acc, 2 * pl);
   a.base = ct;
   a.base_stride = 2 * pl;
   a.w = w;
@@ -146,10 +186,16 @@ int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, const u64* ct, u32 B, u
 // many times over; more would only take workspace.
 u32 linattn_slice(const ckks_ctx* c, u32 B) { return std::max<u32>(B, std::min(1024u, 128u << (c->logN < 16 ? 16 - c->logN : 0))); }
 
+// Tokens up to which the key switches of a state's update form the first two terms of the sums of products themselves. us, that way |
+// by the kernel of the products, 32 components at 2^16, 8 limbs, 1, 2, 4, 8 tokens: 1934 | 2012, 2665 | 2699, 4415 | 4363, 9338 | 8961;
+// 16 at 2^15, 5 60-bit limbs, 2, 5, 8: 1607 | 1618, 3424 | 3353, 5954 | 5785. Beyond two every output fetches factors that a tile shares.
+#define LINATTN_MAPPED_TOKENS 2
+
 struct LinAttn {
   const ckks_ctx* cc;      // for sizes
   ckks_ctx* c;
   const LevelTables* lt;
+  bool whole;              // ring 2^12: the kernels for whole limbs
   u32 C, B, nlimbs, n1, n2;
   u64 pl, ct;              // words of a polynomial, of a ciphertext
   u32 slice, tokens;       // ciphertexts per key switch; tokens whose ciphertexts make at most that many
@@ -172,6 +218,7 @@ struct LinAttn {
     pl = (u64)nlimbs * cc->N, ct = 2 * pl;
     slice = linattn_slice(cc, B);
     tokens = std::min<u32>(C, slice / B);
+    whole = whole_limb(cc, C * B, nlimbs, false);
   }
   // pieces of the workspace of a step (scores = false) or of a chunk
   size_t carve(char* ws, bool scores) {
@@ -207,15 +254,15 @@ struct LinAttn {
       const u32 cnt = std::min(nb, n - i), per = std::min<u32>(R, slice / cnt);
       const u64* ext = (const u64*)(ks + ks_layout(c, cnt, nlimbs).ext);
       for (u32 r0 = 0; r0 < R; r0 += per) {   // (ModDown's scratch takes the digits' place, so a further pass converts again)
-        if ((rc = ext_digits(c, lt, in + i * ct + pl, ct, cnt, nlimbs, ks, st))) return rc;
+        if ((rc = ext_digits(c, lt, whole, in + i * ct + pl, ct, cnt, nlimbs, ks, st))) return rc;
         const u32 rots = std::min(per, R - r0);
         if ((rc = rotations_apart(acc, ext, in + i * ct, cnt, elements.data() + r0, keys + r0, rots))) return rc;
         if (out_stride == (u64)cnt * ct) {
-          if ((rc = ext_mod_down(c, lt, acc, out + r0 * out_stride, rots * cnt, nlimbs, ks, st))) return rc;
+          if ((rc = ext_mod_down(c, lt, whole, acc, out + r0 * out_stride, rots * cnt, nlimbs, ks, st))) return rc;
           continue;
         }
         for (u32 r = 0; r < rots; r++)
-          if ((rc = ext_mod_down(c, lt, acc + (u64)r * cnt * ext_ct, out + (r0 + r) * out_stride + i * ct, cnt, nlimbs, ks, st)))
+          if ((rc = ext_mod_down(c, lt, whole, acc + (u64)r * cnt * ext_ct, out + (r0 + r) * out_stride + i * ct, cnt, nlimbs, ks, st)))
             return rc;
       }
     }
@@ -236,7 +283,7 @@ struct LinAttn {
         if ((rc = launch_inner_rot(c, lt, ia, n, nlimbs, elements + r0, keys + r0, rots, to + r0 * stride, stride, st))) return rc;
         continue;
       }
-      RotSumArgs a = rot_sum_args(c, lt, nlimbs, to + r0 * stride, ct);
+      RotSumArgs a = rot_sum_args(c, lt, whole, nlimbs, to + r0 * stride, ct);
       a.nterms = 1;
       for (u32 r = 0; r < rots; r++) a.term[r] = RotTerm{ext, in + pl, in, keys[r0 + r], elements[r0 + r]};
       if ((rc = launch_rot_sum(c, a, n, st, rots))) return rc;
@@ -259,14 +306,14 @@ struct LinAttn {
       hipLaunchKernelGGL(gather_kernel, dim3((unsigned)((g.words + 255) / 256), with_q ? 3 : 2), dim3(256), 0, st, g);
       HIP_TRY(hipGetLastError());
     }
-    if ((rc = ext_digits(c, lt, d + pl, ct, turned + n, nlimbs, ks, st))) return rc;
+    if ((rc = ext_digits(c, lt, whole, d + pl, ct, turned + n, nlimbs, ks, st))) return rc;
     const u64* ext = (const u64*)(ks + ks_layout(c, turned + n, nlimbs).ext);
     u64* to = acc;
     if ((rc = rotations_apart(to, ext, d, turned, baby.data(), baby_keys, n1 - 1))) return rc;
     to += (u64)(n1 - 1) * turned * ext_ct;
     if ((rc = rotations_apart(to, ext + (u64)turned * lt->beta * lt->next * c->N, d + (u64)turned * ct, n, value.data(), value_keys, n2 - 1)))
       return rc;
-    if ((rc = ext_mod_down(c, lt, acc, rot_a, (n1 - 1) * turned + (n2 - 1) * n, nlimbs, ks, st))) return rc;
+    if ((rc = ext_mod_down(c, lt, whole, acc, rot_a, (n1 - 1) * turned + (n2 - 1) * n, nlimbs, ks, st))) return rc;
     q_rest = rot_a;
     k_rest = rot_a + (with_q ? n * ct : 0);
     v_rest = rot_a + (u64)(n1 - 1) * turned * ct;
@@ -299,7 +346,8 @@ struct LinAttn {
       if (!cnt) continue;
       ProfScope ps(c, PK_PROD_SUM, st);
       const u32 ni = a.i1 - a.i0, nj = a.j1 - a.j0;
-      if (third_only) launch_products<2, 4, 2>(fp, (ni + 1) / 2 * ((nj + 3) / 4), cnt, a);
+      if (third_only && a.tri_out) launch_products<1, 1, 2>(fp, a.tri_out, cnt, a);
+      else if (third_only) launch_products<2, 4, 2>(fp, (ni + 1) / 2 * ((nj + 3) / 4), cnt, a);
       else if (a.tri_out) launch_products<1, 1>(fp, a.tri_out, cnt, a);
       else if (a.tri_sum || (ni == 1 && nj == 1)) launch_products<1, 1>(fp, ni * nj, cnt, a);
       else if (nj == 1) launch_products<4, 1>(fp, (ni + 3) / 4, cnt, a);
@@ -307,6 +355,28 @@ struct LinAttn {
     }
     HIP_TRY(hipGetLastError());
     return CKKS_OK;
+  }
+
+  // out = add + Relin(products of a) on the two-pass rings: only the third terms of the products go through memory, at d; the key
+  // switch forms the other two where it assembles its result.
+  int relin_products(u64* out, const u64* add, const ProdSumArgs& a) {
+    int rc;
+    if ((rc = products(a, true))) return rc;
+    const u32 cnt = (a.tri_out ? a.tri_out : (a.i1 - a.i0) * (a.j1 - a.j0)) * B;
+    KsIo io{a.out, pl, 0, out, {add ? 1u : 0u, add ? 1u : 0u}, nullptr, 0};
+    io.add2 = add;
+    io.more = KS_MAPPED;
+    KsMore& m = io.more_args;
+    m.B = B;
+    m.i0 = a.i0;
+    m.j0 = a.j0;
+    m.nj = a.j1 - a.j0;
+    m.ns = a.ns;
+    m.tri = a.tri_out;
+    m.tri_first = a.tri_first;
+    m.x = a.x;
+    m.y = a.y;
+    return keyswitch_impl(c, io, cnt, nlimbs, mult_key, ks, st);
   }
 
   // state_out = state_in + Relin(sum_s K_s[b] * V_s[g]), then times decay. state_out may be state_in.
@@ -331,20 +401,9 @@ struct LinAttn {
         a.i0 = g, a.i1 = std::min(n2, g + rows);
         a.j0 = b, a.j1 = std::min(n1, b + cols);
         const u64 at = ((u64)g * n1 + b) * B * ct;
-        if (C == 1 && two_pass(c) && c->tune[3] != 1) {
+        if (C <= LINATTN_MAPPED_TOKENS && two_pass(c) && c->tune[3] != 1) {
           // the key switch forms the first two terms of the products where it assembles its result, with the state's addend
-          if ((rc = products(a, true))) return rc;
-          const u32 cnt = (a.i1 - a.i0) * (a.j1 - a.j0) * B;
-          KsIo io{d, pl, 0, state_out + at, {state_in ? 1u : 0u, state_in ? 1u : 0u}, nullptr, 0};
-          io.add2 = state_in ? state_in + at : nullptr;
-          io.more = KS_MAPPED;
-          io.more_args.B = B;
-          io.more_args.i0 = a.i0;
-          io.more_args.j0 = a.j0;
-          io.more_args.nj = a.j1 - a.j0;
-          io.more_args.x = a.x;
-          io.more_args.y = a.y;
-          if ((rc = keyswitch_impl(c, io, cnt, nlimbs, mult_key, ks, st))) return rc;
+          if ((rc = relin_products(state_out + at, state_in ? state_in + at : nullptr, a))) return rc;
           continue;
         }
         a.add = state_in ? state_in + at : nullptr;   // Relin(d) + S = Relin(d + (S, 0))
@@ -387,8 +446,8 @@ struct LinAttn {
       if ((rc = relin(y, d + (u64)n * 3 * pl, (size_t)(n2 - 1) * n))) return rc;
     }
     // the sum of the first group's relinearisation and the others' rotations in the extended basis
-    if ((rc = ext_digits(c, lt, d0 + 2 * pl, 3 * pl, n, nlimbs, ks, st))) return rc;
-    RotSumArgs r = rot_sum_args(c, lt, nlimbs, total, 3 * pl);
+    if ((rc = ext_digits(c, lt, whole, d0 + 2 * pl, 3 * pl, n, nlimbs, ks, st))) return rc;
+    RotSumArgs r = rot_sum_args(c, lt, whole, nlimbs, total, 3 * pl);
     r.base = d0;
     r.base_stride = 3 * pl;
     r.nterms = 1;
@@ -398,9 +457,9 @@ struct LinAttn {
     for (u32 g0 = 0; g0 < others; g0 += per) {
       const u32 cnt = std::min(per, others - g0);
       const u64* yg = y + (u64)g0 * n * ct;
-      if ((rc = ext_digits(c, lt, yg + pl, ct, cnt * n, nlimbs, ks, st))) return rc;
+      if ((rc = ext_digits(c, lt, whole, yg + pl, ct, cnt * n, nlimbs, ks, st))) return rc;
       const u64* ext = (const u64*)(ks + ks_layout(c, cnt * n, nlimbs).ext);
-      RotSumArgs s = rot_sum_args(c, lt, nlimbs, total, ct);
+      RotSumArgs s = rot_sum_args(c, lt, whole, nlimbs, total, ct);
       s.accumulate = 1;
       s.nterms = cnt;
       for (u32 g = 0; g < cnt; g++)
@@ -408,15 +467,15 @@ struct LinAttn {
                             giant_keys[g0 + g], giant[g0 + g]};
       if ((rc = launch_rot_sum(c, s, n, st))) return rc;
     }
-    return ext_mod_down(c, lt, total, o, n, nlimbs, ks, st);
+    return ext_mod_down(c, lt, whole, total, o, n, nlimbs, ks, st);
   }
 
   // out = in + its rotations by the elements, one ModDown for all of them; n <= slice ciphertexts
   int sum_rotations(u64* out, const u64* in, u32 n, const std::vector<u32>& elements, const u64* const* keys) {
     int rc;
     u64* acc = (u64*)(ks + ks_layout(c, n, nlimbs).acc);
-    if ((rc = rotations_to_ext(c, lt, in, n, nlimbs, elements.data(), keys, (u32)elements.size(), nullptr, 1, acc, ks, st))) return rc;
-    return ext_mod_down(c, lt, acc, out, n, nlimbs, ks, st);
+    if ((rc = rotations_to_ext(c, lt, whole, in, n, nlimbs, elements.data(), keys, (u32)elements.size(), nullptr, 1, acc, ks, st))) return rc;
+    return ext_mod_down(c, lt, whole, acc, out, n, nlimbs, ks, st);
   }
 
   // d = sum_{s <= t} p_ts * v_s for tokens [t0, t0 + T)
@@ -442,10 +501,14 @@ struct LinAttn {
         a.out = d;
         a.tri_first = first + i;
         a.tri_out = cnt;
-        if ((rc = products(a))) return rc;
         u64* to = p + i * B * ct;
         u64* stage = n1 > 1 || n2 > 1 ? y : to;
-        if ((rc = relin(stage, d, (size_t)cnt * B))) return rc;
+        if (two_pass(c) && c->tune[3] != 1) {
+          if ((rc = relin_products(stage, nullptr, a))) return rc;
+        } else {
+          if ((rc = products(a))) return rc;
+          if ((rc = relin(stage, d, (size_t)cnt * B))) return rc;
+        }
         if (n1 > 1) {
           u64* next = n2 > 1 ? sums : to;
           if ((rc = sum_rotations(next, stage, cnt * B, baby, baby_keys))) return rc;
@@ -580,6 +643,7 @@ int ckks_rope(ckks_ctx* c, uint64_t* ct_out, const uint64_t* ct_in, uint32_t B, 
     if (!guard.ok) return fail(CKKS_EHIP, "cannot select the context's device");
     hipStream_t st = (hipStream_t)stream;
     const u64* in = (const u64*)ct_in;
+    const bool whole = whole_limb(c, B, nlimbs, false);
     if (R == 1 && two_pass(c) && c->tune[3] != 1) {
       // one rotation: the weights join the fused kernels of a key switch, whose digits never reach memory in the evaluation domain
       const u64 pl = (u64)nlimbs * c->N;
@@ -590,10 +654,10 @@ int ckks_rope(ckks_ctx* c, uint64_t* ct_out, const uint64_t* ct_in, uint32_t B, 
       return keyswitch_impl(c, io, B, nlimbs, (const u64*)evks[0], (char*)ws, st);
     }
     u64* acc = (u64*)((char*)ws + ks_layout(c, B, nlimbs).acc);
-    if ((rc = rotations_to_ext(c, lt, (const u64*)ct_in, B, nlimbs, galois_elts, (const u64* const*)evks, R, (const u64*)pt_ext,
+    if ((rc = rotations_to_ext(c, lt, whole, (const u64*)ct_in, B, nlimbs, galois_elts, (const u64* const*)evks, R, (const u64*)pt_ext,
                                B / npt, acc, (char*)ws, st)))
       return rc;
-    return ext_mod_down(c, lt, acc, (u64*)ct_out, B, nlimbs, (char*)ws, st);
+    return ext_mod_down(c, lt, whole, acc, (u64*)ct_out, B, nlimbs, (char*)ws, st);
   });
 }
 

@@ -154,7 +154,7 @@ static const char* const kProfNames[PK_COUNT] = {
     "ntt16_bconv_rows_kernel<0>", "ntt16_bconv_rows_kernel<1>", "ntt16_bconv_rows_kernel<2>", "moddown_kernel", "ks_final_kernel", "tensor_kernel",
     "pmacc_int_kernel", "pmacc_fp_kernel", "addto_kernel",
     "ks12_front_kernel", "ks12_digits_kernel", "ks12_special_kernel", "ks12_final_kernel", "conv_rows_kernel", "copy",
-    "pmacc_int_staged_kernel", "pmacc_fp_staged_kernel", "rot_sum_fp_kernel", "rot_sum_int_kernel", "prod_sum_kernel"};
+    "pmacc_int_staged_kernel", "pmacc_fp_staged_kernel", "rot_sum_kernel<0>", "rot_sum_kernel", "prod_sum_kernel"};
 struct ProfRec {
   int kind;
   hipEvent_t start, stop;
@@ -1680,24 +1680,17 @@ int hrot_hoisted16(ckks_ctx* c, u64* out_base, u64 out_stride, const u64* ct_in,
   return CKKS_OK;
 }
 
-// Ring 2^12: front, digits, special, final (ks12.hip.h).
-int keyswitch_whole12(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B, u32 nlimbs, const u64* evk, char* ws,
-                      hipStream_t st) {
-  if (io.galois_pc && B > KS_MULTI_MAX) return fail(CKKS_ESHAPE, "internal: per-ciphertext keys for too many ciphertexts");
+// What the context and the level fix of the kernels of ring 2^12, and where they put what they leave (a key-switch workspace).
+Ks12Args ks12_args(const ckks_ctx* c, const LevelTables* lt, u32 B, u32 nlimbs, char* ws) {
   const KsLayout L = ks_layout(c, B, nlimbs);
   Ks12Args a;
-  a.d = io.d;
-  a.d_stride = io.d_stride;
-  a.pa = io.prod_a;
-  a.pb = io.prod_b;
+  a.d = a.pa = a.pb = a.evk = a.add2 = a.add_src = nullptr;
+  a.d_stride = 0;
+  a.out = nullptr;
+  a.mode0 = a.mode1 = a.add2_three = a.d_galois = a.add_galois = a.multi = 0;
   a.dcoef = (u64*)(ws + L.dcoef);
   a.ext = (u64*)(ws + L.ext);
   a.acc = (u64*)(ws + L.acc);
-  a.out = io.out;
-  a.evk = evk;
-  a.add2 = io.add2 ? io.add2 : io.out;
-  a.add_src = io.add_src;
-  a.add2_three = io.add2 && io.add2_three ? 1u : 0u;
   a.tw = c->d_tw_fwd;
   a.twi = c->d_tw_inv;
   a.twfp = c->d_twfp_fwd;
@@ -1722,13 +1715,9 @@ int keyswitch_whole12(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
   for (u32& w : a.fp_mask) w = 0;
   for (u32 i = 0; i < c->nm; i++)
     if (host_class(c, c->mod[i]) == 0) a.fp_mask[i >> 5] |= 1u << (i & 31);
-  a.mode0 = io.mode[0];
-  a.mode1 = io.mode[1];
-  a.d_galois = io.d_galois;
-  a.add_galois = io.add_galois;
-  a.multi = io.galois_pc ? 1u : 0u;
-  if (io.galois_pc)
-    for (u32 i = 0; i < B; i++) a.galois_pc[i] = io.galois_pc[i], a.evk_pc[i] = io.evk_pc[i];
+  return a;
+}
+void launch_ks12_digits(const ckks_ctx* c, const LevelTables* lt, u32 B, u32 nlimbs, const Ks12Args& a, hipStream_t st) {
   const dim3 block(WL_THREADS);
   {
     ProfScope ps(c, PK_KS12_FRONT, st);
@@ -1740,6 +1729,31 @@ int keyswitch_whole12(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
     if (lt->narrow_up) hipLaunchKernelGGL(ks12_digits_kernel<true>, grid, block, 0, st, a);
     else hipLaunchKernelGGL(ks12_digits_kernel<false>, grid, block, 0, st, a);
   }
+}
+
+// Ring 2^12: front, digits, special, final (ks12.hip.h).
+int keyswitch_whole12(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B, u32 nlimbs, const u64* evk, char* ws,
+                      hipStream_t st) {
+  if (io.galois_pc && B > KS_MULTI_MAX) return fail(CKKS_ESHAPE, "internal: per-ciphertext keys for too many ciphertexts");
+  Ks12Args a = ks12_args(c, lt, B, nlimbs, ws);
+  a.d = io.d;
+  a.d_stride = io.d_stride;
+  a.pa = io.prod_a;
+  a.pb = io.prod_b;
+  a.out = io.out;
+  a.evk = evk;
+  a.add2 = io.add2 ? io.add2 : io.out;
+  a.add_src = io.add_src;
+  a.add2_three = io.add2 && io.add2_three ? 1u : 0u;
+  a.mode0 = io.mode[0];
+  a.mode1 = io.mode[1];
+  a.d_galois = io.d_galois;
+  a.add_galois = io.add_galois;
+  a.multi = io.galois_pc ? 1u : 0u;
+  if (io.galois_pc)
+    for (u32 i = 0; i < B; i++) a.galois_pc[i] = io.galois_pc[i], a.evk_pc[i] = io.evk_pc[i];
+  launch_ks12_digits(c, lt, B, nlimbs, a, st);
+  const dim3 block(WL_THREADS);
   {
     ProfScope ps(c, PK_KS12_SPECIAL, st);
     hipLaunchKernelGGL(ks12_special_kernel, dim3(2 * B, c->np), block, 0, st, a);

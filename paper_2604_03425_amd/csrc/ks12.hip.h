@@ -37,6 +37,8 @@ struct Ks12Args {
   u32 multi;               // != 0: ciphertext b uses galois_pc[b] and evk_pc[b]
   u32 galois_pc[KS_MULTI_MAX];
   const u64* evk_pc[KS_MULTI_MAX];
+  const u64* sums = nullptr;   // ks12_*_sums_kernel: [B][2][next][4096], the sums of the digits' products with keys, canonical (with the
+                               // factor 2^-64 on integer classes), formed elsewhere; acc may be the same array
 };
 
 // The constants of a modulus, by scalar loads also where the compiler moves them behind stores and barriers.
@@ -234,15 +236,23 @@ __device__ __forceinline__ void ks12_inner(typename Ks12Mod<FP>::V (&s)[4], cons
   for (int k = 0; k < 4; k++) s[k] = md.settle(s[k]);
 }
 
-// grid = (2B, special limbs): back to coefficient form, scaled by (P/p_k)^-1 / N (times 2^64 on integer classes)
 template <bool FP>
+__device__ __forceinline__ void ks12_load_sums(typename Ks12Mod<FP>::V (&s)[4], const Ks12Args& a, u32 bc, u32 t, const Ks12Mod<FP>& md) {
+  const u64* p = a.sums + ((size_t)bc * a.next + t) * 4096;
+#pragma unroll
+  for (int k = 0; k < 4; k++) s[k] = md.settle(md.load(p[wl_elem(2, k)]));
+}
+
+// grid = (2B, special limbs): back to coefficient form, scaled by (P/p_k)^-1 / N (times 2^64 on integer classes)
+template <bool FP, bool SUMS = false>
 __device__ __forceinline__ void ks12_special(const Ks12Args& a, u64* sm) {
   const u32 bc = blockIdx.x, t = a.nlimbs + blockIdx.y, id = t - a.nlimbs + a.nq;
   const Ks12Mod<FP> md(ks12_mod(a.mods, id));
   typename Ks12Tables<FP>::W w;
   w.load(Ks12Tables<FP>::inv(a, id));
   typename Ks12Mod<FP>::V s[4];
-  ks12_inner<FP>(s, a, bc >> 1, bc & 1, t, id, md);
+  if (SUMS) ks12_load_sums<FP>(s, a, bc, t, md);
+  else ks12_inner<FP>(s, a, bc >> 1, bc & 1, t, id, md);
   u64 y[4];
   ulonglong2 sc;
   scalar_fetch(sc, a.dn_scale, t - a.nlimbs);
@@ -253,7 +263,7 @@ __device__ __forceinline__ void ks12_special(const Ks12Args& a, u64* sm) {
 }
 
 // grid = (2B, nlimbs)
-template <bool FP, bool NARROW>
+template <bool FP, bool NARROW, bool SUMS = false>
 __device__ __forceinline__ void ks12_final(const Ks12Args& a, u64* sm) {
   const u32 bc = blockIdx.x, i = blockIdx.y, b = bc >> 1, c = bc & 1;
   const Ks12Mod<FP> md(ks12_mod(a.mods, i));
@@ -279,7 +289,8 @@ __device__ __forceinline__ void ks12_final(const Ks12Args& a, u64* sm) {
   for (int k = 0; k < 4; k++) x[k] = md.load(y[k]);
   md.forward(x, w, sm);
   typename Ks12Mod<FP>::V s[4];
-  ks12_inner<FP>(s, a, b, c, i, i, md);
+  if (SUMS) ks12_load_sums<FP>(s, a, bc, i, md);
+  else ks12_inner<FP>(s, a, b, c, i, i, md);
   ulonglong2 pv;
   scalar_fetch(pv, a.pinv, i);
   const size_t o0 = (size_t)b * 2 * pl + lo, o1 = o0 + pl;
@@ -318,3 +329,7 @@ KS12_KERNEL(ks12_digits_kernel,
 KS12_KERNEL(ks12_special_kernel, ks12_fp(a, a.nq + blockIdx.y), ks12_special<true>, ks12_special<false>)
 template <bool NARROW>
 KS12_KERNEL(ks12_final_kernel, ks12_fp(a, blockIdx.y), (ks12_final<true, NARROW>), (ks12_final<false, NARROW>))
+// The second half of a key switch from sums that another kernel formed.
+KS12_KERNEL(ks12_special_sums_kernel, ks12_fp(a, a.nq + blockIdx.y), (ks12_special<true, true>), (ks12_special<false, true>))
+template <bool NARROW>
+KS12_KERNEL(ks12_final_sums_kernel, ks12_fp(a, blockIdx.y), (ks12_final<true, NARROW, true>), (ks12_final<false, NARROW, true>))

@@ -380,20 +380,37 @@ __device__ __forceinline__ const u64* prod_operand(const ProdOperand& p, u32 idx
 // What a key switch can do beside the plain one (MORE of the fused kernels; KS_PLAIN leaves no trace of it in them):
 // KS_WEIGHTED: out = (w_1 acc - correction) / P + w_0 add_src + [c = 0] w_1 sigma(add_src), the weighted sum of a ciphertext and one
 //   rotation; w_r of set s at w + (s*2 + r)*next*N over the extended basis, ciphertext b takes set b / per_set;
-// KS_MAPPED: the first two terms of the product x(j) * y(i) are added, for output b = ((i - i0)*nj + j - j0)*B + lanes' ciphertext,
-//   and fin_add2 where a component's mode says so. d holds the third.
+// KS_MAPPED: the first two terms of the products x(j, s) * y(i, s), s < ns, are added, for output b = ((i - i0)*nj + j - j0)*B + lanes'
+//   ciphertext (tri: for pair number tri_first + b / B, pairs j <= i at i (i + 1) / 2 + j), and fin_add2 where a component's mode
+//   says so. d holds the third.
 enum { KS_PLAIN = 0, KS_WEIGHTED = 1, KS_MAPPED = 2 };
 struct KsMore {
   const u64* w;
   u32 per_set;
-  u32 B, i0, j0, nj;
+  u32 B, i0, j0, nj, ns, tri;
+  u64 tri_first;
   ProdOperand x, y;
 };
-__device__ __forceinline__ void ks_mapped(const KsMore& m, u32 b, size_t ct, const u64*& x, const u64*& y) {
-  const u32 o = b / m.B, lanes = b % m.B;
-  x = uniform_ptr(prod_operand(m.x, m.j0 + o % m.nj, 0, ct) + lanes * ct);
-  y = uniform_ptr(prod_operand(m.y, m.i0 + o / m.nj, 0, ct) + lanes * ct);
-}
+struct KsMapped {
+  u32 i, j, lanes;
+  __device__ __forceinline__ KsMapped(const KsMore& m, u32 b) {
+    const u32 o = b / m.B;
+    lanes = b % m.B;
+    i = m.tri ? 0 : m.i0 + o / m.nj;
+    j = m.tri ? 0 : m.j0 + o % m.nj;
+    if (m.tri) {
+      const u64 pair = m.tri_first + o;
+      while ((u64)(i + 1) * (i + 2) / 2 <= pair) i++;
+      j = (u32)(pair - (u64)i * (i + 1) / 2);
+    }
+  }
+  __device__ __forceinline__ const u64* x(const KsMore& m, u32 s, size_t ct) const {
+    return uniform_ptr(prod_operand(m.x, j, s, ct) + lanes * ct);
+  }
+  __device__ __forceinline__ const u64* y(const KsMore& m, u32 s, size_t ct) const {
+    return uniform_ptr(prod_operand(m.y, i, s, ct) + lanes * ct);
+  }
+};
 
 struct FwdInnerArgs {
   const u64* ext;   // [B][beta][next][N], after the row pass
@@ -601,22 +618,33 @@ __device__ __forceinline__ void fwd_inner_c_body_fp(const FwdInnerArgs& a, u32 b
           x[i] += fp_mulmod_var(u2d(as[galois_src_index(pos + i * 16, a.fin_galois, LOGN)]), u2d(w1[pos + i * 16]), qinv, q);
       }
     } else {
-      const u64 *px, *py;
-      ks_mapped(a.more, b, 2 * pl, px, py);
+      const KsMapped at(a.more, b);
       const u32 mode = c ? a.fin_mode1 : a.fin_mode0;
-      const size_t at = (size_t)t * N + pos;
+      const size_t word = (size_t)t * N + pos;
+      const u64 *px = at.x(a.more, 0, 2 * pl) + word, *py = at.y(a.more, 0, 2 * pl) + word;
       take(x);
       ntt16_fwd_blocks_fp_words<true>(x, tw, q, qinv, tile, R, ex, twl, [] {}, [&] {
 #pragma unroll
-        for (int i = 0; i < 16; i++) e[i] = px[at + i * 16];
+        for (int i = 0; i < 16; i++) e[i] = px[i * 16];
       });
 #pragma unroll
-      for (int i = 0; i < 16; i++)
-        x[i] = fp_mulmod_const(fp_reduce(acc[i], qinv, q) - x[i], pv.x, pv.y, q) +
-               fp_mulmod_var(u2d(e[i]), u2d(py[at + (c ? pl : 0) + i * 16]), qinv, q);
-      if (c) {
+      for (int i = 0; i < 16; i++) x[i] = fp_mulmod_const(fp_reduce(acc[i], qinv, q) - x[i], pv.x, pv.y, q);
+#pragma nounroll
+      for (u32 s = 0;;) {   // at most 3.6 q on top of what is below q
 #pragma unroll
-        for (int i = 0; i < 16; i++) x[i] += fp_mulmod_var(u2d(px[at + pl + i * 16]), u2d(py[at + i * 16]), qinv, q);
+        for (int i = 0; i < 16; i++) x[i] += fp_mulmod_var(u2d(e[i]), u2d(py[(c ? pl : 0) + i * 16]), qinv, q);
+        if (c) {
+#pragma unroll
+          for (int i = 0; i < 16; i++) x[i] += fp_mulmod_var(u2d(px[pl + i * 16]), u2d(py[i * 16]), qinv, q);
+        }
+        if (++s == a.more.ns) break;
+        px = at.x(a.more, s, 2 * pl) + word, py = at.y(a.more, s, 2 * pl) + word;
+#pragma unroll
+        for (int i = 0; i < 16; i++) e[i] = px[i * 16];
+        if ((s & 1) == 0) {
+#pragma unroll
+          for (int i = 0; i < 16; i++) x[i] = fp_reduce(x[i], qinv, q);
+        }
       }
       if (mode & 1) {
         const u64* a2 = a.fin_add2 + ((size_t)bc * a.nlimbs + t) * N + pos;
@@ -896,19 +924,23 @@ ntt16_fwd_blocks_inner8_kernel(FwdInnerArgs a) {
             x[k] = addmod(x[k], mont_plain(as[galois_src_index(posC + k, a.fin_galois, a.logN)], f[k], r2, q, mi.minv), q);
         }
       } else if (MORE == KS_MAPPED) {
-        const u64 *px, *py;
-        const size_t pl = (size_t)a.nlimbs * N, at = (size_t)t * N + posC;
-        ks_mapped(a.more, b, 2 * pl, px, py);
-        u64 f[8];
-        inner8_load(ev, px + at);
-        inner8_load(f, py + at + (c ? pl : 0));
+        const KsMapped at(a.more, b);
+        const size_t pl = (size_t)a.nlimbs * N, word = (size_t)t * N + posC;
+        // two words at a time: whole operands beside x and the other component's sums spill
+        auto add_products = [&](const u64* p, const u64* r) {
 #pragma unroll
-        for (int k = 0; k < 8; k++) x[k] = addmod(x[k], mont_plain(ev[k], f[k], r2, q, mi.minv), q);
-        if (c) {
-          inner8_load(ev, px + at + pl);
-          inner8_load(f, py + at);
-#pragma unroll
-          for (int k = 0; k < 8; k++) x[k] = addmod(x[k], mont_plain(ev[k], f[k], r2, q, mi.minv), q);
+          for (int k = 0; k < 4; k++) {
+            const inner8_pair u = *(const inner8_pair*)(p + 2 * k), v = *(const inner8_pair*)(r + 2 * k);
+            x[2 * k] = addmod(x[2 * k], mont_plain(u.x, v.x, r2, q, mi.minv), q);
+            x[2 * k + 1] = addmod(x[2 * k + 1], mont_plain(u.y, v.y, r2, q, mi.minv), q);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        };
+#pragma nounroll
+        for (u32 s = 0; s < a.more.ns; s++) {
+          const u64 *px = at.x(a.more, s, 2 * pl) + word, *py = at.y(a.more, s, 2 * pl) + word;
+          add_products(px, py + (c ? pl : 0));
+          if (c) add_products(px + pl, py);
         }
         if (mode & 1) {
           inner8_load(ev, a.fin_add2 + (((size_t)b * 2 + c) * a.nlimbs + t) * N + posC);

@@ -23,6 +23,7 @@ PARAMS = {
     "ring10": lambda: make_params(10, 4, 50, 2, 60, 2),
     "ring11": lambda: make_params(11, 3, 60, 1, 60, 3),
     "ring12": lambda: make_params(12, 5, 45, 2, 60, 3),
+    "ring12_steps": lambda: make_params(12, 12, 50, 4, 60, 3),   # large batches of it leave the whole-limb kernels
     "ring13": lambda: make_params(13, 4, 50, 2, 60, 2),
     "ring13_int": lambda: make_params(13, 5, 60, 2, 60, 3),
     "ring13_mixed": lambda: _mixed(13),
@@ -137,6 +138,15 @@ def test_work_in_slices():
     """More ciphertexts than one key switch takes at a time: products of the state, tokens of the read, pairs of the scores."""
     _run("step", "ring16", 2, 24, 1, 3, 2, True, True, check=[0, 23])
     _run("chunk", "ring16", 2, 40, 3, 2, 1, True, False, check=[0, 39])
+
+
+def test_ring_12_in_both_forms():
+    """By whole limbs and, from 64 ciphertexts of 12 limbs on, one kernel per step."""
+    test_rope_matches_the_oracle("ring12_steps", 12, 3, 3, 2)
+    test_rope_matches_the_oracle("ring12_steps", 12, 66, 2, 2)
+    _run("step", "ring12_steps", 12, 66, 1, 2, 1, True, True, check=[0, 65])
+    _run("chunk", "ring12_steps", 12, 33, 2, 1, 2, True, False, check=[0, 32])
+    _run("chunk", "ring12_steps", 11, 1, 2, 2, 2, True, False)
 
 
 def test_work_in_more_slices():
