@@ -662,11 +662,18 @@ int ckks_rope(ckks_ctx* c, uint64_t* ct_out, const uint64_t* ct_in, uint32_t B, 
 }
 
 size_t ckks_linattn_workspace_bytes(const ckks_ctx* c, int op, uint32_t tokens, uint32_t B, uint32_t nlimbs, uint32_t n1, uint32_t n2) {
-  if ((op != CKKS_OP_LINATTN_STEP && op != CKKS_OP_LINATTN_CHUNK) || linattn_check(c, tokens, B, nlimbs, n1, n2)) return 0;
-  if (op == CKKS_OP_LINATTN_STEP && tokens != 1) return 0;
-  LinAttn f;
-  f.shape(c, tokens, B, nlimbs, n1, n2);
-  return f.carve(nullptr, op == CKKS_OP_LINATTN_CHUNK);
+  size_t bytes = 0;
+  guarded([&]() -> int {
+    if ((op != CKKS_OP_LINATTN_STEP && op != CKKS_OP_LINATTN_CHUNK) || (op == CKKS_OP_LINATTN_STEP && tokens != 1))
+      return fail(CKKS_EINVAL, "not a linear-attention operation");
+    const int rc = linattn_check(c, tokens, B, nlimbs, n1, n2);
+    if (rc) return rc;
+    LinAttn f;
+    f.shape(c, tokens, B, nlimbs, n1, n2);
+    bytes = f.carve(nullptr, op == CKKS_OP_LINATTN_CHUNK);
+    return CKKS_OK;
+  });
+  return bytes;
 }
 
 int ckks_linattn_step(ckks_ctx* c, uint64_t* o_out, uint64_t* state_out, const uint64_t* q, const uint64_t* k, const uint64_t* v,

@@ -292,3 +292,55 @@ def test_the_example_decrypts_to_plain_attention():
     spec.loader.exec_module(mod)
     errors = mod.main(logN=12, head=8, tokens=3, new=2, quiet=True)
     assert len(errors) == 5 and max(errors) < 5 * 8 * 3 * 3 * 2.0 ** -25, errors
+
+
+@pytest.mark.parametrize("knob,value", [(0, 0), (1, 1), (2, 1), (2, 2), (3, 1), (4, 0), (5, 1)])
+@pytest.mark.parametrize("name", ["ring13_mixed", "ring16"])
+def test_tuning_knobs_change_no_result(name, knob, value):
+    import paper_2604_03425_amd as ck
+    p, rc, ctx = contexts(name)
+    default = {0: -1, 1: 0, 2: 0, 3: 2, 4: 1, 5: 0}[knob]
+    nl = min(3, len(p.q))
+    ck.ckks_tune_set(ctx, knob, value)
+    try:
+        test_rope_matches_the_oracle(name, nl, 2, 1, 1)
+        test_rope_matches_the_oracle(name, nl, 2, 2, 2)
+        _run("step", name, nl, 1, 1, 2, 1, True, True)
+        _run("chunk", name, nl, 1, 2, 1, 2, True, False)
+    finally:
+        ck.ckks_tune_set(ctx, knob, default)
+
+
+def test_a_state_beyond_2_to_32_words():
+    """64 components of 24 lanes' ciphertexts at the benchmark's ring, 38 GB of state: the last ciphertext alone gives the same."""
+    import paper_2604_03425_amd as ck
+    from ckks_inputs import config_params
+    p = config_params("keyswitch_micro")
+    ctx = ck.Context(p, 0)
+    n1 = n2 = 8
+    nl, B, N = 24, 24, p.N
+    gen = torch.Generator(device="cuda").manual_seed(3)
+
+    def residues(lead, moduli):
+        x = torch.empty(tuple(lead) + (len(moduli), N), dtype=torch.int64, device="cuda")
+        for i, m in enumerate(moduli):
+            x[..., i, :].random_(0, m, generator=gen)
+        return x
+
+    key = lambda: residues((p.dnum, 2), p.moduli)   # noqa: E731
+    keys = (key(), [key()] * (n1 - 1), [key()] * (n2 - 1), [key()] * (n2 - 1))
+    q, k, v = (residues((1, B, 2), p.q) for _ in range(3))
+    decay = residues((), p.q)
+    state = residues((n2, n1, B, 2), p.q)
+    assert state.numel() > 1 << 32
+    last = state[:, :, -1:].contiguous()
+    o = torch.empty_like(q)
+    ck.ckks_linattn_step(ctx, o, state, q, k, v, state, decay, B, nl, n1, n2, N // 128, *keys,
+                         ctx.linattn_workspace(ck.OP_LINATTN_STEP, 1, B, nl, n1, n2))
+    one, ql, kl, vl = torch.empty_like(o[:, :1]), *(x[:, -1:].contiguous() for x in (q, k, v))
+    ck.ckks_linattn_step(ctx, one, last, ql, kl, vl, last, decay, 1, nl, n1, n2, N // 128, *keys,
+                         ctx.linattn_workspace(ck.OP_LINATTN_STEP, 1, 1, nl, n1, n2))
+    torch.cuda.synchronize()
+    assert torch.equal(o[:, -1:], one) and torch.equal(state[:, :, -1:], last)
+    del state, last, ctx
+    torch.cuda.empty_cache()
