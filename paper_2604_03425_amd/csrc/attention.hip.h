@@ -9,7 +9,7 @@
 //                 + sum_r w_r[t][n] ( sum_j D_rj[pi_r(n)] evk_r[j][c][id(t)][n] + [c = 0, main primes] P c0_r[b][t][pi_r(n)] ),
 // pi_r the evaluation-domain index map of term r. D_rj is digit j of the term's polynomial in the extended basis: d_r itself on
 // the limbs that the digit holds, the transformed conversions in ext_r elsewhere. Without weights every w is one. On integer
-// moduli of the two-pass rings acc carries the factor 2^-64 that ModDown's constants expect there. A launch computes `outs` such
+// moduli acc carries the factor 2^-64 that ModDown's constants expect there (not on rings that go one kernel per step). A launch computes `outs` such
 // sums from nterms terms each, the accumulators one after another; base belongs to the first.
 struct RotTerm {
   const u64* ext;   // [B][beta][next][N]
@@ -25,7 +25,8 @@ struct RotSumArgs {
   u64* acc;             // [outs][B][2][next][N]
   const ModInfo* mods;
   u64 d_stride;
-  u32 logN, nlimbs, nq, nm, alpha, beta, next, B, nterms, w_first, w_terms, per_set, accumulate, nfp, doubles;   // doubles: ext holds doubles on moduli < 2^50
+  u32 logN, nlimbs, nq, nm, alpha, beta, next, B, nterms, w_first, w_terms, per_set, accumulate, nfp;
+  u32 doubles;          // != 0: ext holds doubles on moduli below 2^50
   unsigned char slots[128];
   RotTerm term[ROT_SUM_TERMS];
 };
@@ -48,8 +49,8 @@ __device__ __forceinline__ void attention_map(u32& what, u32& blk, u32& zi) {
   zi = unit / gridDim.y;
 }
 
-// Moduli below 2^50 where ext holds doubles (rings 2^12 .. 2^16): sums in doubles (|.| < 2^53 = 8q throughout). A lane owns a position of
-// CB ciphertexts, which share the key words. What bounds it is memory, the last-level cache's share included: two rotations of 16
+// Moduli below 2^50 where ext holds doubles: sums in doubles (|.| < 2^53 = 8q throughout). A lane owns a position of CB ciphertexts, which
+// share the key words. What bounds it is memory, the last-level cache's share included: two rotations of 16
 // ciphertexts of 20 limbs, 4 digits, move 2.4 GB in 477 us. CB = 2: with 4 there are fewer waves to hide the gathers (512 us), with 1
 // every ciphertext fetches the keys again (590). With all digits of a term requested ahead, which costs registers, 513 and 550.
 // By (ciphertexts, limb) on an XCD instead, which finds more digits and fewer key words in its L2, 504.
@@ -136,8 +137,9 @@ __device__ __forceinline__ void rot_sum_fp(const RotSumArgs& a, u32 what, u32 bl
   }
 }
 
-// All other moduli: residues in ext, Montgomery products, sums below 2m. PLAIN: acc without the factor 2^-64 (rings whose ModDown
-// takes none). Grid and lanes as above.
+// All other moduli: residues in ext, Montgomery products, sums below 2m. PLAIN: acc without the factor 2^-64. Grid and lanes as above. The 5
+// special limbs of the rotations above take 130 us, nearly three times a double-precision limb: 18 Montgomery products of 12
+// multiplies a position and rotation bound it, not memory; in 128-bit sums with a reduction each 163.
 template <int CB, bool PLAIN>
 __device__ __forceinline__ void rot_sum_int(const RotSumArgs& a, u32 what, u32 blk, u32 zi) {
   const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, comp = (size_t)a.nm * N;
@@ -258,6 +260,9 @@ __device__ __forceinline__ u64 prod_mulmod(u64 x, u64 y, const ModInfo& mi) {
 
 // A lane keeps one position of a tile of TI x TJ outputs, so that a word of x serves TI of them and a word of y TJ. FIRST = 2: only the
 // third component of every product, [i1 - i0][j1 - j0][B][nlimbs][N].
+// What bounds it: memory. At 2^16: the update of 32 outputs from 4 tokens and the read of 32 for 4 tokens, 8 limbs, 1.8 GB in 398 us
+// (one output per lane 820); the read of 64 outputs of 9 limbs with their decay, 1.4 GB in 257 us; the third components of 64
+// outputs of one token, 0.38 GB in 91 us. A copy of 4 GB runs at 4.8 TB/s on this card. Larger tiles cost the waves that hide the loads.
 // grid = (tiles * B, N / 256, limbs)
 template <bool FP, int TI, int TJ, int FIRST>
 __global__ void __launch_bounds__(256) prod_sum_kernel(ProdSumArgs a) {

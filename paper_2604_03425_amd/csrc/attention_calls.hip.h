@@ -182,8 +182,8 @@ int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* 
 }
 
 // ---- linear attention ----
-// Ciphertexts that one key switch of the calls below works on at a time: at least the B of a token. Enough to fill the chip
-// many times over; more would only take workspace.
+// Ciphertexts that one key switch of the calls below works on at a time: at least the B of a token, else what fills the chip many times
+// over (a pass over 128 of 9 limbs at 2^16 is two dozen rounds of workgroups); more would only take workspace, 15 GB of it at 24 limbs.
 u32 linattn_slice(const ckks_ctx* c, u32 B) { return std::max<u32>(B, std::min(1024u, 128u << (c->logN < 16 ? 16 - c->logN : 0))); }
 
 // Tokens up to which the key switches of a state's update form the first two terms of the sums of products themselves. us, that way |
@@ -272,7 +272,9 @@ struct LinAttn {
   int rotations_apart(u64* to, const u64* ext, const u64* in, u32 n, const u32* elements, const u64* const* keys, u32 R) {
     int rc;
     const u64 stride = n * 2 * (u64)lt->next * c->N;
-    const bool streamed = two_pass(c) && lt->beta <= INNER16_ROT_MAX_BETA;   // keeps the digits of a position for all rotations
+    // the kernel that keeps a position's digits for all rotations: a chunk of 4 tokens of 32 components 4236 us, by sums of one term each
+    // 4395; a token of 64 components, whose keys are read once either way, 3395 and 3357
+    const bool streamed = two_pass(c) && lt->beta <= INNER16_ROT_MAX_BETA;
     const u32 most = streamed ? KS_MULTI_MAX : ROT_SUM_TERMS;
     for (u32 r0 = 0; r0 < R; r0 += most) {
       const u32 rots = std::min(most, R - r0);
@@ -291,7 +293,8 @@ struct LinAttn {
     return CKKS_OK;
   }
   // All rotations of a call at once, where they are few: queries (if the state is read), keys and values side by side go through one
-  // decomposition and one ModDown, which takes a third of the launches.
+  // decomposition and one ModDown, which takes a third of the launches. us, all at once | one after another: a token of 4 components at
+  // 2^13 288 | 378, of 16 at 2^14 833 | 933, of 64 at 2^16 3395 | 3425; a chunk of 4 tokens of 32 components 4236 | 4452.
   bool joint(bool with_q) const {
     const u64 baby_cts = (with_q ? 2 : 1) * (u64)(n1 - 1), all = (baby_cts + n2 - 1) * C * B;
     return all && all <= slice && (with_q ? 3u : 2u) * (u64)C * B <= slice;
@@ -645,7 +648,10 @@ int ckks_rope(ckks_ctx* c, uint64_t* ct_out, const uint64_t* ct_in, uint32_t B, 
     const u64* in = (const u64*)ct_in;
     const bool whole = whole_limb(c, B, nlimbs, false);
     if (R == 1 && two_pass(c) && c->tune[3] != 1) {
-      // one rotation: the weights join the fused kernels of a key switch, whose digits never reach memory in the evaluation domain
+      // One rotation: the weights join the fused kernels of a key switch, whose digits never reach memory in the evaluation domain. us,
+      // that way | through sums of rotations: 24 limbs at 2^16, 1, 4, 16, 64 ciphertexts 147 | 185, 367 | 462, 1287 | 1596, 5105 |
+      // 6416; 5 limbs at 2^13, 1, 8, 64: 52 | 55, 63 | 72, 140 | 194; 8 60-bit limbs at 2^15, 1, 8: 76 | 74, 165 | 186. Two rotations would
+      // convert the digits twice.
       const u64 pl = (u64)nlimbs * c->N;
       KsIo io{in + pl, 2 * pl, galois_elts[0], (u64*)ct_out, {0, 0}, in, galois_elts[0]};
       io.more = KS_WEIGHTED;
