@@ -50,10 +50,11 @@ __device__ __forceinline__ void attention_map(u32& what, u32& blk, u32& zi) {
 }
 
 // Moduli below 2^50 where ext holds doubles: sums in doubles (|.| < 2^53 = 8q throughout). A lane owns a position of CB ciphertexts, which
-// share the key words. What bounds it is memory, the last-level cache's share included: two rotations of 16
-// ciphertexts of 20 limbs, 4 digits, move 2.4 GB in 477 us. CB = 2: with 4 there are fewer waves to hide the gathers (512 us), with 1
-// every ciphertext fetches the keys again (590). With all digits of a term requested ahead, which costs registers, 513 and 550.
-// By (ciphertexts, limb) on an XCD instead, which finds more digits and fewer key words in its L2, 504.
+// share the key words, and asks for the next digit while it multiplies this one. What bounds it is the wait for the gathers: two
+// rotations of 16 ciphertexts of 20 limbs, 4 digits, 492 us, 2.6 GB (5.2 TB/s), vector units 40 % busy. CB = 2: with 4 there are fewer
+// waves (7 % longer), with 1 every ciphertext fetches the keys again (24 %); nothing asked ahead 526 us, a whole term ahead 550.
+// Both terms side by side in the order of the Galois map's orbits halve the HBM reads (1.2 GB) and take 593 us; four
+// ciphertext pairs of the same positions in a workgroup ask the L2 for a third less, 559; by (ciphertexts, limb) on an XCD 504.
 // grid = (outs * ceil(B / CB), N / 256, slots).
 template <int CB>
 __device__ __forceinline__ void rot_sum_fp(const RotSumArgs& a, u32 what, u32 blk, u32 zi) {
@@ -94,16 +95,26 @@ __device__ __forceinline__ void rot_sum_fp(const RotSumArgs& a, u32 what, u32 bl
     double v0[CB], v1[CB];
 #pragma unroll
     for (int k = 0; k < CB; k++) v0[k] = v1[k] = 0.0;
-    for (u32 j = 0; j < a.beta; j++, e += 2 * comp) {
+    u64 xn[CB], kn[2];
+    auto request = [&](u32 j) {
       const bool own = j == jo;   // uniform: where the digit's words start, and how far its ciphertexts are apart
       const u64* x = own ? d + (size_t)t * N : ext + ((size_t)j * a.next + t) * N;
       const size_t apart = own ? (size_t)a.d_stride : (size_t)a.beta * a.next * N;
+#pragma unroll
+      for (int k = 0; k < CB; k++) xn[k] = uniform_load(x + bb[k] * apart, m * 8);
+      kn[0] = uniform_load(e, n * 8), kn[1] = uniform_load(e + comp, n * 8);
+      e += 2 * comp;
+    };
+    request(0);
+    for (u32 j = 0; j < a.beta; j++) {
       u64 xr[CB];
 #pragma unroll
-      for (int k = 0; k < CB; k++) xr[k] = uniform_load(x + bb[k] * apart, m * 8);
-      const double e0 = u2d(uniform_load(e, n * 8)), e1 = u2d(uniform_load(e + comp, n * 8));
+      for (int k = 0; k < CB; k++) xr[k] = xn[k];
+      const double e0 = u2d(kn[0]), e1 = u2d(kn[1]);
+      if (j + 1 < a.beta) request(j + 1);
+      __builtin_amdgcn_sched_barrier(0);
       // residues become doubles by setting the exponent and taking 2^52 away, doubles stay what they are
-      const u64 bias = own ? 0x4330000000000000ull : 0ull;
+      const u64 bias = j == jo ? 0x4330000000000000ull : 0ull;
       const double less = __longlong_as_double((long long)bias);
 #pragma unroll
       for (int k = 0; k < CB; k++) {
@@ -175,13 +186,23 @@ __device__ __forceinline__ void rot_sum_int(const RotSumArgs& a, u32 what, u32 b
       v0[k] = v1[k] = 0;
       if (term.c0 && main_prime) v0[k] = mont_mul63(term.c0[(size_t)bb[k] * a.d_stride + (size_t)t * N + m], mi.pmod, q, mi.minv);
     }
-    for (u32 j = 0; j < a.beta; j++, e += 2 * comp) {
-      u64 x[CB];
+    u64 xn[CB], kn[2];
+    auto request = [&](u32 j) {
 #pragma unroll
       for (int k = 0; k < CB; k++)
-        x[k] = j == jo ? term.d[(size_t)bb[k] * a.d_stride + (size_t)t * N + m]
-                       : term.ext[(((size_t)bb[k] * a.beta + j) * a.next + t) * N + m];
-      const u64 e0 = e[0], e1 = e[comp];
+        xn[k] = j == jo ? term.d[(size_t)bb[k] * a.d_stride + (size_t)t * N + m]
+                        : term.ext[(((size_t)bb[k] * a.beta + j) * a.next + t) * N + m];
+      kn[0] = e[0], kn[1] = e[comp];
+      e += 2 * comp;
+    };
+    request(0);
+    for (u32 j = 0; j < a.beta; j++) {
+      u64 x[CB];
+#pragma unroll
+      for (int k = 0; k < CB; k++) x[k] = xn[k];
+      const u64 e0 = kn[0], e1 = kn[1];
+      if (j + 1 < a.beta) request(j + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int k = 0; k < CB; k++) {
         v0[k] = csub(v0[k] + mont_mul63(x[k], e0, q, mi.minv), q2);
