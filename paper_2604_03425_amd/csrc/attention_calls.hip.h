@@ -190,6 +190,10 @@ u32 linattn_slice(const ckks_ctx* c, u32 B) { return std::max<u32>(B, std::min(1
 // by the kernel of the products, 32 components at 2^16, 8 limbs, 1, 2, 4, 8 tokens: 1934 | 2012, 2665 | 2699, 4415 | 4363, 9338 | 8961;
 // 16 at 2^15, 5 60-bit limbs, 2, 5, 8: 1607 | 1618, 3424 | 3353, 5954 | 5785. Beyond two every output fetches factors that a tile shares.
 #define LINATTN_MAPPED_TOKENS 2
+// Words of a component of a read's products up to which all their groups are relinearised from the same launches. us, so | by the fused
+// kernels: a token of 4 components at 2^13, 5 limbs (2^16 words) 263 | 286, of 16 at 2^15, 6 limbs (2^19.6) 603 | 631, 9 limbs
+// (2^20.2) 761 | 775, three of 16 at 2^14 (2^20.4) 831 | 835, eight (2^21.8) 1734 | 1721, one of 16 at 2^16, 8 groups (2^22.2) 1551 | 1534.
+#define LINATTN_BESIDE_WORDS (1ull << 21)
 
 struct LinAttn {
   const ckks_ctx* cc;      // for sizes
@@ -430,39 +434,41 @@ struct LinAttn {
   int read(u64* o, const u64* q, u32 T, const u64* state, const u64* extra, const u64* fade = nullptr) {
     int rc;
     const u32 n = T * B;
-    const u64* d0 = extra;
-    if (state) {
-      if (!q_rest && (rc = rotate(rot_a, (u64)n * ct, q, n, baby, baby_keys))) return rc;
-      ProdSumArgs a{};
-      a.x = ProdOperand{q, q_rest ? q_rest : rot_a, B, q_rest ? turn_step : n, 2};
-      a.y = ProdOperand{state, nullptr, (u64)n1 * B, B, 0};
-      a.i1 = n2;
-      a.j1 = T;
-      a.ns = n1;
-      a.fade = fade;
-      a.out = d;
-      a.add = extra;
-      a.add_comps = 3;
-      a.add_i = 1;
-      if ((rc = products(a))) return rc;
-      d0 = d;
-      if ((rc = relin(y, d + (u64)n * 3 * pl, (size_t)(n2 - 1) * n))) return rc;
-    }
-    // the sum of the first group's relinearisation and the others' rotations in the extended basis
-    if ((rc = ext_digits(c, lt, whole, d0 + 2 * pl, 3 * pl, n, nlimbs, ks, st))) return rc;
-    RotSumArgs r = rot_sum_args(c, lt, whole, nlimbs, total, 3 * pl);
-    r.base = d0;
+    if (!state) return relin(o, extra, n);
+    if (!q_rest && (rc = rotate(rot_a, (u64)n * ct, q, n, baby, baby_keys))) return rc;
+    ProdSumArgs a{};
+    a.x = ProdOperand{q, q_rest ? q_rest : rot_a, B, q_rest ? turn_step : n, 2};
+    a.y = ProdOperand{state, nullptr, (u64)n1 * B, B, 0};
+    a.i1 = n2;
+    a.j1 = T;
+    a.ns = n1;
+    a.fade = fade;
+    a.out = d;
+    a.add = extra;
+    a.add_comps = 3;
+    a.add_i = 1;
+    if ((rc = products(a))) return rc;
+    // The sum of the first group's relinearisation and the others' rotations in the extended basis. Where they are few, the other groups
+    // are relinearised beside the first one, from the same launches; else by the fused kernels, which move less.
+    const bool beside = n2 > 1 && (u64)n2 * n <= slice && (u64)n2 * n * nlimbs * c->N <= LINATTN_BESIDE_WORDS;
+    const u32 first = beside ? n2 * n : n;
+    u64* sum = beside ? acc : total;
+    if (!beside && (rc = relin(y, d + (u64)n * 3 * pl, (size_t)(n2 - 1) * n))) return rc;
+    if ((rc = ext_digits(c, lt, whole, d + 2 * pl, 3 * pl, first, nlimbs, ks, st))) return rc;
+    RotSumArgs r = rot_sum_args(c, lt, whole, nlimbs, sum, 3 * pl);
+    r.base = d;
     r.base_stride = 3 * pl;
     r.nterms = 1;
-    r.term[0] = RotTerm{(const u64*)(ks + ks_layout(c, n, nlimbs).ext), d0 + 2 * pl, nullptr, mult_key, 1};
-    if ((rc = launch_rot_sum(c, r, n, st))) return rc;
-    const u32 others = state ? n2 - 1 : 0, per = std::min<u32>(ROT_SUM_TERMS, slice / n);
+    r.term[0] = RotTerm{(const u64*)(ks + ks_layout(c, first, nlimbs).ext), d + 2 * pl, nullptr, mult_key, 1};
+    if ((rc = launch_rot_sum(c, r, first, st))) return rc;
+    if (beside && (rc = ext_mod_down(c, lt, whole, sum + (u64)n * 2 * lt->next * c->N, y, (n2 - 1) * n, nlimbs, ks, st))) return rc;
+    const u32 others = n2 - 1, per = std::min<u32>(ROT_SUM_TERMS, slice / n);
     for (u32 g0 = 0; g0 < others; g0 += per) {
       const u32 cnt = std::min(per, others - g0);
       const u64* yg = y + (u64)g0 * n * ct;
       if ((rc = ext_digits(c, lt, whole, yg + pl, ct, cnt * n, nlimbs, ks, st))) return rc;
       const u64* ext = (const u64*)(ks + ks_layout(c, cnt * n, nlimbs).ext);
-      RotSumArgs s = rot_sum_args(c, lt, whole, nlimbs, total, ct);
+      RotSumArgs s = rot_sum_args(c, lt, whole, nlimbs, sum, ct);
       s.accumulate = 1;
       s.nterms = cnt;
       for (u32 g = 0; g < cnt; g++)
@@ -470,7 +476,7 @@ struct LinAttn {
                             giant_keys[g0 + g], giant[g0 + g]};
       if ((rc = launch_rot_sum(c, s, n, st))) return rc;
     }
-    return ext_mod_down(c, lt, whole, total, o, n, nlimbs, ks, st);
+    return ext_mod_down(c, lt, whole, sum, o, n, nlimbs, ks, st);
   }
 
   // out = in + its rotations by the elements, one ModDown for all of them; n <= slice ciphertexts
