@@ -231,13 +231,15 @@ __device__ __forceinline__ void rot_sum_int(const RotSumArgs& a, u32 what, u32 b
   }
 }
 
-// KIND 0: double-precision slots; 1: integer ones; 2: every slot, PLAIN; 3: slots of both kinds in one launch, the first nfp of them
-// double-precision ones (ring 2^12, where a launch more costs more than the registers of the other kind)
+// KIND 0: slots of both arithmetic kinds, the first nfp of them double-precision ones; 1: integer ones only; 2: every slot, PLAIN. Both
+// kinds share a launch, whose integer workgroups (bound by their products) run into the tail of the others (bound by their gathers), and
+// a launch costs more than the registers of the other kind. us, one launch | two: two rotations of 4 ciphertexts of 5 limbs at 2^13
+// 62 | 70, of 4 of 24 limbs at 2^16 512 | 524, of 16 of 20 limbs 1653 | 1664; with the kinds mixed block by block 61, 519, 1745.
 template <int KIND, int CB>
 __global__ void __launch_bounds__(256) rot_sum_kernel(RotSumArgs a) {
   u32 what, blk, zi;
   attention_map(what, blk, zi);
-  if (KIND == 0 || (KIND == 3 && zi < a.nfp)) rot_sum_fp<CB>(a, what, blk, zi);
+  if (KIND == 0 && zi < a.nfp) rot_sum_fp<CB>(a, what, blk, zi);
   else rot_sum_int<CB, KIND == 2>(a, what, blk, zi);
 }
 

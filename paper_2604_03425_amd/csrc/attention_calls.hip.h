@@ -127,32 +127,16 @@ void launch_rot_sum_of(u32 outs, u32 slots, const RotSumArgs& a, hipStream_t st)
 int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 outs = 1) {
   a.B = B;
   const LimbMap emap = ext_map(c, a.nlimbs);
-  unsigned char slots[128];
   u32 cnt = 0;
   for (int fp = 1; fp >= 0; fp--) {   // double-precision slots first
     for (u32 s = 0; s < a.next; s++)
-      if ((a.doubles && host_class(c, c->mod[emap.id[s]]) == 0) == (fp == 1)) slots[cnt++] = (unsigned char)s;
+      if ((a.doubles && host_class(c, c->mod[emap.id[s]]) == 0) == (fp == 1)) a.slots[cnt++] = (unsigned char)s;
     if (fp) a.nfp = cnt;
   }
-  auto take = [&](u32 first, u32 n) { std::copy(slots + first, slots + first + n, a.slots); };
-  if (!two_pass(c)) {
-    ProfScope ps(c, PK_ROT_SUM_INT, st);
-    take(0, cnt);
-    if (a.doubles) launch_rot_sum_of<3>(outs, cnt, a, st);
-    else launch_rot_sum_of<2>(outs, cnt, a, st);
-    HIP_TRY(hipGetLastError());
-    return CKKS_OK;
-  }
-  if (a.nfp) {
-    ProfScope ps(c, PK_ROT_SUM, st);
-    take(0, a.nfp);
-    launch_rot_sum_of<0>(outs, a.nfp, a, st);
-  }
-  if (cnt > a.nfp) {
-    ProfScope ps(c, PK_ROT_SUM_INT, st);
-    take(a.nfp, cnt - a.nfp);
-    launch_rot_sum_of<1>(outs, cnt - a.nfp, a, st);
-  }
+  ProfScope ps(c, PK_ROT_SUM, st);
+  if (!a.doubles) launch_rot_sum_of<2>(outs, cnt, a, st);
+  else if (a.nfp == 0) launch_rot_sum_of<1>(outs, cnt, a, st);
+  else launch_rot_sum_of<0>(outs, cnt, a, st);
   HIP_TRY(hipGetLastError());
   return CKKS_OK;
 }

@@ -10,10 +10,9 @@ def _named(part):
 
 
 @pytest.mark.parametrize("part,count,vgprs", [
-    ("rot_sum_kernelILi0E", 2, 64),                      # 8 waves to a SIMD
+    ("rot_sum_kernelILi0E", 2, 72),                      # 7 waves to a SIMD, 8
     ("rot_sum_kernelILi1E", 2, 64),
     ("rot_sum_kernelILi2E", 2, 64),
-    ("rot_sum_kernelILi3E", 2, 80),
     ("prod_sum_kernelILb1E", 5, 96),
     ("prod_sum_kernelILb0E", 5, 168),
     ("inner_c_kernelILi16ELi1E", 1, 168),                # weighted and mapped: 3 waves, as the plain one
