@@ -166,9 +166,15 @@ int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* 
 }
 
 // ---- linear attention ----
-// Ciphertexts that one key switch of the calls below works on at a time: at least the B of a token, else what fills the chip many times
-// over (a pass over 128 of 9 limbs at 2^16 is two dozen rounds of workgroups); more would only take workspace, 15 GB of it at 24 limbs.
-u32 linattn_slice(const ckks_ctx* c, u32 B) { return std::max<u32>(B, std::min(1024u, 128u << (c->logN < 16 ? 16 - c->logN : 0))); }
+// Ciphertexts that one key switch of the calls below works on at a time: all that the call has to switch at once (components of the
+// state; groups of the read; all rotations and what they are taken from, side by side; scores), up to what fills the chip many times over
+// (a pass over 128 of 9 limbs at 2^16 is two dozen rounds of workgroups) or the B of a token: more would only take workspace. 128 of 24
+// limbs at 2^16 take 31 GB in all, the 4 of a step with 4 components 1 GB.
+u32 linattn_slice(const ckks_ctx* c, bool scores, u32 C, u32 B, u32 n1, u32 n2) {
+  const u64 keyed = (u64)C * B, rotated = std::max<u64>(2 * (u64)(n1 - 1) + n2 - 1, 3) * keyed;
+  const u64 needed = std::max<u64>({(u64)n1 * n2 * B, n2 * keyed, n1 * n2 > 1 ? rotated : 0, scores ? keyed * (C + 1) / 2 : 0});
+  return (u32)std::min<u64>(needed, std::max<u32>(B, std::min(1024u, 128u << (c->logN < 16 ? 16 - c->logN : 0))));
+}
 
 // Tokens up to which the key switches of a state's update form the first two terms of the sums of products themselves. us, that way |
 // by the kernel of the products, 32 components at 2^16, 8 limbs, 1, 2, 4, 8 tokens: 1934 | 2012, 2665 | 2699, 4415 | 4363, 9338 | 8961;
@@ -201,10 +207,10 @@ struct LinAttn {
   char* ks;                // a key-switch workspace for `slice` ciphertexts
   size_t ks_bytes;
 
-  void shape(const ckks_ctx* c_, u32 C_, u32 B_, u32 nlimbs_, u32 n1_, u32 n2_) {
+  void shape(const ckks_ctx* c_, bool scores, u32 C_, u32 B_, u32 nlimbs_, u32 n1_, u32 n2_) {
     cc = c_, C = C_, B = B_, nlimbs = nlimbs_, n1 = n1_, n2 = n2_;
     pl = (u64)nlimbs * cc->N, ct = 2 * pl;
-    slice = linattn_slice(cc, B);
+    slice = linattn_slice(cc, scores, C, B, n1, n2);
     tokens = std::min<u32>(C, slice / B);
     whole = whole_limb(cc, C * B, nlimbs, false);
   }
@@ -530,7 +536,7 @@ int linattn_check(const ckks_ctx* c, u32 C, u32 B, u32 nlimbs, u32 n1, u32 n2) {
   if (rc) return rc;
   if (C == 0 || n1 == 0 || n2 == 0) return fail(CKKS_ESHAPE, "tokens, n1 and n2 must be positive");
   if (C > 4096 || n1 > 4096 || n2 > 4096 || (u64)C * B > 32767 || (u64)n1 * n2 * B > 32767 * 64ull || (u64)n2 * C * B > 65535 ||
-      (u64)linattn_slice(c, B) * std::max<u32>(2, c->dnum) > 65535)
+      (u64)B * std::max<u32>(2, c->dnum) > 65535)
     return fail(CKKS_ESHAPE, "too many ciphertexts for one call");
   return CKKS_OK;
 }
@@ -562,7 +568,7 @@ int linattn_run(bool chunk, ckks_ctx* c, const LinAttnCall& io, u32 C, u32 B, u3
   if (io.decay && (overlap(io.o_out, in_bytes, io.decay, ct_bytes / 2) || overlap(io.state_out, state_bytes, io.decay, ct_bytes / 2)))
     return fail(CKKS_EINVAL, "an output overlaps decay");
   LinAttn f;
-  f.shape(c, C, B, nlimbs, n1, n2);
+  f.shape(c, chunk, C, B, nlimbs, n1, n2);
   f.c = c;
   if (!ws || ((uintptr_t)ws & 255)) return fail(CKKS_EWORKSPACE, "workspace is null or not 256-byte aligned");
   const size_t need = f.carve((char*)ws, chunk);
@@ -665,8 +671,9 @@ size_t ckks_linattn_workspace_bytes(const ckks_ctx* c, int op, uint32_t tokens, 
     const int rc = linattn_check(c, tokens, B, nlimbs, n1, n2);
     if (rc) return rc;
     LinAttn f;
-    f.shape(c, tokens, B, nlimbs, n1, n2);
-    bytes = f.carve(nullptr, op == CKKS_OP_LINATTN_CHUNK);
+    const bool scores = op == CKKS_OP_LINATTN_CHUNK;
+    f.shape(c, scores, tokens, B, nlimbs, n1, n2);
+    bytes = f.carve(nullptr, scores);
     return CKKS_OK;
   });
   return bytes;

@@ -1,0 +1,76 @@
+"""What the host side of the attention calls asks for and refuses, and the launches it books, on a stand-in for the HIP runtime: no
+GPU, no kernel runs."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+from launch_trace import ROOT, _runtime
+
+CALLS = r"""
+import ctypes as C, json, sys
+from ckks_inputs.params import find_ntt_primes, find_psi
+logN, q_bits, nq, p_bits, np, dnum, jobs = json.loads(sys.argv[2])
+q = find_ntt_primes(q_bits, nq, logN)
+p = find_ntt_primes(p_bits, np, logN, exclude=set(q))
+lib = C.CDLL(sys.argv[1])
+lib.ckks_linattn_workspace_bytes.restype = C.c_size_t
+lib.ckks_last_error.restype = lib.ckks_prof_kind_name.restype = C.c_char_p
+array = lambda v: (C.c_uint64 * len(v))(*v)
+ctx = C.c_void_p()
+assert lib.ckks_ctx_create(C.byref(ctx), logN, array(q), nq, array(p), np, dnum, array([find_psi(m, logN) for m in q + p]), 0) == 0
+at = lambda k: C.c_void_p(k << 44)      # device addresses, which nothing reads here
+STEP, CHUNK = 9, 10
+def run(job):
+    what, C_, B, nl, n1, n2 = job[:6]
+    op = STEP if what == "step" else CHUNK
+    n = lib.ckks_linattn_workspace_bytes(ctx, op, C_, B, nl, n1, n2)
+    if what == "bytes" or not n:
+        return n
+    keys = lambda k, count: (C.c_void_p * max(1, count))(*[(k << 44) + (i << 36) for i in range(count)])
+    sizes = ([] if op == STEP else [C_]) + [B, nl, n1, n2, max(1, (1 << (logN - 1)) // (n1 * n2))]
+    call = lib.ckks_linattn_step if op == STEP else lib.ckks_linattn_chunk
+    lib.ckks_prof_enable(ctx, 1)
+    rc = call(ctx, *[at(k) for k in range(1, 6)], None, None, *sizes, at(7), keys(8, n1 - 1), keys(9, n2 - 1), keys(10, n2 - 1),
+              at(11), C.c_size_t(n), at(12))
+    if rc: sys.exit(lib.ckks_last_error().decode())
+    lib.ckks_prof_collect(ctx)
+    out = {}
+    for kind in range(lib.ckks_prof_num_kinds()):
+        ms, count = C.c_double(), C.c_uint64()
+        lib.ckks_prof_read(ctx, kind, C.byref(ms), C.byref(count))
+        if count.value: out[lib.ckks_prof_kind_name(kind).decode()] = count.value
+    lib.ckks_prof_reset(ctx)
+    return out
+print(json.dumps([run(job) for job in jobs]), file=sys.stderr)   # stdout has the launches
+"""
+
+
+def answers(shape, jobs):
+    """shape: logN, bits and number of the main primes, of the special primes, digits. Jobs (what, tokens, batch, limbs, n1, n2): "bytes"
+    is the workspace of a chunk, "step" and "chunk" the launches that the library's profile counts, by name (0: the shape is refused).
+    Also the launched kernels' names."""
+    import paper_2604_03425_amd as pkg
+    env = dict(os.environ, LD_LIBRARY_PATH=_runtime(), PYTHONPATH=ROOT)
+    res = subprocess.run([sys.executable, "-c", CALLS, pkg.library_path(), json.dumps(list(shape) + [jobs])], env=env,
+                         stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
+    assert res.returncode == 0, res.stderr
+    launches = [line.split() for line in res.stdout.splitlines()]
+    return json.loads(res.stderr.splitlines()[-1]), [words[2] for words in launches if words[0] == "launch"]
+
+
+@pytest.mark.parametrize("shape,nl", [((12, 45, 5, 60, 2, 3), 5), ((13, 50, 4, 60, 2, 2), 4), ((16, 50, 24, 60, 8, 3), 24)])
+@pytest.mark.parametrize("tokens,batch,n1,n2", [(1, 1, 2, 2), (1, 2, 2, 2), (2, 1, 2, 2), (1, 1, 4, 4), (1, 1, 1, 1)])
+def test_a_small_call_takes_a_small_workspace(shape, nl, tokens, batch, n1, n2):
+    """A call has max(n1 n2, (3 n1 + n2) tokens, tokens (tokens + 1) / 2) * batch ciphertexts at most to switch at a time. For each one
+    there are, in polynomials of one limb: digits beta * next, accumulators twice 2 * next, a product 3 nl, inputs, results and two
+    kinds of scores 4 * 2 nl, ModDown's 2 nl and a coefficient form nl; rotations that a call keeps are among those. Twice that is room
+    for the pieces' own rounding and for the terms from inside a chunk."""
+    (got,), _ = answers(shape, [("bytes", tokens, batch, nl, n1, n2)])
+    logN, _, nq, _, K, dnum = shape
+    alpha = -(-nq // dnum)
+    beta, ext = -(-nl // alpha), nl + K
+    cts = max(n1 * n2, (3 * n1 + n2) * tokens, tokens * (tokens + 1) // 2) * batch
+    assert 0 < got <= 2 * cts * (beta * ext + 4 * ext + 14 * nl) * (8 << logN)
