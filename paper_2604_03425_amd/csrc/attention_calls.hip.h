@@ -299,7 +299,7 @@ struct LinAttn {
     const u64 ext_ct = 2 * (u64)lt->next * c->N;
     GatherArgs g{{(const ulonglong2*)(with_q ? q : k), (const ulonglong2*)(with_q ? k : v), (const ulonglong2*)v}, (ulonglong2*)d, n * ct / 2};
     {
-      ProfScope ps(c, PK_ADD, st);
+      ProfScope ps(c, PK_GATHER, st);
       hipLaunchKernelGGL(gather_kernel, dim3((unsigned)((g.words + 255) / 256), with_q ? 3 : 2), dim3(256), 0, st, g);
       HIP_TRY(hipGetLastError());
     }

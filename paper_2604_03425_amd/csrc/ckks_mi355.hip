@@ -141,7 +141,7 @@ enum ProfKind {
   PK_FWD_ROWS, PK_FWD_BLOCKS = PK_FWD_ROWS + 3, PK_INV_BLOCKS = PK_FWD_BLOCKS + 3, PK_INV_ROWS = PK_INV_BLOCKS + 3,
   PK_FWD_FINAL = PK_INV_ROWS + 3,
   PK_AUTOMORPH = PK_FWD_FINAL + 3, PK_MODUP, PK_INNER, PK_INNER16, PK_INNER16_INT, PK_INNER_C, PK_INNER8, PK_INNER8_BIG, PK_BCONV_ROWS, PK_MODDOWN = PK_BCONV_ROWS + 3, PK_FINAL, PK_TENSOR, PK_PMACC, PK_PMACC_FP, PK_ADD,
-  PK_KS12_FRONT, PK_KS12_DIGITS, PK_KS12_SPECIAL, PK_KS12_FINAL, PK_CONV_ROWS, PK_COPY, PK_PMACC_STAGED, PK_PMACC_FP_STAGED, PK_ROT_SUM, PK_PROD_SUM, PK_COUNT
+  PK_KS12_FRONT, PK_KS12_DIGITS, PK_KS12_SPECIAL, PK_KS12_FINAL, PK_CONV_ROWS, PK_COPY, PK_PMACC_STAGED, PK_PMACC_FP_STAGED, PK_ROT_SUM, PK_PROD_SUM, PK_GATHER, PK_COUNT
 };
 static const char* const kProfNames[PK_COUNT] = {
     "ntt_fwd_pass", "ntt_inv_pass",
@@ -154,7 +154,7 @@ static const char* const kProfNames[PK_COUNT] = {
     "ntt16_bconv_rows_kernel<0>", "ntt16_bconv_rows_kernel<1>", "ntt16_bconv_rows_kernel<2>", "moddown_kernel", "ks_final_kernel", "tensor_kernel",
     "pmacc_int_kernel", "pmacc_fp_kernel", "addto_kernel",
     "ks12_front_kernel", "ks12_digits_kernel", "ks12_special_kernel", "ks12_final_kernel", "conv_rows_kernel", "copy",
-    "pmacc_int_staged_kernel", "pmacc_fp_staged_kernel", "rot_sum_kernel", "prod_sum_kernel"};
+    "pmacc_int_staged_kernel", "pmacc_fp_staged_kernel", "rot_sum_kernel", "prod_sum_kernel", "gather_kernel"};
 struct ProfRec {
   int kind;
   hipEvent_t start, stop;

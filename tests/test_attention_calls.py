@@ -74,3 +74,12 @@ def test_a_small_call_takes_a_small_workspace(shape, nl, tokens, batch, n1, n2):
     beta, ext = -(-nl // alpha), nl + K
     cts = max(n1 * n2, (3 * n1 + n2) * tokens, tokens * (tokens + 1) // 2) * batch
     assert 0 < got <= 2 * cts * (beta * ext + 4 * ext + 14 * nl) * (8 << logN)
+
+
+@pytest.mark.parametrize("shape", [(10, 50, 4, 60, 2, 2), (13, 50, 4, 60, 2, 2)])
+@pytest.mark.parametrize("what,tokens", [("step", 1), ("chunk", 2)])
+def test_the_profile_names_the_kernels_that_ran(shape, what, tokens):
+    (counts,), launched = answers(shape, [(what, tokens, 2, 4, 2, 2)])
+    for name in ("gather_kernel", "addto_kernel", "rot_sum_kernel", "prod_sum_kernel"):
+        assert counts.get(name, 0) == sum(name in k for k in launched), name
+    assert counts["gather_kernel"] == 1
