@@ -337,7 +337,9 @@ int ckks_rope(ckks_ctx* ctx, uint64_t* ct_out, const uint64_t* ct_in, uint32_t B
  *   sum1(x) = ModDown(P x + sum_{b=1..n1-1} (A(sigma_b(c1); evk_baby[b-1]) + (P sigma_b(c0), 0))) and sum2 the same over the giant
  *   steps: the scores of a lane end up in all of its slots.
  * Without a state (state_in NULL: the start of a sequence) S is zero; read(q, 0, e) = Relin(e). state_out may be state_in.
- * Scales: the state has the square of the inputs' scale, o its cube (times decay's for the state, where given); no rescale.
+ * Scales: the state has the square of the inputs' scale, o its cube (times decay's for the state, where given); no rescale. state_in is
+ * added to products of k and v, so it must have their scale: a state_out that took a decay is rescaled before it is a state_in again,
+ * and the next call has a limb less.
  *   evk_mult    device, the relinearisation key; evk_baby, evk_giant as for ckks_pcmm_bsgs
  *   evk_value   host array of n2-1 device pointers; evk_value[g-1] switches 5^(-g*n1*stride). Where n1*n2*stride = N/2 that is the
  *               key of the giant step n2 - g.
