@@ -313,7 +313,7 @@ int ckks_add(ckks_ctx* ctx, uint64_t* out, const uint64_t* a, const uint64_t* b,
  *                limbs of every w_0 are not read); ciphertext b of the batch uses set b / (B / npt), npt divides B
  *   galois_elts, evks   host arrays of R entries (R = 0: a plain product with w_0)
  * ct_in, ct_out: device [B][2][nlimbs][N]; ct_out may overlap neither ct_in nor pt_ext. Output scale = input scale times the
- * weights' (no rescale). Workspace: CKKS_OP_ROPE.
+ * weights' (no rescale). Workspace: CKKS_OP_ROPE. With digits = ceil(nlimbs / alpha), Limits: B <= 32767; B * max(2, digits) <= 65535.
  */
 int ckks_rope(ckks_ctx* ctx, uint64_t* ct_out, const uint64_t* ct_in, uint32_t B, uint32_t nlimbs, const uint64_t* pt_ext,
               uint32_t npt, const uint32_t* galois_elts, const uint64_t* const* evks, uint32_t R, void* ws, size_t ws_bytes,
@@ -321,12 +321,15 @@ int ckks_rope(ckks_ctx* ctx, uint64_t* ct_out, const uint64_t* ct_in, uint32_t B
 
 /*
  * Linear attention with a decay for each head: o_t = q_t^T S_t, S_t = decay S_{t-1} + k_t v_t^T, for lanes of d = n1 * n2
- * components (n1 * n2 * stride = N/2 slots makes every rotation cyclic within a lane, which is what the formulas below need to be
- * this sum). The state is held as its d diagonals,
+ * components. The formulas below are this sum where every rotation is cyclic within a lane: n1 * n2 * stride = N/2 slots, or a divisor
+ * of it with all vectors repeated over the slots. That takes a d which is a power of two (smaller heads are filled up with zeros);
+ * any other n1, n2 and stride are not refused, but the formulas then mix lanes. The state is held as its d diagonals,
  *   state[g][b] (slot i * stride + lane) = S[i + b][i - g n1],      device [n2][n1][B][2][nlimbs][N].
  * Decays within a call are folded into q and k, which carry decay^(t+1) and decay^(-t-1) at token t = 0.. of the call (the weights
  * of ckks_rope do that at no cost); `decay` (device [nlimbs][N], evaluation domain, or NULL for none) holds decay^tokens for every
- * lane. With K[b] = HRot_{b stride}(k), Q[b] likewise, V[g] = HRot_{-g n1 stride}(v), and * a product in three components:
+ * lane. A query's error at token t grows by the keys' decay^(-t-1): the tokens of a call have to be few enough for the smallest decay
+ * (decay 0.7 and 16 tokens cost 8 bits, 64 tokens 33).
+ * With K[b] = HRot_{b stride}(k), Q[b] likewise, V[g] = HRot_{-g n1 stride}(v), and * a product in three components:
  *   read(q, S, e) = ModDown( A(d2; evk_mult) + (P d0, P d1) + sum_{g>=1} ( A(sigma_g(y_g.c1); evk_giant[g-1]) + (P sigma_g(y_g.c0), 0) ) ),
  *     d = e + sum_b Q[b] * S[0][b],  y_g = Relin(sum_b Q[b] * S[g][b]),  sigma_g of the rotation by g * n1 * stride.
  * ckks_linattn_step, a token for each of B ciphertexts of lanes (the recurrent form):
@@ -344,7 +347,8 @@ int ckks_rope(ckks_ctx* ctx, uint64_t* ct_out, const uint64_t* ct_in, uint32_t B
  *   evk_value   host array of n2-1 device pointers; evk_value[g-1] switches 5^(-g*n1*stride). Where n1*n2*stride = N/2 that is the
  *               key of the giant step n2 - g.
  * No output may overlap an input, but for state_out = state_in. Workspace: ckks_linattn_workspace_bytes (0 on a bad argument);
- * tokens = 1 for a step. Limits: tokens, n1, n2 <= 4096, tokens * B <= 32767, n2 * tokens * B <= 65535.
+ * tokens = 1 for a step. Limits: tokens, n1, n2 <= 4096; tokens * B <= 32767; n2 * tokens * B <= 65535; n1 * n2 * B <= 2097088;
+ * B * max(2, dnum) <= 65535.
  */
 size_t ckks_linattn_workspace_bytes(const ckks_ctx* ctx, int op, uint32_t tokens, uint32_t B, uint32_t nlimbs, uint32_t n1,
                                     uint32_t n2);

@@ -2,9 +2,12 @@
 GPU, no kernel runs."""
 import json
 import os
+import random
+import re
 import subprocess
 import sys
 
+import numpy as np
 import pytest
 
 from launch_trace import ROOT, _runtime
@@ -16,7 +19,7 @@ logN, q_bits, nq, p_bits, np, dnum, jobs = json.loads(sys.argv[2])
 q = find_ntt_primes(q_bits, nq, logN)
 p = find_ntt_primes(p_bits, np, logN, exclude=set(q))
 lib = C.CDLL(sys.argv[1])
-lib.ckks_linattn_workspace_bytes.restype = C.c_size_t
+lib.ckks_linattn_workspace_bytes.restype = lib.ckks_workspace_bytes.restype = C.c_size_t
 lib.ckks_last_error.restype = lib.ckks_prof_kind_name.restype = C.c_char_p
 array = lambda v: (C.c_uint64 * len(v))(*v)
 ctx = C.c_void_p()
@@ -26,6 +29,9 @@ STEP, CHUNK = 9, 10
 def run(job):
     what, C_, B, nl, n1, n2 = job[:6]
     op = STEP if what == "step" else CHUNK
+    if what == "rope":
+        n = lib.ckks_workspace_bytes(ctx, 8, B, nl, 0)
+        return lib.ckks_rope(ctx, at(1), at(2), B, nl, at(3), 1, (C.c_uint32 * 1)(5), (C.c_void_p * 1)(4 << 44), 1, at(5), C.c_size_t(n), at(6))
     n = lib.ckks_linattn_workspace_bytes(ctx, op, C_, B, nl, n1, n2)
     if what == "bytes" or not n:
         return n
@@ -50,8 +56,8 @@ print(json.dumps([run(job) for job in jobs]), file=sys.stderr)   # stdout has th
 
 def answers(shape, jobs):
     """shape: logN, bits and number of the main primes, of the special primes, digits. Jobs (what, tokens, batch, limbs, n1, n2): "bytes"
-    is the workspace of a chunk, "step" and "chunk" the launches that the library's profile counts, by name (0: the shape is refused).
-    Also the launched kernels' names."""
+    is the workspace of a chunk, "step" and "chunk" the launches that the library's profile counts, by name (0: the shape is refused),
+    "rope" the code that one rotation returns. Also the launched kernels' names."""
     import paper_2604_03425_amd as pkg
     env = dict(os.environ, LD_LIBRARY_PATH=_runtime(), PYTHONPATH=ROOT)
     res = subprocess.run([sys.executable, "-c", CALLS, pkg.library_path(), json.dumps(list(shape) + [jobs])], env=env,
@@ -85,3 +91,69 @@ def test_the_profile_names_the_kernels_that_ran(shape, what, tokens):
     assert counts["gather_kernel"] == 1
     # (a relinearisation in steps starts from a copy of its first two components, which the profile counts among the additions)
     assert counts.get("addto_kernel", 0) == sum("addto_kernel" in k or "first_two_components_kernel" in k for k in launched)
+
+
+def _limits(call):
+    """The limits that the header states for a call, as Python expressions."""
+    text = open(os.path.join(ROOT, "include", "ckks_mi355.h")).read()
+    text = text[re.search(r"\* %s[:,] " % call, text).start():]
+    text = re.sub(r"\n \* *", " ", text[text.index("Limits: "):text.index("*/")])
+    return re.search(r"Limits: ([^.]*)\.", text).group(1).split("; ")
+
+
+def _within(limits, **names):
+    for limit in limits:
+        lefts, right = limit.split(" <= ")
+        for left in re.split(r", (?![^(]*\))", lefts):
+            if eval(left, dict(names, max=max)) > int(right):
+                return False
+    return True
+
+
+@pytest.mark.parametrize("dnum", [1, 3, 5])
+def test_the_header_states_the_limits_of_linear_attention(dnum):
+    """Shapes on both sides of every limit: a workspace is asked for where the header allows the call, nowhere else."""
+    limits, rng = _limits("ckks_linattn_step"), random.Random(dnum)
+    shapes = [(1, b, 5, n1, n2) for n1 in (1, 2) for n2 in (1, 2) for b in (65535 // max(2, dnum), 65535 // max(2, dnum) + 1, 32767, 32768)]
+    shapes += [(1, 511, 5, 64, 64), (1, 512, 5, 64, 64), (4096, 1, 5, 1, 1), (4097, 1, 5, 1, 1), (1, 1, 5, 4096, 1), (1, 1, 5, 4097, 1),
+               (1, 1, 5, 1, 4096), (1, 1, 5, 1, 4097), (4095, 8, 5, 2, 2), (4096, 8, 5, 2, 2), (3, 4369, 5, 1, 5), (3, 4370, 5, 1, 5)]
+    for _ in range(200):
+        at = lambda most: min(most, int(2 ** rng.uniform(0, most.bit_length())))   # noqa: E731
+        shapes.append((max(1, at(8192)), max(1, at(40000)), 5, max(1, at(5000)), max(1, at(5000))))
+    got, _ = answers((10, 50, 5, 60, 5, dnum), [("bytes",) + s for s in shapes])
+    want = [_within(limits, tokens=t, B=b, n1=n1, n2=n2, dnum=dnum) for t, b, _, n1, n2 in shapes]
+    assert [bool(n) for n in got] == want and 20 < sum(want) < len(want) - 20
+
+
+@pytest.mark.parametrize("dnum", [1, 3, 5])
+def test_the_header_states_the_limits_of_rotary_positions(dnum):
+    limits, nl = _limits("ckks_rope"), 5
+    digits = -(-nl // -(-5 // dnum))
+    batches = [1, 65535 // max(2, digits), 65535 // max(2, digits) + 1, 32767, 32768]
+    got, _ = answers((10, 50, 5, 60, 5, dnum), [("rope", 1, b, nl, 1, 1) for b in batches])
+    assert [rc == 0 for rc in got] == [_within(limits, B=b, digits=digits) for b in batches]
+    assert set(got) == {0, -2}
+
+
+@pytest.mark.parametrize("n1,n2,stride,valid", [(2, 4, 8, True), (4, 2, 8, True), (1, 8, 8, True), (2, 4, 2, True), (4, 4, 1, True),
+                                                (3, 2, 8, False), (2, 2, 24, False), (5, 1, 12, False)])
+def test_the_slot_formulas_are_attention_where_the_header_says_so(n1, n2, stride, valid):
+    """One lane set of S = 64 slots, rotations as they are: K[b] V[g] are diagonals of k v^T, the read's sum is q^T S, and sum1 and sum2 give
+    a lane's score in all of its slots, where n1 n2 stride divides S and the vectors repeat."""
+    S, d = 64, n1 * n2
+    rng = np.random.default_rng(d)
+    assert valid == (S % (d * stride) == 0)
+    q, k, v = rng.integers(-9, 10, (3, d, stride))
+    spread = lambda x: np.resize(x.reshape(-1), S)       # component i of lane l in slot i * stride + l, again and again   # noqa: E731
+    rot = lambda x, r: np.roll(x, -r)                    # noqa: E731
+    Q, K = ([rot(spread(x), b * stride) for b in range(n1)] for x in (q, k))
+    V = [rot(spread(v), -g * n1 * stride) for g in range(n2)]
+    state = [[K[b] * V[g] for b in range(n1)] for g in range(n2)]
+    o = sum(rot(sum(Q[b] * state[g][b] for b in range(n1)), g * n1 * stride) for g in range(n2))
+    want = spread((q * k).sum(axis=0) * v)
+    assert (o == want).all() == valid
+    p = spread(q) * spread(k)
+    p = sum(rot(p, b * stride) for b in range(n1))
+    p = sum(rot(p, g * n1 * stride) for g in range(n2))
+    if valid:
+        assert (p * spread(v) == want).all()
