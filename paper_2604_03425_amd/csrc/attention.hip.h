@@ -148,9 +148,11 @@ __device__ __forceinline__ void rot_sum_fp(const RotSumArgs& a, u32 what, u32 bl
   }
 }
 
-// All other moduli: residues in ext, Montgomery products, sums below 2m. PLAIN: acc without the factor 2^-64. Grid and lanes as above. The 5
-// special limbs of the rotations above take 130 us, nearly three times a double-precision limb: 18 Montgomery products of 12
-// multiplies a position and rotation bound it, not memory; in 128-bit sums with a reduction each 163.
+// All other moduli: residues in ext, Montgomery products, sums below 2m. PLAIN: acc without the factor 2^-64. Grid and lanes as above. A
+// position, ciphertext and rotation with 4 digits takes 11 Montgomery products on a special limb (8 with keys, 2 with the weight, 1 that
+// prepares it) and 12 on a main one, 10 multiplies each. They cost little on top of the gathers that double-precision limbs wait for: the
+// rotations above with 25 limbs of this kind 620 us, with 25 doubles 570, with 20 doubles and 5 special limbs of this kind 575. In
+// 128-bit sums with a reduction each the 5 special limbs alone took 163, this way 130.
 template <int CB, bool PLAIN>
 __device__ __forceinline__ void rot_sum_int(const RotSumArgs& a, u32 what, u32 blk, u32 zi) {
   const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, comp = (size_t)a.nm * N;

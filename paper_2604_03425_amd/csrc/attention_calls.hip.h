@@ -646,8 +646,8 @@ int ckks_rope(ckks_ctx* c, uint64_t* ct_out, const uint64_t* ct_in, uint32_t B, 
     if (R == 1 && two_pass(c) && c->tune[3] != 1) {
       // One rotation: the weights join the fused kernels of a key switch, whose digits never reach memory in the evaluation domain. us,
       // that way | through sums of rotations: 24 limbs at 2^16, 1, 4, 16, 64 ciphertexts 147 | 185, 367 | 462, 1287 | 1596, 5105 |
-      // 6416; 5 limbs at 2^13, 1, 8, 64: 52 | 55, 63 | 72, 140 | 194; 8 60-bit limbs at 2^15, 1, 8: 76 | 74, 165 | 186. Two rotations would
-      // convert the digits twice.
+      // 6416; 5 limbs at 2^13, 1, 8, 64: 52 | 55, 63 | 72, 140 | 194; 8 60-bit limbs at 2^15, 1, 8: 76 | 74, 165 | 186. They hold
+      // one rotation's digits and sums; two rotations go through the sums of rotations, the only form there is for them.
       const u64 pl = (u64)nlimbs * c->N;
       KsIo io{in + pl, 2 * pl, galois_elts[0], (u64*)ct_out, {0, 0}, in, galois_elts[0]};
       io.more = KS_WEIGHTED;

@@ -15,11 +15,12 @@ import numpy as np
 
 def rope_frequencies(rot_dim, base=10000.0, scaling=None):
     """(frequencies of the rot_dim / 2 pairs, factor of the turned components). scaling: None, or a dict of
-        kind "linear":   positions divided by `factor`;
-        kind "base":     the base raised so that the slowest pair turns `factor` times slower and the fastest stays as it is;
+        kind "linear":   positions divided by `factor` (position interpolation, arXiv 2306.15595);
+        kind "base":     the base raised so that the slowest pair turns `factor` times slower and the fastest stays as it is (arXiv
+                         2309.00071, Sec. 3);
         kind "by_parts": pairs that turn more than `fast` times over `original` positions stay, those that turn less than `slow` times
                          are slowed by `factor`, the ones between are mixed linearly in the number of turns' index; the turned
-                         components grow by 0.1 ln(factor) + 1."""
+                         components grow by 0.1 ln(factor) + 1 (the same paper's rule by parts)."""
     if rot_dim < 2 or rot_dim % 2:
         raise ValueError("rot_dim must be even and positive")
     i = np.arange(rot_dim // 2)
