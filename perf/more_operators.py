@@ -591,7 +591,7 @@ def prepare(case, seed):
     pairs = sum(len(seen) for _, seen in s["visible"])
     s.update(out=torch.empty((len(s["visible"]), 2, nl - 1 - s["squarings"], N), dtype=torch.int64, device=DEVICE),
              k_pages=[s["k_cache"][i] for i in pages], v_pages=[s["v_cache"][i] for i in pages],
-             ws=ctx.attn_workspace(len(s["visible"]), pairs, len(pages), nl, s["n1"], s["n2"], s["squarings"]))
+             ws=ctx.attn_workspace(len(s["visible"]), pairs, nl, s["n1"], s["n2"], s["squarings"]))
     return s
 
 
