@@ -363,6 +363,63 @@ int ckks_linattn_chunk(ckks_ctx* ctx, uint64_t* o_out, uint64_t* state_out, cons
                        void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Attention over a paged cache of ciphertexts, and a root-mean-square norm (extensions, like the calls above; layout of lanes as there,
+ * d = n1 * n2 components). ModDown' divides by P q_{nlimbs-1} at once: the last limb joins the special ones as a source of one centred
+ * conversion to the others, so that the result has a limb less and a product's scale is back at its factors'. It is Rescale(ModDown(.)) up
+ * to the rounding (one of them instead of two). With A and P as above,
+ *   Relin'(d) = ModDown'(A(d2; evk_mult) + (P d0, P d1));
+ *   slotsum'(d) = sum2(sum1(Relin(d))), the sum over a lane's components in all of its slots: sum1 and sum2 as for ckks_linattn_chunk
+ *   (sum1 if n1 > 1, sum2 if n2 > 1), the last of the steps there are with ModDown' in the place of ModDown.
+ *
+ * The cache. Sequence b of `seqs` (a ciphertext of lanes, i.e. a batch of heads or users that move in step) has lens[b] tokens, the
+ * last new_lens[b] of which are new; its tokens lie in ceil(lens[b] / page_tokens) pages, whose pointers follow one another in k_pages
+ * and v_pages, sequence after sequence. A page is device [page_tokens][2][k_limbs][N], or v_limbs: values need fewer limbs than keys. Pages
+ * may belong to several sequences (a common prefix) as long as nobody appends to the same place twice. new_lens, lens and the page
+ * arrays are host arrays. Rows (of q, o_out, k, v) are the new tokens, sequence after sequence; a sequence may have none.
+ *
+ * ckks_kv_append copies the first k_limbs and v_limbs limbs of the new tokens' keys and values, device [rows][2][in_limbs][N], into
+ * their places. Nothing else in the pages is written; pages without new tokens may be null.
+ *
+ * ckks_attn_paged: the query at position t of its sequence sees the tokens s <= t with t - s < window (window = 0: all) or s < sinks:
+ *   u_ts = slotsum'(q_t * k_s) + bias;   squarings times u_ts = Relin'(u_ts * u_ts);   o_t = Relin(sum_s u_ts * v_s),
+ * a score function (x + bias)^(2^squarings) of the scores x (for squarings = 0 the scores and a constant). With bias = 2^squarings at the
+ * scores' scale it is 2^(squarings 2^squarings) times the approximation (1 + x / 2^squarings)^(2^squarings) of exp(x). There is no
+ * division by the sum of the weights: ckks_rmsnorm after it makes the result independent of their scale.
+ *   q       device [rows][2][nlimbs][N];   o_out device [rows][2][nlimbs - 1 - squarings][N], at the product of u's and v's scale
+ *   bias    added to every slot as an integer
+ * k_limbs >= nlimbs and v_limbs >= nlimbs - 1 - squarings >= 1; pages that no new token sees may be null. o_out may overlap neither q nor
+ * a page that is read. Keys as for ckks_linattn_chunk. Workspace: ckks_attn_workspace_bytes for the number of rows and of (query, token) pairs that see
+ * each other, or more of both; beyond a bound that fills the chip it does not grow with the pairs. Rows <= 32767. No rows: nothing is done.
+ *
+ * ckks_rmsnorm: with h = ct_x + ct_res (ct_res NULL: ct_x; the sum is written to h_out if that is given),
+ *   m = slotsum'(square h * h) + eps;   y = start - m;
+ *   iterations times, k = 0..: u = Relin'(m * y), w = Relin'(y * y), y = Relin'(factors[k] y - u * w);
+ *   ct_out = Relin(g * y),   g = h, or Rescale(gain (.) h) of h's first L + 1 limbs;   L = nlimbs - 1 - 2 iterations limbs.
+ * These are Newton's steps y (3 - m y^2) / 2 for 1 / sqrt(m) from y = start - m; eps, start and the factors are integers that every slot
+ * gets and that hold the scales (paper_2604_03425_amd.rmsnorm_plan makes them).
+ *   ct_x, ct_res, h_out   device [B][2][nlimbs][N];   gain device [L + 1][N] or NULL, evaluation domain;   ct_out device [B][2][L][N]
+ *   factors               host array of `iterations` integers
+ * ct_out may overlap no input; h_out may be ct_x or ct_res. No rescale at the end. Workspace: ckks_rmsnorm_workspace_bytes. B <= 32767.
+ *
+ * Both need special primes and n1, n2 <= 4096; workspace sizes are 0 on a bad argument.
+ */
+int ckks_kv_append(ckks_ctx* ctx, const uint64_t* k, const uint64_t* v, uint32_t in_limbs, uint32_t seqs, const uint32_t* new_lens,
+                   const uint32_t* lens, uint64_t* const* k_pages, uint64_t* const* v_pages, uint32_t page_tokens, uint32_t k_limbs,
+                   uint32_t v_limbs, void* stream);
+size_t ckks_attn_workspace_bytes(const ckks_ctx* ctx, uint32_t rows, uint64_t pairs, uint32_t nlimbs, uint32_t n1, uint32_t n2,
+                                 uint32_t squarings);
+int ckks_attn_paged(ckks_ctx* ctx, uint64_t* o_out, const uint64_t* q, uint32_t nlimbs, uint32_t seqs, const uint32_t* new_lens,
+                    const uint32_t* lens, const uint64_t* const* k_pages, const uint64_t* const* v_pages, uint32_t page_tokens,
+                    uint32_t k_limbs, uint32_t v_limbs, uint32_t window, uint32_t sinks, int64_t bias, uint32_t squarings, uint32_t n1,
+                    uint32_t n2, uint32_t stride, const uint64_t* evk_mult, const uint64_t* const* evk_baby,
+                    const uint64_t* const* evk_giant, void* ws, size_t ws_bytes, void* stream);
+size_t ckks_rmsnorm_workspace_bytes(const ckks_ctx* ctx, uint32_t B, uint32_t nlimbs, uint32_t n1, uint32_t n2, uint32_t iterations);
+int ckks_rmsnorm(ckks_ctx* ctx, uint64_t* ct_out, uint64_t* h_out, const uint64_t* ct_x, const uint64_t* ct_res, const uint64_t* gain,
+                 int64_t square, int64_t eps, int64_t start, const int64_t* factors, uint32_t iterations, uint32_t B, uint32_t nlimbs,
+                 uint32_t n1, uint32_t n2, uint32_t stride, const uint64_t* evk_mult, const uint64_t* const* evk_baby,
+                 const uint64_t* const* evk_giant, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Measurement support (not part of the paper's operator set). While enabled, every kernel
  * launch the library makes is bracketed by two HIP events on the stream it is launched on;
  * ckks_prof_collect() waits for the recorded events and adds their elapsed times to

@@ -248,6 +248,25 @@ class RefContext:
                                        C.c_uint32(nl)))
         return out
 
+    def switch_sum(self, base, evk=None, y=None, galois_elts=(), evks=(), more=False):
+        """ModDown of P base plus, with evk, the key switch of base's third component plus the rotations of y; base
+        [B][2 or 3][nl][N]. more: division by P q_{nl-1}, the result a limb lower."""
+        base, bp = _u64(base)
+        B, comps, nl, _ = base.shape
+        G = len(galois_elts)
+        assert comps == (2 if evk is None else 3) and len(evks) == G and (not G or y.shape == (B, 2, nl, self.N))
+        ep = None
+        if evk is not None:
+            evk, ep = _u64(evk)
+        y, yp = _u64(y if G else np.zeros(1, dtype=np.uint64))
+        keep = [_u64(k) for k in evks]
+        keys = (u64p * max(1, G))(*[k[1] for k in keep])
+        gs = (C.c_uint32 * max(1, G))(*[int(g) for g in galois_elts])
+        out = np.empty((B, 2, nl - (1 if more else 0), self.N), dtype=np.uint64)
+        _check(lib().ref_switch_sum(self._h, out.ctypes.data_as(u64p), bp, ep, yp, C.c_uint32(G), gs, keys, C.c_uint32(B),
+                                    C.c_uint32(nl), C.c_int(1 if more else 0)))
+        return out
+
     def tensor_acc(self, ct_a, ct_b, d_acc=None):
         """Un-relinearised product [B][3][nl][N], added to d_acc when given (late relinearisation, Sec. 5.2)."""
         ct_a, ap = _u64(ct_a)

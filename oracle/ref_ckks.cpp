@@ -328,14 +328,16 @@ std::vector<u64> keyswitch_accumulate(const RefCtx* c, const u64* d, int nlimbs,
 
 // Second half: ModDown of both accumulators (evaluation domain, [2][nlimbs + K][N], overwritten):
 // x_c = INTT(x); t = BConv_{P->Q_l}(x_c|P); ks_i = NTT((x_c,i - t_i) * P^-1). Writes ks (2 x nlimbs x N).
-void moddown_pair(const RefCtx* c, u64* ks, std::vector<u64>& acc, int nlimbs) {
+// more: division by P q_{nlimbs-1} instead, that limb being one more source of the conversion; writes ks (2 x (nlimbs - 1) x N).
+void moddown_pair(const RefCtx* c, u64* ks, std::vector<u64>& acc, int nlimbs, bool more = false) {
   const size_t N = c->N;
-  const int K = c->np, next = nlimbs + K;
+  const int next = nlimbs + c->np, K = c->np + (more ? 1 : 0);
   std::vector<int> ext_id(next);
   for (int t = 0; t < nlimbs; t++) ext_id[t] = t;
-  for (int k = 0; k < K; k++) ext_id[nlimbs + k] = c->nq + k;
+  for (int k = 0; k < c->np; k++) ext_id[nlimbs + k] = c->nq + k;
+  if (more) nlimbs--;   // what is kept; the sources follow it
   std::vector<u64> psrc, qdst;
-  for (int k = 0; k < K; k++) psrc.push_back(c->mod[c->nq + k]);
+  for (int k = 0; k < K; k++) psrc.push_back(c->mod[ext_id[nlimbs + k]]);
   for (int i = 0; i < nlimbs; i++) qdst.push_back(c->mod[i]);
   BConvPlan down = make_bconv(psrc, qdst);
   for (int comp = 0; comp < 2; comp++) {
@@ -350,7 +352,7 @@ void moddown_pair(const RefCtx* c, u64* ks, std::vector<u64>& acc, int nlimbs) {
     for (int i = 0; i < nlimbs; i++) {
       u64 m = c->mod[i];
       u64 pinv = 1;
-      for (int k = 0; k < K; k++) pinv = mulm(pinv, c->mod[c->nq + k] % m, m);
+      for (int k = 0; k < K; k++) pinv = mulm(pinv, psrc[k] % m, m);
       pinv = invm(pinv, m);
       u64* o = ks + ((size_t)comp * nlimbs + i) * N;
       for (size_t n = 0; n < N; n++) o[n] = mulm(subm(x[(size_t)i * N + n], tq[(size_t)i * N + n], m), pinv, m);
@@ -851,6 +853,46 @@ int ref_relin_rotated(const RefCtx* c, u64* ct_out, const u64* d, const u64* evk
       add_main(0, r0.data());
     }
     moddown_pair(c, ct_out + bi * 2 * pl, T, nlimbs);
+  });
+  return 0;
+}
+
+// out = ModDown( (P b0, P b1) + [evk != null] A(b2; evk) + sum_g rot_g(y) ), rot_g(y) = A(sigma_g(y1); evks[g]) + (P sigma_g(y0), 0):
+// base [B][2 or 3][nlimbs][N] (three components with evk), y [B][2][nlimbs][N]. more: ModDown by P q_{nlimbs-1}, out with a limb less.
+int ref_switch_sum(const RefCtx* c, u64* out, const u64* base, const u64* evk, const u64* y, uint32_t G, const uint32_t* galois,
+                   const u64* const* evks, uint32_t B, uint32_t nlimbs, int more) {
+  if (nlimbs < (more ? 2u : 1u) || nlimbs > (uint32_t)c->nq) return fail("bad limb count");
+  const size_t N = c->N, pl = (size_t)nlimbs * N;
+  const int next = (int)nlimbs + c->np;
+  const size_t el = (size_t)next * N, comps = evk ? 3 : 2;
+  auto ext_mod = [&](int t) { return c->mod[t < (int)nlimbs ? t : c->nq + (t - (int)nlimbs)]; };
+  parallel_for(B, [&](size_t bi) {
+    std::vector<u64> T(2 * el, 0), r0(pl), r1(pl);
+    auto add = [&](const std::vector<u64>& A) {
+      for (size_t k = 0; k < 2 * el; k++) T[k] = addm(T[k], A[k], ext_mod((int)(k % el / N)));
+    };
+    auto add_main = [&](int comp, const u64* x) {
+      for (size_t k = 0; k < pl; k++) {
+        const u64 m = c->mod[k / N];
+        u64 v = x[k];
+        for (int i = 0; i < c->np; i++) v = mulm(v, c->mod[c->nq + i] % m, m);
+        T[comp * el + k] = addm(T[comp * el + k], v, m);
+      }
+    };
+    const u64* b = base + bi * comps * pl;
+    if (evk) add(keyswitch_accumulate(c, b + 2 * pl, nlimbs, evk));
+    add_main(0, b);
+    add_main(1, b + pl);
+    for (uint32_t g = 0; g < G; g++) {
+      const u64* x = y + bi * 2 * pl;
+      for (uint32_t i = 0; i < nlimbs; i++) {
+        automorph_eval(c, &r0[(size_t)i * N], x + (size_t)i * N, i, galois[g]);
+        automorph_eval(c, &r1[(size_t)i * N], x + pl + (size_t)i * N, i, galois[g]);
+      }
+      add(keyswitch_accumulate(c, r1.data(), nlimbs, evks[g]));
+      add_main(0, r0.data());
+    }
+    moddown_pair(c, out + bi * 2 * (nlimbs - (more ? 1 : 0)) * N, T, nlimbs, more != 0);
   });
   return 0;
 }

@@ -8,5 +8,6 @@ from .binding import (Context, CkksError, ckks_ntt, ckks_intt, ckks_automorph, c
                       ckks_noalloc_scratch_bytes, ckks_tensor_acc, ckks_relin, ckks_pcmm_bsgs_hoisted, ckks_pcmm_bsgs_double_hoisted, ckks_rescale, ckks_pmult, ckks_add, ckks_workspace_bytes, ckks_prof_enable, ckks_tune_set, ckks_prof_reset, ckks_prof_collect, ckks_prof_copy, library_path, exported_symbols,
                       OP_KEYSWITCH, OP_HROT, OP_HMULT_RELIN, OP_PCMM_BSGS, OP_RESCALE, OP_PCMM_BSGS_DH, OP_HROT_SUM, OP_ROPE, OP_LINATTN_STEP,
                       OP_LINATTN_CHUNK, ckks_rope, ckks_linattn_step, ckks_linattn_chunk,
-                      ckks_linattn_workspace_bytes)
+                      ckks_linattn_workspace_bytes, attn_pairs, ckks_kv_append, ckks_attn_workspace_bytes, ckks_attn_paged,
+                      ckks_rmsnorm_workspace_bytes, ckks_rmsnorm)
 from .rope import rope_frequencies, rope_tables

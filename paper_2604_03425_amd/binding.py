@@ -21,7 +21,8 @@ _SYMBOLS = ["ckks_last_error", "ckks_ctx_create", "ckks_ctx_destroy", "ckks_work
             "ckks_hrot_hoisted", "ckks_pcmm_bsgs_hoisted", "ckks_hrot_multi", "ckks_hrot_add", "ckks_tensor_acc",
             "ckks_relin", "ckks_pcmm_bsgs_double_hoisted", "ckks_hrot_sum", "ckks_hrot_noalloc",
             "ckks_noalloc_scratch_bytes", "ckks_rope", "ckks_linattn_workspace_bytes", "ckks_linattn_step",
-            "ckks_linattn_chunk"]
+            "ckks_linattn_chunk", "ckks_kv_append", "ckks_attn_workspace_bytes", "ckks_attn_paged",
+            "ckks_rmsnorm_workspace_bytes", "ckks_rmsnorm"]
 
 
 class CkksError(RuntimeError):
@@ -82,6 +83,15 @@ def _load():
     tail = [u64p, keys, keys, keys, vp, C.c_size_t, vp]
     lib.ckks_linattn_step.argtypes = [vp] + [u64p] * 7 + [C.c_uint32] * 5 + tail
     lib.ckks_linattn_chunk.argtypes = [vp] + [u64p] * 7 + [C.c_uint32] * 6 + tail
+    lib.ckks_kv_append.argtypes = [vp, u64p, u64p, C.c_uint32, C.c_uint32, u32p, u32p, keys, keys] + [C.c_uint32] * 3 + [vp]
+    lib.ckks_attn_workspace_bytes.restype = C.c_size_t
+    lib.ckks_attn_workspace_bytes.argtypes = [vp, C.c_uint32, C.c_uint64] + [C.c_uint32] * 4
+    key_tail = [u64p, keys, keys, vp, C.c_size_t, vp]
+    lib.ckks_attn_paged.argtypes = [vp, u64p, u64p, C.c_uint32, C.c_uint32, u32p, u32p, keys, keys] + [C.c_uint32] * 5 \
+        + [C.c_int64] + [C.c_uint32] * 4 + key_tail
+    lib.ckks_rmsnorm_workspace_bytes.restype = C.c_size_t
+    lib.ckks_rmsnorm_workspace_bytes.argtypes = [vp] + [C.c_uint32] * 5
+    lib.ckks_rmsnorm.argtypes = [vp] + [u64p] * 5 + [C.c_int64] * 3 + [C.POINTER(C.c_int64)] + [C.c_uint32] * 6 + key_tail
     lib.ckks_prof_enable.argtypes = [vp, C.c_int]
     lib.ckks_prof_copy.argtypes = [vp, vp, vp, C.c_size_t, vp]
     lib.ckks_tune_set.argtypes = [vp, C.c_int, C.c_int]
@@ -161,6 +171,18 @@ class Context:
 
     def linattn_workspace(self, op, tokens, batch, nlimbs, n1, n2):
         n = ckks_linattn_workspace_bytes(self, op, tokens, batch, nlimbs, n1, n2)
+        if n == 0:
+            raise CkksError(-2, "bad shape for workspace query")
+        return torch.empty(n // 8, dtype=torch.int64, device="cuda:%d" % self.device)
+
+    def attn_workspace(self, rows, pairs, nlimbs, n1, n2, squarings):
+        n = ckks_attn_workspace_bytes(self, rows, pairs, nlimbs, n1, n2, squarings)
+        if n == 0:
+            raise CkksError(-2, "bad shape for workspace query")
+        return torch.empty(n // 8, dtype=torch.int64, device="cuda:%d" % self.device)
+
+    def rmsnorm_workspace(self, batch, nlimbs, n1, n2, iterations):
+        n = ckks_rmsnorm_workspace_bytes(self, batch, nlimbs, n1, n2, iterations)
         if n == 0:
             raise CkksError(-2, "bad shape for workspace query")
         return torch.empty(n // 8, dtype=torch.int64, device="cuda:%d" % self.device)
@@ -383,3 +405,72 @@ def ckks_linattn_chunk(ctx, o_out, state_out, q, k, v, state_in, decay, tokens, 
                              evk_giant, evk_value)
     _check(_lib.ckks_linattn_chunk(ctx.handle, *tensors, tokens, B, nlimbs, n1, n2, stride, *keys, _ptr(ws, "ws", ctx),
                                    ws.numel() * 8, _stream()))
+
+
+def attn_pairs(new_lens, lens, window=0, sinks=0):
+    """The number of (query, token) pairs that ckks_attn_paged scores, which its workspace is sized by."""
+    total = 0
+    for n, m in zip(lens, new_lens):
+        for t in range(n - m, n):
+            tail = 0 if window == 0 or t < window else t - window + 1
+            total += min(sinks, tail) + t - tail + 1
+    return total
+
+
+def ckks_attn_workspace_bytes(ctx, rows, pairs, nlimbs, n1, n2, squarings):
+    return int(_lib.ckks_attn_workspace_bytes(ctx.handle, rows, pairs, nlimbs, n1, n2, squarings))
+
+
+def _cache(ctx, new_lens, lens, k_pages, v_pages, page_tokens, k_limbs, v_limbs):
+    """The host arrays that describe a cache. Pages are tensors [page_tokens][2][limbs][N], sequence after sequence; None: not there."""
+    if len(new_lens) != len(lens):
+        raise ValueError("need a number of new tokens for every sequence")
+    if min(list(lens) + list(new_lens) + [0]) < 0 or page_tokens < 1:
+        raise ValueError("lengths must not be negative and pages not empty")
+    count = sum(-(-n // page_tokens) for n in lens)
+    if len(k_pages) != count or len(v_pages) != count:
+        raise ValueError("need %d pages of keys and of values" % count)
+
+    def pages(name, tensors, limbs):
+        e = page_tokens * 2 * limbs * ctx.N
+        return (C.c_void_p * max(1, count))(*[None if t is None else _ptr(t, name, ctx, e).value for t in tensors])
+
+    return len(lens), _ids(new_lens)[0], _ids(lens)[0], pages("k_pages", k_pages, k_limbs), pages("v_pages", v_pages, v_limbs)
+
+
+def ckks_kv_append(ctx, k, v, in_limbs, new_lens, lens, k_pages, v_pages, page_tokens, k_limbs, v_limbs):
+    e = sum(new_lens) * 2 * in_limbs * ctx.N
+    cache = _cache(ctx, new_lens, lens, k_pages, v_pages, page_tokens, k_limbs, v_limbs)
+    _check(_lib.ckks_kv_append(ctx.handle, _ptr(k, "k", ctx, e), _ptr(v, "v", ctx, e), in_limbs, *cache, page_tokens, k_limbs, v_limbs,
+                               _stream()))
+
+
+def ckks_attn_paged(ctx, o_out, q, nlimbs, new_lens, lens, k_pages, v_pages, page_tokens, k_limbs, v_limbs, window, sinks, bias,
+                    squarings, n1, n2, stride, evk_mult, evk_baby, evk_giant, ws):
+    if len(evk_baby) != n1 - 1 or len(evk_giant) != n2 - 1:
+        raise ValueError("need n1-1 baby-step keys and n2-1 giant-step keys")
+    rows = sum(new_lens)
+    cache = _cache(ctx, new_lens, lens, k_pages, v_pages, page_tokens, k_limbs, v_limbs)
+    _check(_lib.ckks_attn_paged(ctx.handle, _ptr(o_out, "o_out", ctx, max(0, rows * 2 * (nlimbs - 1 - squarings) * ctx.N)),
+                                _ptr(q, "q", ctx, rows * 2 * nlimbs * ctx.N), nlimbs, *cache, page_tokens, k_limbs, v_limbs, window,
+                                sinks, bias, squarings, n1, n2, stride, _ptr(evk_mult, "evk_mult", ctx, _key_elems(ctx)),
+                                _keys(ctx, "evk_baby", evk_baby), _keys(ctx, "evk_giant", evk_giant), _ptr(ws, "ws", ctx),
+                                ws.numel() * 8, _stream()))
+
+
+def ckks_rmsnorm_workspace_bytes(ctx, batch, nlimbs, n1, n2, iterations):
+    return int(_lib.ckks_rmsnorm_workspace_bytes(ctx.handle, batch, nlimbs, n1, n2, iterations))
+
+
+def ckks_rmsnorm(ctx, ct_out, h_out, ct_x, ct_res, gain, square, eps, start, factors, B, nlimbs, n1, n2, stride, evk_mult, evk_baby,
+                 evk_giant, ws):
+    if len(evk_baby) != n1 - 1 or len(evk_giant) != n2 - 1:
+        raise ValueError("need n1-1 baby-step keys and n2-1 giant-step keys")
+    e, L = B * 2 * nlimbs * ctx.N, nlimbs - 1 - 2 * len(factors)
+    numbers = (C.c_int64 * max(1, len(factors)))(*factors)
+    optional = [None if t is None else _ptr(t, name, ctx, n) for t, name, n in
+                ((h_out, "h_out", e), (ct_res, "ct_res", e), (gain, "gain", max(0, (L + 1) * ctx.N)))]
+    _check(_lib.ckks_rmsnorm(ctx.handle, _ptr(ct_out, "ct_out", ctx, max(0, B * 2 * L * ctx.N)), optional[0],
+                             _ptr(ct_x, "ct_x", ctx, e), optional[1], optional[2], square, eps, start, numbers, len(factors), B, nlimbs,
+                             n1, n2, stride, _ptr(evk_mult, "evk_mult", ctx, _key_elems(ctx)), _keys(ctx, "evk_baby", evk_baby),
+                             _keys(ctx, "evk_giant", evk_giant), _ptr(ws, "ws", ctx), ws.numel() * 8, _stream()))

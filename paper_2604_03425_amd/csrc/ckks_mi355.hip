@@ -16,6 +16,7 @@
 #include "ntt16_kernels.hip.h"
 #include "ntt_limb.hip.h"
 #include "attention.hip.h"
+#include "decoder.hip.h"
 
 typedef unsigned __int128 u128;
 
@@ -131,6 +132,12 @@ struct LevelTables {
   u64* rs_mat = nullptr;           // [nlimbs-1][5] row i = (1, 0, 0, 0, -q_last) mod q_i, Montgomery form
   ulonglong2* rs_qinv = nullptr;   // [nlimbs-1]   q_last^-1 mod q_i, Shoup pair
   ulonglong2* rs_qinv16 = nullptr; // same for the two-pass kernels: (c, c/q) doubles on double-precision moduli
+  // ModDown by D = P q_{nlimbs-1} from this limb count; sources q_{nlimbs-1}, p_0 .. p_{K-1}
+  uint4* dm_pieces = nullptr;      // [nlimbs-1] matrices of bytes of (D/c_i) mod q_t, for conv_wide_kernel (scaled like dn_pieces)
+  ulonglong2* dm_inv = nullptr;    // [K+1]  (D/c_i)^-1 mod c_i, Shoup pairs
+  ulonglong2* dm_scale = nullptr;  // [K+1]  the same / N (two-pass rings: in the form of the class, integer ones times 2^64)
+  ulonglong2* dm_pinv = nullptr;   // [nlimbs-1]  D^-1 mod q_t, Shoup pairs
+  ulonglong2* dm_pinv2 = nullptr;  // [nlimbs-1]  the same in the form of pinv2
 };
 
 }  // namespace
@@ -141,7 +148,8 @@ enum ProfKind {
   PK_FWD_ROWS, PK_FWD_BLOCKS = PK_FWD_ROWS + 3, PK_INV_BLOCKS = PK_FWD_BLOCKS + 3, PK_INV_ROWS = PK_INV_BLOCKS + 3,
   PK_FWD_FINAL = PK_INV_ROWS + 3,
   PK_AUTOMORPH = PK_FWD_FINAL + 3, PK_MODUP, PK_INNER, PK_INNER16, PK_INNER16_INT, PK_INNER_C, PK_INNER8, PK_INNER8_BIG, PK_BCONV_ROWS, PK_MODDOWN = PK_BCONV_ROWS + 3, PK_FINAL, PK_TENSOR, PK_PMACC, PK_PMACC_FP, PK_ADD,
-  PK_KS12_FRONT, PK_KS12_DIGITS, PK_KS12_SPECIAL, PK_KS12_FINAL, PK_CONV_ROWS, PK_COPY, PK_PMACC_STAGED, PK_PMACC_FP_STAGED, PK_ROT_SUM, PK_PROD_SUM, PK_GATHER, PK_COUNT
+  PK_KS12_FRONT, PK_KS12_DIGITS, PK_KS12_SPECIAL, PK_KS12_FINAL, PK_CONV_ROWS, PK_COPY, PK_PMACC_STAGED, PK_PMACC_FP_STAGED, PK_ROT_SUM, PK_PROD_SUM, PK_GATHER,
+  PK_PAIR_PRODUCTS, PK_WEIGHTED_VALUES, PK_CT_PRODUCTS, PK_NORM_START, PK_KV_APPEND, PK_COUNT
 };
 static const char* const kProfNames[PK_COUNT] = {
     "ntt_fwd_pass", "ntt_inv_pass",
@@ -154,7 +162,8 @@ static const char* const kProfNames[PK_COUNT] = {
     "ntt16_bconv_rows_kernel<0>", "ntt16_bconv_rows_kernel<1>", "ntt16_bconv_rows_kernel<2>", "moddown_kernel", "ks_final_kernel", "tensor_kernel",
     "pmacc_int_kernel", "pmacc_fp_kernel", "addto_kernel",
     "ks12_front_kernel", "ks12_digits_kernel", "ks12_special_kernel", "ks12_final_kernel", "conv_rows_kernel", "copy",
-    "pmacc_int_staged_kernel", "pmacc_fp_staged_kernel", "rot_sum_kernel", "prod_sum_kernel", "gather_kernel"};
+    "pmacc_int_staged_kernel", "pmacc_fp_staged_kernel", "rot_sum_kernel", "prod_sum_kernel", "gather_kernel",
+    "pair_products_kernel", "weighted_values_kernel", "ct_products_kernel", "norm_start_kernel", "kv_append_kernel"};
 struct ProfRec {
   int kind;
   hipEvent_t start, stop;
@@ -451,6 +460,38 @@ LevelTables build_level(const ckks_ctx* c, u32 nlimbs, LevelArena& arena) {
   const u64 q_last = c->mod[nlimbs - 1], n_inv = h_inv(c->N % q_last, q_last), one = 1;
   for (u32 i = 0; i + 1 < nlimbs; i++) conv_rows_of(rs_pieces, i, 1, &one, 1, is_fp(q_last) ? 7 : CONV_PIECES, c->mod[i]);
   std::vector<ulonglong2> rs_scale(1, is_fp(q_last) ? as_fp(n_inv, q_last) : ulonglong2{n_inv, h_shoup(n_inv, q_last)});
+  if (nlimbs > 1 && K) {
+    std::vector<u64> src(1, q_last);
+    for (u32 k = 0; k < K; k++) src.push_back(c->mod[c->nq + k]);
+    const u32 n = K + 1, keep = nlimbs - 1, groups = conv_groups(n);
+    auto others = [&](u32 i, u64 m) {   // the product of all sources but number i (of all for i = n), modulo m
+      u64 v = 1 % m;
+      for (u32 k = 0; k < n; k++)
+        if (k != i) v = h_mul(v, src[k] % m, m);
+      return v;
+    };
+    std::vector<ulonglong2> dm_inv(n), dm_scale(n), dm_pinv(keep), dm_pinv2(keep);
+    std::vector<unsigned char> dm_pieces(pieces_bytes(1, keep, groups, true), 0);
+    for (u32 i = 0; i < n; i++) {
+      const u64 m = src[i], inv = h_inv(others(i, m), m), v = h_mul(inv, h_inv(c->N % m, m), m), w = h_mont(v, m);
+      dm_inv[i] = ulonglong2{inv, h_shoup(inv, m)};
+      dm_scale[i] = is_fp(m) ? as_fp(v, m) : ulonglong2{w, h_shoup(w, m)};
+    }
+    for (u32 t_ = 0; t_ < keep; t_++) {
+      const u64 m = c->mod[t_], inv = h_inv(others(n, m), m), w = h_mont(inv, m);
+      const u64 less = !is_fp(m) && c->logN >= 13 && c->logN <= 16 ? h_inv(h_mont(1, m), m) : 1;
+      std::vector<u64> row(n);
+      for (u32 i = 0; i < n; i++) row[i] = h_mul(others(i, m), less, m);
+      wide_rows_of(dm_pieces, 0, t_, (keep + 3) / 4, groups, row.data(), n, m);
+      dm_pinv[t_] = ulonglong2{inv, h_shoup(inv, m)};
+      dm_pinv2[t_] = is_fp(m) ? as_fp(inv, m) : ulonglong2{w, h_shoup(w, m)};
+    }
+    t.dm_pieces = (uint4*)arena.add(dm_pieces);
+    t.dm_inv = arena.add(dm_inv);
+    t.dm_scale = arena.add(dm_scale);
+    t.dm_pinv = arena.add(dm_pinv);
+    t.dm_pinv2 = arena.add(dm_pinv2);
+  }
   t.rs_pieces = (uint4*)arena.add(rs_pieces);
   t.rs_scale = arena.add(rs_scale);
   t.rs_one = arena.add(rs_one);
@@ -511,6 +552,9 @@ int build_levels(ckks_ctx* c) {
     if (t.up_direct) rebase(t.up_direct);
     if (t.dn_direct) rebase(t.dn_direct);
     rebase(t.rs_pieces); rebase(t.rs_scale); rebase(t.rs_one); rebase(t.rs_mat); rebase(t.rs_qinv); rebase(t.rs_qinv16);
+    if (nl > 1 && c->np) {
+      rebase(t.dm_pieces); rebase(t.dm_inv); rebase(t.dm_scale); rebase(t.dm_pinv); rebase(t.dm_pinv2);
+    }
   }
   if (c->d_levels) {
     // a knob changed: nothing may still be reading the old tables
@@ -857,10 +901,12 @@ void launch_modup_n(const ckks_ctx* c, const ModUpArgs& a, u32 beta, u32 B, hipS
   if (c->alpha <= 4) hipLaunchKernelGGL((modup_kernel<4, PRESCALED, NARROW>), grid, block, 0, st, a, a.dcoef, a.ext, a.mods, a.mat);
   else hipLaunchKernelGGL((modup_kernel<8, PRESCALED, NARROW>), grid, block, 0, st, a, a.dcoef, a.ext, a.mods, a.mat);
 }
-// Conversions of more than 8 sources, on the matrix cores.
+// Conversions of more than 8 sources (and ModDown's by a main prime too, of any number), on the matrix cores.
 void launch_wide(const WideArgs& a, u32 digits, u32 npoly, hipStream_t st) {
   const dim3 block(WIDE_THREADS), grid(std::max(1u, (1u << a.logN) / WIDE_THREADS), digits, npoly);
   switch (conv_groups(a.alpha)) {
+    case 1: hipLaunchKernelGGL(conv_wide_kernel<1>, grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL(conv_wide_kernel<2>, grid, block, 0, st, a); break;
     case 3: hipLaunchKernelGGL(conv_wide_kernel<3>, grid, block, 0, st, a); break;
     case 4: hipLaunchKernelGGL(conv_wide_kernel<4>, grid, block, 0, st, a); break;
     case 6: hipLaunchKernelGGL(conv_wide_kernel<6>, grid, block, 0, st, a); break;
@@ -882,7 +928,7 @@ void launch_modup(const ckks_ctx* c, const LevelTables* lt, const ModUpArgs& a, 
     w.mods = c->d_mods;
     w.inv = PRESCALED ? nullptr : lt->up_inv;
     w.logN = a.logN;
-    w.src_slot0 = w.src_id0 = 0;
+    w.src_slot0 = w.src_id0 = w.first_id = 0;
     w.src_nlimbs = a.nlimbs;
     w.alpha = c->alpha;
     w.beta = beta;
@@ -915,7 +961,7 @@ void launch_moddown(const ckks_ctx* c, const LevelTables* lt, const ModDownArgs&
     w.inv = PRESCALED ? nullptr : lt->dn_inv;
     w.logN = a.logN;
     w.src_slot0 = a.src_slot;
-    w.src_id0 = a.src_id0;
+    w.src_id0 = w.first_id = a.src_id0;
     w.src_nlimbs = w.alpha = a.K;
     w.beta = 1;
     w.skip_own = 0;
@@ -2890,3 +2936,4 @@ int ckks_add(ckks_ctx* c, uint64_t* out, const uint64_t* a, const uint64_t* b, u
 }  // extern "C"
 
 #include "attention_calls.hip.h"
+#include "decoder_calls.hip.h"

@@ -28,6 +28,7 @@ struct WideArgs {
   const ulonglong2* inv;     // != null: [beta][alpha] Shoup pairs the sources are multiplied by first
   u32 logN, src_slot0, src_id0, src_nlimbs, alpha, beta, skip_own, ntarget;   // as in ConvArgs
   u32 main, special;         // target t: modulus t below main, t - main + special from there on
+  u32 first_id;              // modulus id of source 0 of all (src_id0, or a main prime before the special ones)
 };
 // The sums of one target put together: V = lo + mid 2^32 + top 2^48 (mod m).
 __device__ __forceinline__ void wide_join(u32& lo, u32& mid, u32& top, int s0, int s1, int s2, int s3, int s4, int s5, int s6, int s7) {
@@ -97,7 +98,7 @@ __global__ void __launch_bounds__(WIDE_THREADS) conv_wide_kernel(WideArgs a) {
 #pragma unroll
   for (int k = 0; k < 4 * G; k++) {
     const u32 i = min((u32)k, len - 1);   // uniform
-    const u64 m = scalar_words(a.mods + a.src_id0 + lo + i)[offsetof(ModInfo, m) / 8], h = m >> 1;
+    const u64 m = scalar_words(a.mods + (lo + i ? a.src_id0 + lo + i : a.first_id))[offsetof(ModInfo, m) / 8], h = m >> 1;
     u64 v = y[k];
     if (a.inv) {
       const const_u64_ptr w = scalar_words(a.inv + (size_t)j * a.alpha + i);

@@ -1,0 +1,198 @@
+// Kernels of attention over a paged cache of ciphertexts and of the root-mean-square norm: what stands between their key switches.
+#pragma once
+#include "attention.hip.h"
+
+#define DECODER_PAIRS 128   // (query, key) pairs or cache entries per launch (their places travel in the kernel's arguments)
+
+// Ciphertexts in memory: component c of ciphertext b at `at + b * stride + c * comp`, limbs N words apart.
+struct CtRef {
+  const u64* at;
+  u64 stride, comp;
+};
+// A signed number modulo m.
+__device__ __forceinline__ u64 signed_residue(long long v, const ModInfo& mi) {
+  const u64 a = v < 0 ? 0 - (u64)v : (u64)v;
+  const u64 r = csub(a - mul_hi64(a, mi.mu64) * mi.m, mi.m);
+  return v < 0 && r ? mi.m - r : r;
+}
+__device__ __forceinline__ ulonglong2 word_pair(const u64* p) { return *(const ulonglong2*)p; }
+__device__ __forceinline__ ulonglong2 plus_number(ulonglong2 x, u64 a, u64 m) { return {addmod(x.x, a, m), addmod(x.y, a, m)}; }
+
+// x * y in three components for two positions.
+template <bool FP>
+struct PairAcc {
+  ProdAcc<FP> v[2][3];
+  __device__ __forceinline__ void mac(const ulonglong2 (&x)[2], const ulonglong2 (&y)[2], const ModInfo& mi) {
+    const u64 a[2][2] = {{x[0].x, x[1].x}, {x[0].y, x[1].y}}, b[2][2] = {{y[0].x, y[1].x}, {y[0].y, y[1].y}};
+#pragma unroll
+    for (int e = 0; e < 2; e++) {
+      v[e][0].mac(a[e][0], b[e][0], mi);
+      v[e][1].mac(a[e][0], b[e][1], mi);
+      v[e][1].mac(a[e][1], b[e][0], mi);
+      v[e][2].mac(a[e][1], b[e][1], mi);
+    }
+  }
+  __device__ __forceinline__ void fold(const ModInfo& mi) {
+#pragma unroll
+    for (int e = 0; e < 2; e++)
+#pragma unroll
+      for (int c = 0; c < 3; c++) v[e][c].fold(mi);
+  }
+  __device__ __forceinline__ ulonglong2 value(int c, const ModInfo& mi) const { return {v[0][c].value(mi), v[1][c].value(mi)}; }
+};
+
+// Scores before their sum over the components: out[i] = q[row[i]] * key[i], three components [pairs][3][nlimbs][N].
+struct PairArgs {
+  CtRef q;
+  u64 key_comp;         // words between the two components of a cached key
+  u64* out;
+  const ModInfo* mods;
+  u32 logN, nlimbs, fp_on;
+  u32 row[DECODER_PAIRS];
+  const u64* key[DECODER_PAIRS];
+};
+template <bool FP>
+__device__ __forceinline__ void pair_products(const PairArgs& a, const ModInfo& mi) {
+  const size_t N = (size_t)1 << a.logN, n = (blockIdx.x * 256 + threadIdx.x) * 2, l = blockIdx.y, i = blockIdx.z;
+  const u64 *q = a.q.at + a.row[i] * a.q.stride + l * N + n, *k = a.key[i] + l * N + n;
+  const ulonglong2 x[2] = {word_pair(q), word_pair(q + a.q.comp)}, y[2] = {word_pair(k), word_pair(k + a.key_comp)};
+  PairAcc<FP> s;
+  s.mac(x, y, mi);
+  u64* o = a.out + (i * 3 * a.nlimbs + l) * N + n;
+#pragma unroll
+  for (int c = 0; c < 3; c++) *(ulonglong2*)(o + c * a.nlimbs * N) = s.value(c, mi);
+}
+// grid = (N / 512, limbs, pairs)
+__global__ void __launch_bounds__(256) pair_products_kernel(PairArgs a) {
+  const ModInfo mi = a.mods[blockIdx.y];
+  if (mod_class(mi.m, a.fp_on) == 0) pair_products<true>(a, mi);
+  else pair_products<false>(a, mi);
+}
+
+// out[r] (+)= sum over the pairs i of row r of (u[i] + bias) * value[i], three components; bias is added to every slot.
+struct ValueArgs {
+  CtRef u;
+  u64 value_comp;
+  u64* out;             // [rows][3][nlimbs][N]
+  const ModInfo* mods;
+  long long bias;
+  u32 logN, nlimbs, fp_on;
+  u32 row[DECODER_PAIRS];                       // row and first pair of each sum of the launch; bit 31 of row: adds to what is there
+  u32 begin[DECODER_PAIRS + 1];
+  const u64* value[DECODER_PAIRS];
+};
+template <bool FP>
+__device__ __forceinline__ void weighted_values(const ValueArgs& a, const ModInfo& mi) {
+  const size_t N = (size_t)1 << a.logN, n = (blockIdx.x * 256 + threadIdx.x) * 2, l = blockIdx.y, r = blockIdx.z;
+  const u64 bias = signed_residue(a.bias, mi);
+  const u32 first = a.begin[r], end = a.begin[r + 1];
+  PairAcc<FP> s;
+  for (u32 i = first; i < end; i++) {
+    const u64 *u = a.u.at + i * a.u.stride + l * N + n, *v = a.value[i] + l * N + n;
+    const ulonglong2 x[2] = {plus_number(word_pair(u), bias, mi.m), word_pair(u + a.u.comp)}, y[2] = {word_pair(v), word_pair(v + a.value_comp)};
+    s.mac(x, y, mi);
+    // in doubles a sum takes 6 products below 0.9 q on top of a folded one, 128 bits take 130 products below 2^120
+    if (FP ? (i - first) % 3 == 2 : ((i - first) & 63) == 63) s.fold(mi);
+  }
+  u64* o = a.out + ((size_t)(a.row[r] & 0x7FFFFFFFu) * 3 * a.nlimbs + l) * N + n;
+  const bool add = a.row[r] >> 31;
+#pragma unroll
+  for (int c = 0; c < 3; c++) {
+    ulonglong2 w = s.value(c, mi);
+    ulonglong2* to = (ulonglong2*)(o + c * a.nlimbs * N);
+    if (add) {
+      const ulonglong2 old = *to;
+      w = {addmod(w.x, old.x, mi.m), addmod(w.y, old.y, mi.m)};
+    }
+    *to = w;
+  }
+}
+// grid = (N / 512, limbs, rows)
+__global__ void __launch_bounds__(256) weighted_values_kernel(ValueArgs a) {
+  const ModInfo mi = a.mods[blockIdx.y];
+  if (mod_class(mi.m, a.fp_on) == 0) weighted_values<true>(a, mi);
+  else weighted_values<false>(a, mi);
+}
+
+// out[b] = factor (x[b] + bias) * (y[b] + bias) + (z_factor z[b], 0), three components; the biases are added to every slot. z may be
+// null. Ciphertexts from `second` on (0: none) are those of x2 and y2.
+struct ProductArgs {
+  CtRef x, y, x2, y2, z;
+  u64* out;             // [B][3][nlimbs][N]
+  const ModInfo* mods;
+  long long factor, bias, z_factor;
+  u32 logN, nlimbs, fp_on, second;
+};
+template <bool FP>
+__device__ __forceinline__ void ct_products(const ProductArgs& a, const ModInfo& mi) {
+  const size_t N = (size_t)1 << a.logN, n = (blockIdx.x * 256 + threadIdx.x) * 2, l = blockIdx.y, b = blockIdx.z;
+  const bool other = a.second && b >= a.second;
+  const size_t k = other ? b - a.second : b;
+  const CtRef &rx = other ? a.x2 : a.x, &ry = other ? a.y2 : a.y;
+  const u64 *px = rx.at + k * rx.stride + l * N + n, *py = ry.at + k * ry.stride + l * N + n;
+  const u64 bias = signed_residue(a.bias, mi);
+  ulonglong2 x[2] = {plus_number(word_pair(px), bias, mi.m), word_pair(px + rx.comp)};
+  const ulonglong2 y[2] = {plus_number(word_pair(py), bias, mi.m), word_pair(py + ry.comp)};
+  if (a.factor != 1) {
+    const u64 f = signed_residue(a.factor, mi);
+#pragma unroll
+    for (int c = 0; c < 2; c++) x[c] = {prod_mulmod<FP>(x[c].x, f, mi), prod_mulmod<FP>(x[c].y, f, mi)};
+  }
+  PairAcc<FP> s;
+  s.mac(x, y, mi);
+  u64* o = a.out + (b * 3 * a.nlimbs + l) * N + n;
+  const u64 zf = a.z.at ? signed_residue(a.z_factor, mi) : 0;
+#pragma unroll
+  for (int c = 0; c < 3; c++) {
+    ulonglong2 w = s.value(c, mi);
+    if (a.z.at && c < 2) {
+      const ulonglong2 z = word_pair(a.z.at + b * a.z.stride + c * a.z.comp + l * N + n);
+      w = {addmod(w.x, prod_mulmod<FP>(z.x, zf, mi), mi.m), addmod(w.y, prod_mulmod<FP>(z.y, zf, mi), mi.m)};
+    }
+    *(ulonglong2*)(o + c * a.nlimbs * N) = w;
+  }
+}
+// grid = (N / 512, limbs, ciphertexts)
+__global__ void __launch_bounds__(256) ct_products_kernel(ProductArgs a) {
+  const ModInfo mi = a.mods[blockIdx.y];
+  if (mod_class(mi.m, a.fp_on) == 0) ct_products<true>(a, mi);
+  else ct_products<false>(a, mi);
+}
+
+// m += eps and y = start - m, numbers in every slot. Ciphertexts [B][2][nlimbs][N]; grid = (N / 512, limbs, 2 B).
+__global__ void __launch_bounds__(256) norm_start_kernel(u64* m, u64* y, const ModInfo* mods, long long eps, long long start, u32 logN,
+                                                         u32 nlimbs) {
+  const size_t N = (size_t)1 << logN, at = ((size_t)blockIdx.z * nlimbs + blockIdx.y) * N + (blockIdx.x * 256 + threadIdx.x) * 2;
+  const ModInfo mi = mods[blockIdx.y];
+  const bool first = (blockIdx.z & 1) == 0;
+  const u64 e = first ? signed_residue(eps, mi) : 0, s = first ? signed_residue(start, mi) : 0;
+  const ulonglong2 x = plus_number(word_pair(m + at), e, mi.m);
+  *(ulonglong2*)(m + at) = x;
+  *(ulonglong2*)(y + at) = {submod(s, x.x, mi.m), submod(s, x.y, mi.m)};
+}
+
+// out = pt (.) x on the first nlimbs limbs of ciphertexts, [B][2][nlimbs][N]; grid = (N / 512, limbs, 2 B).
+__global__ void __launch_bounds__(256) cut_pmult_kernel(u64* out, CtRef x, const u64* pt, const ModInfo* mods, u32 logN, u32 nlimbs) {
+  const size_t N = (size_t)1 << logN, n = (blockIdx.x * 256 + threadIdx.x) * 2 + blockIdx.y * N;
+  const ModInfo mi = mods[blockIdx.y];
+  const ulonglong2 w = word_pair(pt + n), v = word_pair(x.at + (blockIdx.z / 2) * x.stride + (blockIdx.z & 1) * x.comp + n);
+  *(ulonglong2*)(out + (size_t)blockIdx.z * nlimbs * N + n) = {mulmod(v.x, w.x, mi), mulmod(v.y, w.y, mi)};
+}
+
+// New tokens into their places in the pages of a cache: the first limbs of both components. Entry i < ntokens is a key, the others
+// are values; grid = (N / 512, most limbs, 2 * entries).
+struct AppendArgs {
+  const u64 *k, *v;     // [tokens][2][in_limbs][N]
+  u32 logN, in_limbs, k_limbs, v_limbs, ntokens, first;
+  u64* to[2 * DECODER_PAIRS];
+};
+__global__ void __launch_bounds__(256) kv_append_kernel(AppendArgs a) {
+  const size_t N = (size_t)1 << a.logN;
+  const u32 i = blockIdx.z / 2, c = blockIdx.z & 1, l = blockIdx.y;
+  const bool value = i >= a.ntokens;
+  const u32 limbs = value ? a.v_limbs : a.k_limbs;
+  if (l >= limbs) return;
+  const size_t n = (blockIdx.x * 256 + threadIdx.x) * 2;
+  const u64* from = (value ? a.v : a.k) + ((((size_t)a.first + (value ? i - a.ntokens : i)) * 2 + c) * a.in_limbs + l) * N + n;
+  *(ulonglong2*)(a.to[i] + ((size_t)c * limbs + l) * N + n) = word_pair(from);
+}
