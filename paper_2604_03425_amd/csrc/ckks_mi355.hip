@@ -133,6 +133,7 @@ struct LevelTables {
   ulonglong2* rs_qinv = nullptr;   // [nlimbs-1]   q_last^-1 mod q_i, Shoup pair
   ulonglong2* rs_qinv16 = nullptr; // same for the two-pass kernels: (c, c/q) doubles on double-precision moduli
   // ModDown by D = P q_{nlimbs-1} from this limb count; sources q_{nlimbs-1}, p_0 .. p_{K-1}
+  uint4* dm_rows = nullptr;        // [nlimbs-1] the same for conv_rows_kernel with residues as sources (at most 8 of them, two-pass rings)
   uint4* dm_pieces = nullptr;      // [nlimbs-1] matrices of bytes of (D/c_i) mod q_t, for conv_wide_kernel (scaled like dn_pieces)
   ulonglong2* dm_inv = nullptr;    // [K+1]  (D/c_i)^-1 mod c_i, Shoup pairs
   ulonglong2* dm_scale = nullptr;  // [K+1]  the same / N (two-pass rings: in the form of the class, integer ones times 2^64)
@@ -471,7 +472,9 @@ LevelTables build_level(const ckks_ctx* c, u32 nlimbs, LevelArena& arena) {
       return v;
     };
     std::vector<ulonglong2> dm_inv(n), dm_scale(n), dm_pinv(keep), dm_pinv2(keep);
-    std::vector<unsigned char> dm_pieces(pieces_bytes(1, keep, groups, true), 0);
+    const bool rows_fit = n <= CONV_MAX_SRC && c->logN >= 13 && c->logN <= 16 &&
+                          std::all_of(c->mod.begin(), c->mod.end(), [&](u64 m) { return is_fp(m) || h_bits(m) > CONV_INT_MIN_BITS; });
+    std::vector<unsigned char> dm_pieces(pieces_bytes(1, keep, groups, true), 0), dm_rows(rows_fit ? pieces_bytes(1, keep, groups, false) : 0, 0);
     for (u32 i = 0; i < n; i++) {
       const u64 m = src[i], inv = h_inv(others(i, m), m), v = h_mul(inv, h_inv(c->N % m, m), m), w = h_mont(v, m);
       dm_inv[i] = ulonglong2{inv, h_shoup(inv, m)};
@@ -483,10 +486,12 @@ LevelTables build_level(const ckks_ctx* c, u32 nlimbs, LevelArena& arena) {
       std::vector<u64> row(n);
       for (u32 i = 0; i < n; i++) row[i] = h_mul(others(i, m), less, m);
       wide_rows_of(dm_pieces, 0, t_, (keep + 3) / 4, groups, row.data(), n, m);
+      if (rows_fit) conv_rows_of(dm_rows, t_, groups, row.data(), n, CONV_PIECES, m);
       dm_pinv[t_] = ulonglong2{inv, h_shoup(inv, m)};
       dm_pinv2[t_] = is_fp(m) ? as_fp(inv, m) : ulonglong2{w, h_shoup(w, m)};
     }
     t.dm_pieces = (uint4*)arena.add(dm_pieces);
+    if (rows_fit) t.dm_rows = (uint4*)arena.add(dm_rows);
     t.dm_inv = arena.add(dm_inv);
     t.dm_scale = arena.add(dm_scale);
     t.dm_pinv = arena.add(dm_pinv);
@@ -553,7 +558,9 @@ int build_levels(ckks_ctx* c) {
     if (t.dn_direct) rebase(t.dn_direct);
     rebase(t.rs_pieces); rebase(t.rs_scale); rebase(t.rs_one); rebase(t.rs_mat); rebase(t.rs_qinv); rebase(t.rs_qinv16);
     if (nl > 1 && c->np) {
-      rebase(t.dm_pieces); rebase(t.dm_inv); rebase(t.dm_scale); rebase(t.dm_pinv); rebase(t.dm_pinv2);
+      rebase(t.dm_pieces);
+      if (t.dm_rows) rebase(t.dm_rows);
+      rebase(t.dm_inv); rebase(t.dm_scale); rebase(t.dm_pinv); rebase(t.dm_pinv2);
     }
   }
   if (c->d_levels) {
@@ -991,6 +998,9 @@ struct KsIo {
   // ciphertexts [B][2][nlimbs][N], whose other two product terms are the addends
   const u64 *prod_a = nullptr, *prod_b = nullptr;
   bool steps = false;          // ring 2^12: one kernel per step (whole_limb said no)
+  // two-pass rings with knob 3 at its default, addends add2 only: division by the last main prime too, so that out has a limb less. The
+  // addends come divided by that prime, and P times their last limb (on integer moduli times 2^-64) lies in the accumulators already.
+  bool drop = false;
   int more = KS_PLAIN;         // two-pass rings with knob 3 at its default: KS_WEIGHTED or KS_MAPPED with these arguments
   KsMore more_args = {};
 };
@@ -1062,6 +1072,7 @@ void launch_conv_len(const ConvJob& j, dim3 grid, hipStream_t st) {
 template <int LOGR>
 void launch_conv_of(const ConvJob& j, dim3 grid, hipStream_t st) {
   if (j.a.direct) launch_conv_direct<LOGR>(j, grid, st);
+  else if (j.a.alpha <= 4 && j.ready) hipLaunchKernelGGL((conv_rows_kernel<LOGR, 4, false, true>), grid, dim3(CONV_THREADS), 0, st, j.a);
   else if (j.a.alpha <= 4) launch_conv_len<LOGR, 4, false>(j, grid, st);
   else if (j.ready) launch_conv_len<LOGR, 8, true>(j, grid, st);
   else launch_conv_len<LOGR, 8, false>(j, grid, st);
@@ -1112,6 +1123,7 @@ void conv_plan(const ckks_ctx* c, ConvJob& job, TargetId target_id) {
       if (fp) a.nfp++;
       else a.nint++;
     }
+  a.first_id = a.src_id0;
   job.fp = host_class(c, c->mod[a.src_id0]) == 0;
   const u32 len = std::min(a.alpha, a.src_nlimbs), own = a.skip_own ? len : 0;   // own limbs: of the sources' kind, not converted
   const u32 targets = a.nfp + a.nint - own, wtargets = (a.nfp - (job.fp ? own : 0)) * 4 + (a.nint - (job.fp ? 0 : own)) * 7;
@@ -1185,6 +1197,29 @@ ConvJob conv_down_job(const ckks_ctx* c, const LevelTables* lt, const u64* acc, 
   return job;
 }
 
+// The conversion of ModDown by P q_{nlimbs-1}: from limb nlimbs - 1 and the special ones of both accumulators, in coefficient form, to tq.
+WideArgs drop_wide_args(const ckks_ctx* c, const LevelTables* lt, const u64* acc, u64* tq, u32 nlimbs) {
+  WideArgs w;
+  w.src = acc;
+  w.dst = tq;
+  w.src_poly_stride = (u64)lt->next * c->N;
+  w.dst_poly_stride = (u64)(nlimbs - 1) * c->N;
+  w.pieces = lt->dm_pieces;
+  w.red = c->d_wide_red;
+  w.mods = c->d_mods;
+  w.inv = two_pass(c) ? nullptr : lt->dm_inv;
+  w.logN = c->logN;
+  w.src_slot0 = nlimbs - 1;
+  w.src_id0 = c->nq - 1;
+  w.first_id = nlimbs - 1;
+  w.src_nlimbs = w.alpha = c->np + 1;
+  w.beta = 1;
+  w.skip_own = 0;
+  w.ntarget = w.main = nlimbs - 1;
+  w.special = 0;
+  return w;
+}
+
 // ModDown's conversion and the first forward pass of its result on the two-pass path: the special limbs of both
 // accumulators back to coefficient form (scaled by (P/p_k)^-1 / N), P -> Q_l, stages 0..7; tq receives the converted
 // limbs in row-pass form. Knob 2 = 1 does the conversion inside the row pass (ntt16_bconv_rows_kernel).
@@ -1246,6 +1281,64 @@ int ks16_moddown_rows(ckks_ctx* c, const LevelTables* lt, u32 B, u32 nlimbs, u64
   a.pitch = lt->dn_pitch;
   for (u32 i = 0; i < 128; i++) a.id[i] = (unsigned char)(i < nlimbs ? i : 0);
   return launch_bconv_rows(c, a, B * 2, lt->narrow_dn, [&](u32 s) { return host_class(c, c->mod[s]); }, st);
+}
+
+// The same where the last main limb is divided away with the special ones: it joins them as a source. Sources are of any kind, so they
+// all go through their inverse pass before the conversion, which takes residues.
+int ks16_drop_rows(ckks_ctx* c, const LevelTables* lt, u32 B, u32 nlimbs, u64* acc, u64* tq, hipStream_t st, bool int_blocks_done) {
+  int rc;
+  const u32 N = c->N, next = lt->next, K = c->np, keep = nlimbs - 1;
+  LimbMap sources = identity_map(0), special = identity_map(0);
+  sources.id[0] = (unsigned char)keep;
+  for (u32 k = 0; k < K; k++) sources.id[k + 1] = special.id[k] = (unsigned char)(c->nq + k);
+  auto inverse = [&](u32 slot0, u32 n, const LimbMap& ids, const NttOpts& o) {
+    return launch_ntt(c, true, acc, (u64)next * N, acc, (u64)next * N, B * 2, slot0, n, ids, 0, 0, st, o);
+  };
+  NttOpts o;
+  o.scale = lt->dm_scale;
+  if (int_blocks_done) {
+    NttOpts blocks = o, rows = o;
+    blocks.blocks_only = true;
+    if ((rc = inverse(keep, 1, sources, blocks))) return rc;
+    blocks.scale = lt->dm_scale + 1;
+    blocks.only_class = 0;
+    if ((rc = inverse(nlimbs, K, special, blocks))) return rc;
+    rows.rows_only = true;
+    if ((rc = inverse(keep, K + 1, sources, rows))) return rc;
+  } else if ((rc = inverse(keep, K + 1, sources, o))) {
+    return rc;
+  }
+  if (lt->dm_rows && c->tune[2] == 0) {
+    ConvJob job;
+    ConvArgs& a = job.a;
+    a.src = acc;
+    a.dst = tq;
+    a.src_poly_stride = (u64)next * N;
+    a.dst_poly_stride = (u64)keep * N;
+    a.src_slot0 = keep;
+    a.src_id0 = c->nq - 1;
+    a.src_nlimbs = a.alpha = K + 1;
+    a.beta = 1;
+    a.skip_own = 0;
+    a.ntarget = keep;
+    a.pieces = lt->dm_rows;
+    a.scale = lt->dm_scale;
+    job.npoly = B * 2;
+    conv_plan(c, job, [](u32 s) { return s; });
+    a.first_id = keep;
+    job.fp = false;
+    job.ready = true;
+    a.nsplit = conv_shares((u64)job.npoly * (N / CONV_TILE), K + 1, a.nfp * 4 + a.nint * 7, keep);
+    return launch_conv_rows(c, job, st);
+  }
+  {
+    ProfScope ps(c, PK_MODDOWN, st);
+    launch_wide(drop_wide_args(c, lt, acc, tq, nlimbs), 1, B * 2, st);
+    HIP_TRY(hipGetLastError());
+  }
+  NttOpts rows;
+  rows.rows_only = true;
+  return launch_ntt(c, false, tq, (u64)keep * N, tq, (u64)keep * N, B * 2, 0, keep, identity_map(keep), 0, 0, st, rows);
 }
 
 // Last kernel of a key switch on the two-pass path: block pass of tq fused with (acc - tq) / P and the addends.
@@ -1491,7 +1584,8 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
     for (int cls = 1; cls <= 2; cls++) {
       u32 cnt = 0;
       for (u32 s_ = 0; s_ < next; s_++)
-        if (ext_class(s_) == cls && (s_ >= nlimbs ? special : main_slots)) a.slots[cnt++] = (unsigned char)s_;
+        if (ext_class(s_) == cls && (s_ >= nlimbs ? special : main_slots && !(fin && io.drop && s_ + 1 == nlimbs)))
+          a.slots[cnt++] = (unsigned char)s_;
       if (!cnt) continue;
       ProfScope ps(c, PK_INNER8 + cls - 1, st);
       const dim3 grid(B, N / 2048, cnt);
@@ -1499,7 +1593,7 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
       else launch_inner8_of<2>(grid, a, fin, io.more, st);
     }
   };
-  const bool stored = fused_fp && !acc_add && !io.prod_a && io.more == KS_PLAIN && int_sums_stored(c, B, nlimbs, false);
+  const bool stored = fused_fp && !acc_add && !io.prod_a && !io.drop && io.more == KS_PLAIN && int_sums_stored(c, B, nlimbs, false);
   launch_inner8(ia, true, acc_add || !fused_fp || stored, false);
   HIP_TRY(hipGetLastError());
   // double-precision slots whose accumulators are needed in memory: the special ones always (ModDown reads them),
@@ -1532,8 +1626,24 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
     if ((rc = launch_inner_fp(true, acc_add || !fused_fp, st))) return rc;
   }
   if (acc_add) return CKKS_OK;
+  const u32 keep = io.drop ? nlimbs - 1 : nlimbs;
+  if (io.drop) {   // the last main limb's accumulators, on top of what lies there
+    FwdInnerArgs a = ia;
+    a.accumulate = 1;
+    a.twi = nullptr;
+    a.slots[0] = (unsigned char)keep;
+    const int cls = ext_class(keep);
+    ProfScope ps(c, cls == 0 ? (int)PK_INNER_C : PK_INNER8 + cls - 1, st);
+    const dim3 grid(B, N / 2048, 1);
+    if (cls == 0) launch_inner_c(c, B, 1, a, st);
+    else if (cls == 1) launch_inner8_of<1>(grid, a, false, KS_PLAIN, st);
+    else launch_inner8_of<2>(grid, a, false, KS_PLAIN, st);
+    HIP_TRY(hipGetLastError());
+  }
   // 4.
-  if ((rc = ks16_moddown_rows(c, lt, B, nlimbs, acc, tq, st, true))) return rc;
+  if (io.drop) rc = ks16_drop_rows(c, lt, B, nlimbs, acc, tq, st, true);
+  else rc = ks16_moddown_rows(c, lt, B, nlimbs, acc, tq, st, true);
+  if (rc) return rc;
   if (fork && fused_fp) HIP_TRY(hipStreamWaitEvent(st, c->ev_join, 0));
   // 5.
   if (!fused_fp) return ks16_assemble(c, lt, io, B, nlimbs, acc, tq, st);
@@ -1543,14 +1653,15 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
   a.fin_add_src = io.add_src;
   a.fin_add2 = io.add2 ? io.add2 : io.out;
   a.fin_add2_three = io.add2 && io.add2_three ? 1u : 0u;
-  a.fin_pinv = lt->pinv2;
+  a.fin_pinv = io.drop ? lt->dm_pinv2 : lt->pinv2;
+  a.fin_limbs = keep;
   a.fin_mode0 = io.mode[0];
   a.fin_mode1 = io.mode[1];
   a.fin_galois = io.add_galois;
   a.prod_a = io.prod_a;
   a.prod_b = io.prod_b;
   u32 cnt = 0;
-  for (u32 s_ = 0; s_ < nlimbs; s_++)
+  for (u32 s_ = 0; s_ < keep; s_++)
     if (ext_class(s_) == 0) a.slots[cnt++] = (unsigned char)s_;
   if (cnt) {
     ProfScope ps(c, PK_INNER_C, st);

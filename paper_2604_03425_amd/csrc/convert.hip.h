@@ -48,6 +48,7 @@ struct ConvArgs {
   u64 src_poly_stride;       // elements between the source rows of consecutive (p / beta)
   u64 dst_poly_stride;       // elements between consecutive destination polynomials p
   u32 src_slot0, src_id0;    // limb index inside a source row, and modulus id, of the first source of digit 0
+  u32 first_id;              // modulus id of source 0 itself (src_id0, or a main prime's before special ones)
   u32 src_nlimbs, alpha, beta;  // digit j = p % beta owns sources j*alpha .. j*alpha + len - 1
   u32 skip_own;              // != 0: target slots j*alpha .. j*alpha + len - 1 are the digit's own limbs: left alone
   u32 ntarget;               // targets of a digit in the constant tables
@@ -558,7 +559,7 @@ __global__ void __launch_bounds__(CONV_THREADS) __attribute__((amdgpu_waves_per_
       for (int i = 0; i < 4; i++) y[k][i] = 0;
       return;
     }
-    const u32 id = a.src_id0 + lo + k;
+    const u32 id = k == 0 && lo == 0 ? a.first_id : a.src_id0 + lo + k;
     const ModInfo mi = conv_mod(a.mods, id);
     ulonglong2 sc;
     if (!READY) scalar_fetch(sc, a.scale, lo + k);

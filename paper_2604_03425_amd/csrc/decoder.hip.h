@@ -41,13 +41,38 @@ struct PairAcc {
   __device__ __forceinline__ ulonglong2 value(int c, const ModInfo& mi) const { return {v[0][c].value(mi), v[1][c].value(mi)}; }
 };
 
-// Scores before their sum over the components: out[i] = q[row[i]] * key[i], three components [pairs][3][nlimbs][N].
+// Products in three components, where a key switch that divides by P (kept = nlimbs) or by P and the last prime (kept = nlimbs - 1) expects
+// them. In the latter case the first two components are divided by that prime on the limbs that stay, and P times their last limb, in the
+// form of the accumulators there, starts those.
+struct ProductOut {
+  u64* out;                 // [..][3][nlimbs][N]
+  const ulonglong2* less;   // null: kept = nlimbs; else [nlimbs - 1] Shoup pairs of q_last^-1
+  u64* last;                // limb nlimbs - 1 of accumulator c of ciphertext b at last + (2 b + c) * last_stride
+  u64 last_stride;
+  u32 nlimbs;
+};
+template <bool FP>
+__device__ __forceinline__ void store_product(const ProductOut& o, size_t b, int c, u32 l, size_t n, size_t N, ulonglong2 w, const ModInfo& mi) {
+  if (o.less && c < 2) {
+    if (l + 1 == o.nlimbs) {
+      if (FP) w = {prod_mulmod<true>(w.x, mi.pmod, mi), prod_mulmod<true>(w.y, mi.pmod, mi)};
+      else w = {csub(mont_mul63(w.x, mi.pmod, mi.m, mi.minv), mi.m), csub(mont_mul63(w.y, mi.pmod, mi.m, mi.minv), mi.m)};
+      *(ulonglong2*)(o.last + (2 * b + c) * o.last_stride + n) = w;
+      return;
+    }
+    const ulonglong2 f = o.less[l];
+    w = {shoup(w.x, f.x, f.y, mi.m), shoup(w.y, f.x, f.y, mi.m)};
+  }
+  *(ulonglong2*)(o.out + ((b * 3 + c) * o.nlimbs + l) * N + n) = w;
+}
+
+// Scores before their sum over the components: q[row[i]] * key[i] for pair i.
 struct PairArgs {
   CtRef q;
   u64 key_comp;         // words between the two components of a cached key
-  u64* out;
+  ProductOut o;
   const ModInfo* mods;
-  u32 logN, nlimbs, fp_on;
+  u32 logN, fp_on;
   u32 row[DECODER_PAIRS];
   const u64* key[DECODER_PAIRS];
 };
@@ -58,9 +83,8 @@ __device__ __forceinline__ void pair_products(const PairArgs& a, const ModInfo& 
   const ulonglong2 x[2] = {word_pair(q), word_pair(q + a.q.comp)}, y[2] = {word_pair(k), word_pair(k + a.key_comp)};
   PairAcc<FP> s;
   s.mac(x, y, mi);
-  u64* o = a.out + (i * 3 * a.nlimbs + l) * N + n;
 #pragma unroll
-  for (int c = 0; c < 3; c++) *(ulonglong2*)(o + c * a.nlimbs * N) = s.value(c, mi);
+  for (int c = 0; c < 3; c++) store_product<FP>(a.o, i, c, (u32)l, n, N, s.value(c, mi), mi);
 }
 // grid = (N / 512, limbs, pairs)
 __global__ void __launch_bounds__(256) pair_products_kernel(PairArgs a) {
@@ -114,42 +138,48 @@ __global__ void __launch_bounds__(256) weighted_values_kernel(ValueArgs a) {
   else weighted_values<false>(a, mi);
 }
 
-// out[b] = factor (x[b] + bias) * (y[b] + bias) + (z_factor z[b], 0), three components; the biases are added to every slot. z may be
-// null. Ciphertexts from `second` on (0: none) are those of x2 and y2.
+// factor (x[b] + bias) * (y[b] + bias) + (z_factor z[b], 0) for ciphertext b; the biases are added to every slot. z may be null.
+// second != 0: also x2[b] * y[b], as ciphertext second + b.
 struct ProductArgs {
-  CtRef x, y, x2, y2, z;
-  u64* out;             // [B][3][nlimbs][N]
+  CtRef x, y, x2, z;
+  ProductOut o;
   const ModInfo* mods;
   long long factor, bias, z_factor;
-  u32 logN, nlimbs, fp_on, second;
+  u32 logN, fp_on, second;
 };
 template <bool FP>
 __device__ __forceinline__ void ct_products(const ProductArgs& a, const ModInfo& mi) {
   const size_t N = (size_t)1 << a.logN, n = (blockIdx.x * 256 + threadIdx.x) * 2, l = blockIdx.y, b = blockIdx.z;
-  const bool other = a.second && b >= a.second;
-  const size_t k = other ? b - a.second : b;
-  const CtRef &rx = other ? a.x2 : a.x, &ry = other ? a.y2 : a.y;
-  const u64 *px = rx.at + k * rx.stride + l * N + n, *py = ry.at + k * ry.stride + l * N + n;
+  const u64 *px = a.x.at + b * a.x.stride + l * N + n, *py = a.y.at + b * a.y.stride + l * N + n;
   const u64 bias = signed_residue(a.bias, mi);
-  ulonglong2 x[2] = {plus_number(word_pair(px), bias, mi.m), word_pair(px + rx.comp)};
-  const ulonglong2 y[2] = {plus_number(word_pair(py), bias, mi.m), word_pair(py + ry.comp)};
+  ulonglong2 x[2] = {plus_number(word_pair(px), bias, mi.m), word_pair(px + a.x.comp)};
+  const ulonglong2 y[2] = {plus_number(word_pair(py), bias, mi.m), word_pair(py + a.y.comp)};
   if (a.factor != 1) {
     const u64 f = signed_residue(a.factor, mi);
 #pragma unroll
     for (int c = 0; c < 2; c++) x[c] = {prod_mulmod<FP>(x[c].x, f, mi), prod_mulmod<FP>(x[c].y, f, mi)};
   }
-  PairAcc<FP> s;
-  s.mac(x, y, mi);
-  u64* o = a.out + (b * 3 * a.nlimbs + l) * N + n;
-  const u64 zf = a.z.at ? signed_residue(a.z_factor, mi) : 0;
+  {
+    PairAcc<FP> s;
+    s.mac(x, y, mi);
+    const u64 zf = a.z.at ? signed_residue(a.z_factor, mi) : 0;
 #pragma unroll
-  for (int c = 0; c < 3; c++) {
-    ulonglong2 w = s.value(c, mi);
-    if (a.z.at && c < 2) {
-      const ulonglong2 z = word_pair(a.z.at + b * a.z.stride + c * a.z.comp + l * N + n);
-      w = {addmod(w.x, prod_mulmod<FP>(z.x, zf, mi), mi.m), addmod(w.y, prod_mulmod<FP>(z.y, zf, mi), mi.m)};
+    for (int c = 0; c < 3; c++) {
+      ulonglong2 w = s.value(c, mi);
+      if (a.z.at && c < 2) {
+        const ulonglong2 z = word_pair(a.z.at + b * a.z.stride + c * a.z.comp + l * N + n);
+        w = {addmod(w.x, prod_mulmod<FP>(z.x, zf, mi), mi.m), addmod(w.y, prod_mulmod<FP>(z.y, zf, mi), mi.m)};
+      }
+      store_product<FP>(a.o, b, c, (u32)l, n, N, w, mi);
     }
-    *(ulonglong2*)(o + c * a.nlimbs * N) = w;
+  }
+  if (a.second) {
+    const u64* p2 = a.x2.at + b * a.x2.stride + l * N + n;
+    const ulonglong2 x2[2] = {word_pair(p2), word_pair(p2 + a.x2.comp)};
+    PairAcc<FP> s;
+    s.mac(x2, y, mi);
+#pragma unroll
+    for (int c = 0; c < 3; c++) store_product<FP>(a.o, a.second + b, c, (u32)l, n, N, s.value(c, mi), mi);
   }
 }
 // grid = (N / 512, limbs, ciphertexts)

@@ -11,40 +11,8 @@ int ext_mod_down_more(ckks_ctx* c, const LevelTables* lt, u64* acc, u64* out, u3
   int rc;
   const u32 N = c->N, next = lt->next, K = c->np, keep = nlimbs - 1;
   u64* tq = (u64*)(ws + ks_layout(c, B, nlimbs).tq);
-  LimbMap sources = identity_map(0);
-  sources.id[0] = (unsigned char)keep;
-  for (u32 k = 0; k < K; k++) sources.id[k + 1] = (unsigned char)(c->nq + k);
-  NttOpts o1;
-  if (two_pass(c)) o1.scale = lt->dm_scale;
-  if ((rc = launch_ntt(c, true, acc, (u64)next * N, acc, (u64)next * N, B * 2, keep, K + 1, sources, 0, 0, st, o1))) return rc;
-  WideArgs w;
-  w.src = acc;
-  w.dst = tq;
-  w.src_poly_stride = (u64)next * N;
-  w.dst_poly_stride = (u64)keep * N;
-  w.pieces = lt->dm_pieces;
-  w.red = c->d_wide_red;
-  w.mods = c->d_mods;
-  w.inv = two_pass(c) ? nullptr : lt->dm_inv;
-  w.logN = c->logN;
-  w.src_slot0 = keep;
-  w.src_id0 = c->nq - 1;
-  w.first_id = keep;
-  w.src_nlimbs = w.alpha = K + 1;
-  w.beta = 1;
-  w.skip_own = 0;
-  w.ntarget = w.main = keep;
-  w.special = 0;
-  {
-    ProfScope ps(c, PK_MODDOWN, st);
-    launch_wide(w, 1, B * 2, st);
-    HIP_TRY(hipGetLastError());
-  }
-  const LimbMap qmap = identity_map(keep);
   if (two_pass(c)) {
-    NttOpts o2;
-    o2.rows_only = true;
-    if ((rc = launch_ntt(c, false, tq, (u64)keep * N, tq, (u64)keep * N, B * 2, 0, keep, qmap, 0, 0, st, o2))) return rc;
+    if ((rc = ks16_drop_rows(c, lt, B, nlimbs, acc, tq, st, false))) return rc;
     FwdFinalArgs a;
     a.tq = tq;
     a.acc = acc;
@@ -67,7 +35,16 @@ int ext_mod_down_more(ckks_ctx* c, const LevelTables* lt, u64* acc, u64* out, u3
     HIP_TRY(hipGetLastError());
     return CKKS_OK;
   }
-  if ((rc = launch_ntt(c, false, tq, (u64)keep * N, tq, (u64)keep * N, B * 2, 0, keep, qmap, 0, 0, st))) return rc;
+  LimbMap sources = identity_map(0);
+  sources.id[0] = (unsigned char)keep;
+  for (u32 k = 0; k < K; k++) sources.id[k + 1] = (unsigned char)(c->nq + k);
+  if ((rc = launch_ntt(c, true, acc, (u64)next * N, acc, (u64)next * N, B * 2, keep, K + 1, sources, 0, 0, st))) return rc;
+  {
+    ProfScope ps(c, PK_MODDOWN, st);
+    launch_wide(drop_wide_args(c, lt, acc, tq, nlimbs), 1, B * 2, st);
+    HIP_TRY(hipGetLastError());
+  }
+  if ((rc = launch_ntt(c, false, tq, (u64)keep * N, tq, (u64)keep * N, B * 2, 0, keep, identity_map(keep), 0, 0, st))) return rc;
   FinalArgs a{acc, tq, out, c->d_mods, lt->dm_pinv, c->logN, keep, next, 0};
   ProfScope ps(c, PK_FINAL, st);
   hipLaunchKernelGGL(ks_final_kernel, dim3(N / 256, keep, B * 2), dim3(256), 0, st, a);
@@ -112,6 +89,20 @@ struct Decoder {
     for (u32 i = 1; i < n1; i++) baby.push_back(rotation_element(c, (u64)i * stride % slots));
     for (u32 i = 1; i < n2; i++) giant.push_back(rotation_element(c, (u64)i * n1 % slots * stride % slots));
   }
+  // Whether a relinearisation that divides by the last prime too takes the fused kernels of a key switch; products for one go where it
+  // wants them (`more` of product_out).
+  bool fused() const { return two_pass(cc) && cc->tune[3] != 1; }
+  int product_out(ProductOut* o, u64* out, u32 n, u32 limbs, bool more) const {
+    int rc;
+    *o = ProductOut{out, nullptr, nullptr, 0, limbs};
+    if (!more || !fused()) return CKKS_OK;
+    const LevelTables* lt;
+    if ((rc = get_level(c, limbs, &lt))) return rc;
+    o->less = lt->rs_qinv;
+    o->last = (u64*)(ks + ks_layout(c, n, limbs).acc) + poly(limbs - 1);
+    o->last_stride = poly(lt->next);
+    return CKKS_OK;
+  }
   // Relin of products in three components (at `limbs` limbs); more: dividing by the last prime too.
   int relin(u64* out, const u64* in, u32 n, u32 limbs, bool more) {
     int rc;
@@ -119,6 +110,13 @@ struct Decoder {
     const LevelTables* lt;
     if ((rc = get_level(c, limbs, &lt))) return rc;
     const u64 pl = poly(limbs);
+    if (fused()) {
+      KsIo io{in + 2 * pl, 3 * pl, 0, out, {1, 1}, nullptr, 0};
+      io.add2 = in;
+      io.add2_three = true;
+      io.drop = true;
+      return keyswitch_impl(c, io, n, limbs, mult_key, ks, st);
+    }
     const KsLayout L = ks_layout(c, n, limbs);
     if ((rc = ext_digits(c, lt, false, in + 2 * pl, 3 * pl, n, limbs, ks, st))) return rc;
     u64* acc = (u64*)(ks + L.acc);
@@ -155,11 +153,12 @@ struct Decoder {
     out = y[at];
     return CKKS_OK;
   }
-  int products(ProductArgs a, u32 n, u32 limbs, u64* out) {
-    a.out = out;
+  // to d, for relin() of n ciphertexts (2 n with `second`)
+  int products(ProductArgs a, u32 n, u32 limbs, bool more) {
+    int rc;
+    if ((rc = product_out(&a.o, d, a.second ? 2 * n : n, limbs, more))) return rc;
     a.mods = c->d_mods;
     a.logN = c->logN;
-    a.nlimbs = limbs;
     a.fp_on = (u32)fp_on();
     ProfScope ps(c, PK_CT_PRODUCTS, st);
     hipLaunchKernelGGL(ct_products_kernel, dim3(c->N / 512, limbs, n), dim3(256), 0, st, a);
@@ -222,10 +221,10 @@ struct PagedAttn : Decoder {
       PairArgs a;
       a.q = cts(q, nlimbs);
       a.key_comp = poly(k_limbs);
-      a.out = d + i * 3 * poly(nlimbs);
+      if ((rc = product_out(&a.o, d + i * 3 * poly(nlimbs), n, nlimbs, n1 == 1 && n2 == 1))) return rc;
+      a.o.last += 2 * i * a.o.last_stride;
       a.mods = c->d_mods;
       a.logN = c->logN;
-      a.nlimbs = nlimbs;
       a.fp_on = (u32)fp_on();
       for (u32 k = 0; k < cnt; k++) a.row[k] = pairs[i + k].row, a.key[k] = pairs[i + k].k;
       ProfScope ps(c, PK_PAIR_PRODUCTS, st);
@@ -241,7 +240,7 @@ struct PagedAttn : Decoder {
       a.x = a.y = cts(u, limbs);
       a.factor = 1;
       a.bias = add;
-      if ((rc = products(a, n, limbs, d))) return rc;
+      if ((rc = products(a, n, limbs, true))) return rc;
       if ((rc = relin(u, d, n, limbs, true))) return rc;
       add = 0;
       limbs--;
@@ -343,7 +342,7 @@ struct RmsNorm : Decoder {
     ProductArgs a{};
     a.x = a.y = cts(in, nlimbs);
     a.factor = square;
-    if ((rc = products(a, n, nlimbs, d))) return rc;
+    if ((rc = products(a, n, nlimbs, n1 == 1 && n2 == 1))) return rc;
     u64* mean;
     if ((rc = slot_sum(mean, n))) return rc;
     u32 limbs = nlimbs - 1;
@@ -357,10 +356,10 @@ struct RmsNorm : Decoder {
     for (u32 k = 0; k < iterations; k++) {
       ProductArgs p{};
       p.x = cts(mean, nlimbs - 1);
-      p.y = p.x2 = p.y2 = cts(v, limbs);
+      p.y = p.x2 = cts(v, limbs);
       p.factor = 1;
       p.second = n;
-      if ((rc = products(p, 2 * n, limbs, d))) return rc;
+      if ((rc = products(p, n, limbs, true))) return rc;
       if ((rc = relin(uw, d, 2 * n, limbs, true))) return rc;
       ProductArgs s{};
       s.x = cts(uw, limbs - 1);
@@ -368,7 +367,7 @@ struct RmsNorm : Decoder {
       s.factor = -1;
       s.z = cts(v, limbs);
       s.z_factor = factors[k];
-      if ((rc = products(s, n, limbs - 1, d))) return rc;
+      if ((rc = products(s, n, limbs - 1, true))) return rc;
       if ((rc = relin(v, d, n, limbs - 1, true))) return rc;
       limbs -= 2;
     }
@@ -386,7 +385,7 @@ struct RmsNorm : Decoder {
       if ((rc = ckks_rescale(c, (uint64_t*)g, (const uint64_t*)g_in, n, limbs + 1, rs, rs_bytes, st))) return rc;
       e.x = cts(g, limbs);
     }
-    if ((rc = products(e, n, limbs, d))) return rc;
+    if ((rc = products(e, n, limbs, false))) return rc;
     return relin(out, d, n, limbs, false);
   }
 };

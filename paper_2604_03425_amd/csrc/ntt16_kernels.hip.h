@@ -449,6 +449,7 @@ struct FwdInnerArgs {
   const u64* fin_add_src = nullptr;
   const ulonglong2* fin_pinv = nullptr;
   u32 fin_mode0 = 0, fin_mode1 = 0, fin_galois = 0, fin_add2_three = 0;
+  u32 fin_limbs = 0;   // limbs of fin_tq and fin_out: nlimbs, or one less where the last limb is divided away with the special ones
   // the same kernels: != null switches the product of the second components of two ciphertexts ([B][2][nlimbs][N] each; d is
   // not read) and adds the other two terms of the product to the result (fin_mode0 == fin_mode1 == 4)
   const u64 *prod_a = nullptr, *prod_b = nullptr;
@@ -528,7 +529,7 @@ __device__ __forceinline__ void fwd_inner_c_body_fp(const FwdInnerArgs& a, u32 b
   const u32 beta = a.beta;
   const u32 jo = t < a.nlimbs ? t / a.alpha : 0xFFFFFFFFu;   // the digit that holds limb t itself (none for special slots)
   auto ext_limb = [&](u32 j) { return a.ext + (((size_t)b * beta + j) * a.next + t) * N; };
-  const u64* tq_limb = a.fin_tq ? a.fin_tq + ((size_t)bc * a.nlimbs + t) * N : nullptr;
+  const u64* tq_limb = a.fin_tq ? a.fin_tq + ((size_t)bc * a.fin_limbs + t) * N : nullptr;
   double acc[16], x[16];
   u64 e[16];
 #pragma unroll
@@ -678,7 +679,7 @@ __device__ __forceinline__ void fwd_inner_c_body_fp(const FwdInnerArgs& a, u32 b
       }
     });
     const double2 pv = ((const double2*)a.fin_pinv)[t];
-    u64* o = a.fin_out + ((size_t)bc * a.nlimbs + t) * N + lane_pos();
+    u64* o = a.fin_out + ((size_t)bc * a.fin_limbs + t) * N + lane_pos();
     const u32 pos = lane_pos();
     if (mode == 4) {   // d0 = a0 b0, d1 = a0 b1 + a1 b0; e holds a0
       const size_t c0 = ((size_t)b * 2 * a.nlimbs + t) * N + pos, c1 = c0 + (size_t)a.nlimbs * N;
@@ -830,7 +831,7 @@ ntt16_fwd_blocks_inner8_kernel(FwdInnerArgs a) {
   const u32 jo = t < a.nlimbs ? t / a.alpha : 0xFFFFFFFFu;   // the digit that holds limb t itself (none for special slots)
   auto ext_limb = [&](u32 j) { return a.ext + (((size_t)b * beta + j) * a.next + t) * N; };
   u32 jn = jo == 0 ? 1u : 0u;   // next converted digit
-  auto tq_limb = [&](u32 c) { return a.fin_tq + (((size_t)b * 2 + c) * a.nlimbs + t) * N; };
+  auto tq_limb = [&](u32 c) { return a.fin_tq + (((size_t)b * 2 + c) * a.fin_limbs + t) * N; };
   auto prod_limb = [&](const u64* p, u32 c) { return p + (((size_t)b * 2 + c) * a.nlimbs + t) * N + posC; };
   const u64 r2 = MORE != KS_PLAIN || (FIN && a.prod_a) ? mont_r2(mi) : 0;
   if (jn < beta) request(ext_limb(jn));
@@ -965,7 +966,7 @@ ntt16_fwd_blocks_inner8_kernel(FwdInnerArgs a) {
           if (mode == 3) x[k] = addmod(x[k], as[galois_src_index(posC + k, gf, a.logN)], q);
         }
       }
-      u64* o = a.fin_out + (((size_t)b * 2 + c) * a.nlimbs + t) * N + posC;
+      u64* o = a.fin_out + (((size_t)b * 2 + c) * a.fin_limbs + t) * N + posC;
 #pragma unroll
       for (int k = 0; k < 4; k++) *(inner8_pair*)(o + 2 * k) = inner8_pair{x[2 * k], x[2 * k + 1]};
     };
