@@ -245,6 +245,235 @@ __global__ void __launch_bounds__(256) rot_sum_kernel(RotSumArgs a) {
   else rot_sum_int<CB, KIND == 2>(a, what, blk, zi);
 }
 
+// The unweighted sum of rotations of one decomposition (all terms have the same ext, d, c0) whose Galois maps keep every aligned block of
+// 256 positions: g = 1 mod 2N / 256, which all rotations by multiples of the stride are where a head of at most 256 components fills the
+// slots. A workgroup takes such a block of CB ciphertexts, puts a digit into LDS once and reads it there for every rotation; a lane owns a
+// position and shares the key words among its ciphertexts.
+// Doubles: digits within q / 2, key words below q < 2^50, so that four products stay within 2^101 of H = 1.5 * 2^102, in whose binade
+// sums are multiples of 2^50 and what a product loses in joining H is exact and goes to L: 4 instructions a term, 6 every fourth.
+#define BLOCK_SUM 256
+template <int CB>
+__device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 blk, u32 zi, u64* sm) {
+  constexpr double M = 1.5 * 5070602400912917605986812821504.0;   // 1.5 * 2^102
+  const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, comp = (size_t)a.nm * N;
+  const u32 tid = threadIdx.x, n = blk * BLOCK_SUM + tid, t = a.slots[zi], b0 = what * CB;
+  const bool main_prime = t < a.nlimbs;
+  const u32 id = main_prime ? t : t - a.nlimbs + a.nq;
+  const ModInfo mi = a.mods[id];
+  const double q = mi.qd, qinv = mi.qinv;
+  const u64 *ext = a.term[0].ext + (size_t)t * N + n, *d = a.term[0].d + (size_t)t * N + n;
+  const u32 jo = main_prime ? t / a.alpha : 0xFFFFFFFFu;   // the digit that holds limb t itself
+  u32 bb[CB];   // surplus places repeat the last ciphertext and store nothing
+  double H0[CB], L0[CB], H1[CB], L1[CB];
+#pragma unroll
+  for (int k = 0; k < CB; k++) {
+    bb[k] = min(b0 + k, a.B - 1);
+    H0[k] = H1[k] = M;
+    L0[k] = L1[k] = 0.0;
+  }
+  auto settle = [&](double& H, double& L) {
+    const double h = H - M;
+    L = __builtin_fma(-__builtin_rint(__builtin_fma(L, qinv, h * qinv)), q, h) + L;   // at most 1.3 q
+    H = M;
+  };
+  double* tile = (double*)sm;
+  u64 ahead[CB];
+  auto request = [&](u32 j) {
+#pragma unroll
+    for (int k = 0; k < CB; k++)
+      ahead[k] = j == jo ? d[(size_t)bb[k] * a.d_stride] : ext[((size_t)bb[k] * a.beta + j) * a.next * N];
+  };
+  const u32 R = a.nterms;
+  request(0);
+  u64 k0, k1;
+  {
+    const u64* e = a.term[0].evk + (size_t)id * N + n;
+    k0 = e[0], k1 = e[comp];
+  }
+  u32 count = 0;
+  for (u32 j = 0; j < a.beta; j++) {
+    const u64 bias = j == jo ? 0x4330000000000000ull : 0ull;   // residues become doubles, doubles stay what they are
+    const double less = __longlong_as_double((long long)bias);
+#pragma unroll
+    for (int k = 0; k < CB; k++) {
+      const double v = __longlong_as_double((long long)(ahead[k] | bias)) - less;
+      tile[k * BLOCK_SUM + tid] = j == jo ? fp_reduce(v, qinv, q) : v;
+    }
+    lds_barrier();   // the other tile's readers are past it, since they have written this one
+    if (j + 1 < a.beta) request(j + 1);
+    for (u32 r = 0; r < R; r++) {
+      const double e0 = u2d(k0), e1 = u2d(k1);
+      const u32 rn = r + 1 < R ? r + 1 : 0, jn = min(r + 1 < R ? j : j + 1, a.beta - 1);
+      const u64* e = a.term[rn].evk + (size_t)jn * 2 * comp + (size_t)id * N + n;
+      k0 = e[0], k1 = e[comp];
+      const u32 m = galois_src_index(n, a.term[r].galois, a.logN) & (BLOCK_SUM - 1);
+#pragma unroll
+      for (int k = 0; k < CB; k++) {
+        const double x = tile[k * BLOCK_SUM + m];
+        const double p0 = __builtin_fma(x, e0, H0[k]), h0 = p0 - H0[k];
+        L0[k] += __builtin_fma(x, e0, -h0);
+        H0[k] = p0;
+        const double p1 = __builtin_fma(x, e1, H1[k]), h1 = p1 - H1[k];
+        L1[k] += __builtin_fma(x, e1, -h1);
+        H1[k] = p1;
+      }
+      if ((++count & 3) == 0) {
+#pragma unroll
+        for (int k = 0; k < CB; k++) settle(H0[k], L0[k]), settle(H1[k], L1[k]);
+      }
+    }
+    tile = (double*)sm + (tile == (double*)sm ? CB * BLOCK_SUM : 0);
+  }
+  if (main_prime) {   // P (base + sum of the rotated first components), P base
+    const u64* c0 = a.term[0].c0 + (size_t)t * N + n;
+    double v[CB];
+#pragma unroll
+    for (int k = 0; k < CB; k++) tile[k * BLOCK_SUM + tid] = u2d(c0[(size_t)bb[k] * a.d_stride]), v[k] = 0.0;
+    lds_barrier();
+    for (u32 r = 0; r < R; r++) {
+      const u32 m = galois_src_index(n, a.term[r].galois, a.logN) & (BLOCK_SUM - 1);
+#pragma unroll
+      for (int k = 0; k < CB; k++) v[k] += tile[k * BLOCK_SUM + m];
+      if ((r & 3) == 3) {
+#pragma unroll
+        for (int k = 0; k < CB; k++) v[k] = fp_reduce(v[k], qinv, q);
+      }
+    }
+    const double pm = u2d(mi.pmod);
+#pragma unroll
+    for (int k = 0; k < CB; k++) {
+      settle(H0[k], L0[k]);
+      settle(H1[k], L1[k]);
+      if (a.base) {
+        const u64* x = a.base + (size_t)bb[k] * a.base_stride + (size_t)t * N + n;
+        v[k] += u2d(x[0]);
+        L1[k] += fp_mulmod_var(u2d(x[pl]), pm, qinv, q);
+      }
+      L0[k] += fp_mulmod_var(fp_reduce(v[k], qinv, q), pm, qinv, q);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < CB; k++) {
+    if (b0 + k >= a.B) break;
+    settle(H0[k], L0[k]);
+    settle(H1[k], L1[k]);
+    u64* to = a.acc + ((size_t)bb[k] * 2 * a.next + t) * N + n;
+    if (a.accumulate) L0[k] += u2d(to[0]), L1[k] += u2d(to[(size_t)a.next * N]);
+    to[0] = d2u_canon(fp_reduce(L0[k], qinv, q), q);
+    to[(size_t)a.next * N] = d2u_canon(fp_reduce(L1[k], qinv, q), q);
+  }
+}
+// Integer moduli (PLAIN: all of them, acc without the factor 2^-64): 30-bit halves, 4 multiply-adds a term and carries every 11.
+template <int CB, bool PLAIN>
+__device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32 blk, u32 zi, u64* tile) {
+  const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, comp = (size_t)a.nm * N;
+  const u32 tid = threadIdx.x, n = blk * BLOCK_SUM + tid, t = a.slots[zi], b0 = what * CB;
+  const bool main_prime = t < a.nlimbs;
+  const u32 id = main_prime ? t : t - a.nlimbs + a.nq;
+  const ModInfo mi = a.mods[id];
+  const u64 q = mi.m, nm = neg_opaque(q);
+  const u64 *ext = a.term[0].ext + (size_t)t * N + n, *d = a.term[0].d + (size_t)t * N + n;
+  const u32 jo = main_prime ? t / a.alpha : 0xFFFFFFFFu;
+  u64* const sm = tile;
+  u32 bb[CB];
+  Dot30 s0[CB], s1[CB];
+#pragma unroll
+  for (int k = 0; k < CB; k++) {
+    bb[k] = min(b0 + k, a.B - 1);
+    dot30_init(s0[k]);
+    dot30_init(s1[k]);
+  }
+  u64 ahead[CB];
+  auto request = [&](u32 j) {
+#pragma unroll
+    for (int k = 0; k < CB; k++)
+      ahead[k] = j == jo ? d[(size_t)bb[k] * a.d_stride] : ext[((size_t)bb[k] * a.beta + j) * a.next * N];
+  };
+  const u32 R = a.nterms;
+  request(0);
+  u64 k0, k1;
+  {
+    const u64* e = a.term[0].evk + (size_t)id * N + n;
+    k0 = e[0], k1 = e[comp];
+  }
+  u32 count = 0;
+  auto carry = [&] {
+    if (++count < 11) return;
+    count = 0;
+#pragma unroll
+    for (int k = 0; k < CB; k++) dot30_settle(s0[k], mi.mu64, nm), dot30_settle(s1[k], mi.mu64, nm);
+  };
+  for (u32 j = 0; j < a.beta; j++) {
+#pragma unroll
+    for (int k = 0; k < CB; k++) tile[k * BLOCK_SUM + tid] = ahead[k];
+    lds_barrier();
+    if (j + 1 < a.beta) request(j + 1);
+    for (u32 r = 0; r < R; r++) {
+      const u32 e00 = (u32)k0 & M30, e01 = (u32)(k0 >> 30), e10 = (u32)k1 & M30, e11 = (u32)(k1 >> 30);
+      const u32 rn = r + 1 < R ? r + 1 : 0, jn = min(r + 1 < R ? j : j + 1, a.beta - 1);
+      const u64* e = a.term[rn].evk + (size_t)jn * 2 * comp + (size_t)id * N + n;
+      k0 = e[0], k1 = e[comp];
+      const u32 m = galois_src_index(n, a.term[r].galois, a.logN) & (BLOCK_SUM - 1);
+#pragma unroll
+      for (int k = 0; k < CB; k++) {
+        const u64 x = tile[k * BLOCK_SUM + m];
+        const u32 x0 = (u32)x & M30, x1 = (u32)(x >> 30);
+        dot30_mac(s0[k], x0, x1, e00, e01);
+        dot30_mac(s1[k], x0, x1, e10, e11);
+      }
+      carry();
+    }
+    tile = sm + (tile == sm ? CB * BLOCK_SUM : 0);
+  }
+  if (main_prime) {
+    const u64* c0 = a.term[0].c0 + (size_t)t * N + n;
+    const u32 p0 = (u32)mi.pmod & M30, p1 = (u32)(mi.pmod >> 30);
+#pragma unroll
+    for (int k = 0; k < CB; k++) tile[k * BLOCK_SUM + tid] = c0[(size_t)bb[k] * a.d_stride];
+    lds_barrier();
+    for (u32 r = 0; r < R; r++) {
+      const u32 m = galois_src_index(n, a.term[r].galois, a.logN) & (BLOCK_SUM - 1);
+#pragma unroll
+      for (int k = 0; k < CB; k++) {
+        const u64 x = tile[k * BLOCK_SUM + m];
+        dot30_mac(s0[k], (u32)x & M30, (u32)(x >> 30), p0, p1);
+      }
+      carry();
+    }
+    if (a.base) {
+#pragma unroll
+      for (int k = 0; k < CB; k++) {
+        const u64* x = a.base + (size_t)bb[k] * a.base_stride + (size_t)t * N + n;
+        dot30_mac(s0[k], (u32)x[0] & M30, (u32)(x[0] >> 30), p0, p1);
+        dot30_mac(s1[k], (u32)x[pl] & M30, (u32)(x[pl] >> 30), p0, p1);
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < CB; k++) {
+    if (b0 + k >= a.B) break;
+    u64* to = a.acc + ((size_t)bb[k] * 2 * a.next + t) * N + n;
+#pragma unroll
+    for (int c = 0; c < 2; c++) {
+      Dot30& s = c ? s1[k] : s0[k];
+      dot30_settle(s, mi.mu64, nm);
+      u64 v = PLAIN ? reduce128(dot30_value(s), mi) : csub(csub(redc(dot30_value(s), q, mi.minv), q), q);
+      u64* o = to + (size_t)c * a.next * N;
+      if (a.accumulate) v = addmod(v, *o, q);
+      *o = v;
+    }
+  }
+}
+// Kinds as for rot_sum_kernel. grid = (ceil(B / CB), N / 256, slots)
+template <int KIND, int CB>
+__global__ void __launch_bounds__(BLOCK_SUM) block_sum_kernel(RotSumArgs a) {
+  __shared__ u64 sm[2 * CB * BLOCK_SUM];
+  u32 what, blk, zi;
+  attention_map(what, blk, zi);
+  if (KIND == 0 && zi < a.nfp) block_sum_fp<CB>(a, what, blk, zi, sm);
+  else block_sum_int<CB, KIND == 2>(a, what, blk, zi, sm);
+}
+
 // out[i][j][b] = sum_{s < ns} x(j, s)[b] * y(i, s)[b] in three components (+ add in the first two, or in all three), for i0 <= i < i1 and
 // j0 <= j < j1. Products of moduli below 2^60 are kept as 128-bit sums, of those below 2^50 in doubles.
 struct ProdSumArgs {

@@ -124,7 +124,20 @@ void launch_rot_sum_of(u32 outs, u32 slots, const RotSumArgs& a, hipStream_t st)
   if (a.B > 1) hipLaunchKernelGGL((rot_sum_kernel<KIND, 2>), dim3(outs * ((a.B + 1) / 2), (1u << a.logN) / 256, slots), block, 0, st, a);
   else hipLaunchKernelGGL((rot_sum_kernel<KIND, 1>), dim3(outs, (1u << a.logN) / 256, slots), block, 0, st, a);
 }
-int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 outs = 1) {
+template <int CB>
+void launch_block_sum_of(u32 slots, const RotSumArgs& a, hipStream_t st) {
+  const dim3 grid((a.B + CB - 1) / CB, (1u << a.logN) / BLOCK_SUM, slots), block(BLOCK_SUM);
+  if (!a.doubles) hipLaunchKernelGGL((block_sum_kernel<2, CB>), grid, block, 0, st, a);
+  else if (a.nfp == 0) hipLaunchKernelGGL((block_sum_kernel<1, CB>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((block_sum_kernel<0, CB>), grid, block, 0, st, a);
+}
+// Whether all rotations keep the blocks that block_sum_kernel holds.
+bool rotations_near(const ckks_ctx* c, const u32* galois, u32 R) {
+  for (u32 r = 0; r < R; r++)
+    if (galois[r] % (2 * c->N / BLOCK_SUM) != 1) return false;
+  return R != 0;
+}
+int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 outs = 1, bool near = false) {
   a.B = B;
   const LimbMap emap = ext_map(c, a.nlimbs);
   u32 cnt = 0;
@@ -134,7 +147,15 @@ int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 
     if (fp) a.nfp = cnt;
   }
   ProfScope ps(c, PK_ROT_SUM, st);
-  if (!a.doubles) launch_rot_sum_of<2>(outs, cnt, a, st);
+  if (near) {
+    const u32 groups = (B + 3) / 4;
+    switch ((B + groups - 1) / groups) {   // ciphertexts a lane, as even as possible
+      case 1: launch_block_sum_of<1>(cnt, a, st); break;
+      case 2: launch_block_sum_of<2>(cnt, a, st); break;
+      case 3: launch_block_sum_of<3>(cnt, a, st); break;
+      default: launch_block_sum_of<4>(cnt, a, st); break;
+    }
+  } else if (!a.doubles) launch_rot_sum_of<2>(outs, cnt, a, st);
   else if (a.nfp == 0) launch_rot_sum_of<1>(outs, cnt, a, st);
   else launch_rot_sum_of<0>(outs, cnt, a, st);
   HIP_TRY(hipGetLastError());
@@ -154,11 +175,12 @@ int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* 
   a.w = w;
   a.w_terms = R + 1;
   a.per_set = per_set;
+  const bool near = !w && rotations_near(c, galois, R);
   for (u32 r0 = 0; r0 == 0 || r0 < R; r0 += ROT_SUM_TERMS) {
     a.nterms = std::min<u32>(ROT_SUM_TERMS, R - r0);
     a.w_first = r0;
     for (u32 r = 0; r < a.nterms; r++) a.term[r] = RotTerm{ext, ct + pl, ct, evks[r0 + r], galois[r0 + r]};
-    if ((rc = launch_rot_sum(c, a, B, st))) return rc;
+    if ((rc = launch_rot_sum(c, a, B, st, 1, near))) return rc;
     a.base = nullptr;
     a.accumulate = 1;
   }
