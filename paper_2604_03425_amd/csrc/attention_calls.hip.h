@@ -31,10 +31,12 @@ u32 rotation_element(const ckks_ctx* c, u64 steps) {   // 5^steps mod 2N
 // in 3 digits 1012 and 880.
 // Digits of B polynomials in the extended basis, evaluation domain, at L.ext of the key-switch workspace: (b, limb t) is at
 // d + b * d_stride + t * N. Doubles on the double-precision moduli of the two-pass rings and of whole limbs, canonical residues elsewhere.
-int ext_digits(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* d, u64 d_stride, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
+// last_int (two-pass rings): limb nlimbs - 1 in residues whatever its class.
+int ext_digits(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* d, u64 d_stride, u32 B, u32 nlimbs, char* ws, hipStream_t st,
+               bool last_int = false) {
   int rc;
   FwdInnerArgs unused;
-  if (two_pass(c)) return hoist_front16(c, lt, d, d_stride, B, nlimbs, ws, st, unused);
+  if (two_pass(c)) return hoist_front16(c, lt, d, d_stride, B, nlimbs, ws, st, unused, last_int);
   if (whole) {
     Ks12Args a = ks12_args(c, lt, B, nlimbs, ws);
     a.d = d;
@@ -137,13 +139,13 @@ bool rotations_near(const ckks_ctx* c, const u32* galois, u32 R) {
     if (galois[r] % (2 * c->N / BLOCK_SUM) != 1) return false;
   return R != 0;
 }
-int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 outs = 1, bool near = false) {
+int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 outs = 1, bool near = false, bool last_int = false) {
   a.B = B;
   const LimbMap emap = ext_map(c, a.nlimbs);
   u32 cnt = 0;
   for (int fp = 1; fp >= 0; fp--) {   // double-precision slots first
     for (u32 s = 0; s < a.next; s++)
-      if ((a.doubles && host_class(c, c->mod[emap.id[s]]) == 0) == (fp == 1)) a.slots[cnt++] = (unsigned char)s;
+      if ((a.doubles && host_class(c, c->mod[emap.id[s]]) == 0 && !(last_int && s + 1 == a.nlimbs)) == (fp == 1)) a.slots[cnt++] = (unsigned char)s;
     if (fp) a.nfp = cnt;
   }
   ProfScope ps(c, PK_ROT_SUM, st);
@@ -164,10 +166,10 @@ int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 
 
 // acc = P w_0 ct + sum_r w_{r+1} (accumulators of the rotation of ct by galois[r]); ws: a key-switch workspace for B.
 int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* ct, u32 B, u32 nlimbs, const u32* galois,
-                     const u64* const* evks, u32 R, const u64* w, u32 per_set, u64* acc, char* ws, hipStream_t st) {
+                     const u64* const* evks, u32 R, const u64* w, u32 per_set, u64* acc, char* ws, hipStream_t st, bool last_int = false) {
   int rc;
   const u64 pl = (u64)nlimbs * c->N;
-  if (R && (rc = ext_digits(c, lt, whole, ct + pl, 2 * pl, B, nlimbs, ws, st))) return rc;
+  if (R && (rc = ext_digits(c, lt, whole, ct + pl, 2 * pl, B, nlimbs, ws, st, last_int))) return rc;
   const u64* ext = (const u64*)(ws + ks_layout(c, B, nlimbs).ext);
   RotSumArgs a = rot_sum_args(c, lt, whole, nlimbs, acc, 2 * pl);
   a.base = ct;
@@ -180,7 +182,7 @@ int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* 
     a.nterms = std::min<u32>(ROT_SUM_TERMS, R - r0);
     a.w_first = r0;
     for (u32 r = 0; r < a.nterms; r++) a.term[r] = RotTerm{ext, ct + pl, ct, evks[r0 + r], galois[r0 + r]};
-    if ((rc = launch_rot_sum(c, a, B, st, 1, near))) return rc;
+    if ((rc = launch_rot_sum(c, a, B, st, 1, near, last_int))) return rc;
     a.base = nullptr;
     a.accumulate = 1;
   }

@@ -137,6 +137,7 @@ struct LevelTables {
   uint4* dm_pieces = nullptr;      // [nlimbs-1] matrices of bytes of (D/c_i) mod q_t, for conv_wide_kernel (scaled like dn_pieces)
   ulonglong2* dm_inv = nullptr;    // [K+1]  (D/c_i)^-1 mod c_i, Shoup pairs
   ulonglong2* dm_scale = nullptr;  // [K+1]  the same / N (two-pass rings: in the form of the class, integer ones times 2^64)
+  ulonglong2* dm_iscale = nullptr; // [K+1]  the same, all in integer form
   ulonglong2* dm_pinv = nullptr;   // [nlimbs-1]  D^-1 mod q_t, Shoup pairs
   ulonglong2* dm_pinv2 = nullptr;  // [nlimbs-1]  the same in the form of pinv2
 };
@@ -471,14 +472,15 @@ LevelTables build_level(const ckks_ctx* c, u32 nlimbs, LevelArena& arena) {
         if (k != i) v = h_mul(v, src[k] % m, m);
       return v;
     };
-    std::vector<ulonglong2> dm_inv(n), dm_scale(n), dm_pinv(keep), dm_pinv2(keep);
+    std::vector<ulonglong2> dm_inv(n), dm_scale(n), dm_iscale(n), dm_pinv(keep), dm_pinv2(keep);
     const bool rows_fit = n <= CONV_MAX_SRC && c->logN >= 13 && c->logN <= 16 &&
                           std::all_of(c->mod.begin(), c->mod.end(), [&](u64 m) { return is_fp(m) || h_bits(m) > CONV_INT_MIN_BITS; });
     std::vector<unsigned char> dm_pieces(pieces_bytes(1, keep, groups, true), 0), dm_rows(rows_fit ? pieces_bytes(1, keep, groups, false) : 0, 0);
     for (u32 i = 0; i < n; i++) {
       const u64 m = src[i], inv = h_inv(others(i, m), m), v = h_mul(inv, h_inv(c->N % m, m), m), w = h_mont(v, m);
       dm_inv[i] = ulonglong2{inv, h_shoup(inv, m)};
-      dm_scale[i] = is_fp(m) ? as_fp(v, m) : ulonglong2{w, h_shoup(w, m)};
+      dm_iscale[i] = ulonglong2{w, h_shoup(w, m)};
+      dm_scale[i] = is_fp(m) ? as_fp(v, m) : dm_iscale[i];
     }
     for (u32 t_ = 0; t_ < keep; t_++) {
       const u64 m = c->mod[t_], inv = h_inv(others(n, m), m), w = h_mont(inv, m);
@@ -494,6 +496,7 @@ LevelTables build_level(const ckks_ctx* c, u32 nlimbs, LevelArena& arena) {
     if (rows_fit) t.dm_rows = (uint4*)arena.add(dm_rows);
     t.dm_inv = arena.add(dm_inv);
     t.dm_scale = arena.add(dm_scale);
+    t.dm_iscale = arena.add(dm_iscale);
     t.dm_pinv = arena.add(dm_pinv);
     t.dm_pinv2 = arena.add(dm_pinv2);
   }
@@ -560,7 +563,7 @@ int build_levels(ckks_ctx* c) {
     if (nl > 1 && c->np) {
       rebase(t.dm_pieces);
       if (t.dm_rows) rebase(t.dm_rows);
-      rebase(t.dm_inv); rebase(t.dm_scale); rebase(t.dm_pinv); rebase(t.dm_pinv2);
+      rebase(t.dm_inv); rebase(t.dm_scale); rebase(t.dm_iscale); rebase(t.dm_pinv); rebase(t.dm_pinv2);
     }
   }
   if (c->d_levels) {
@@ -690,10 +693,11 @@ struct NttOpts {
   bool raw_out = false;               // with blocks_only: leave reduced doubles on double-precision moduli
   int only_class = -1;                // >= 0: touch only the slots of this modulus class
   int exclude_class = -1;             // >= 0: leave the slots of this modulus class alone
+  int int_id = -1;                    // >= 0: two-pass only, this modulus id has integer bodies (class 2) here
   // a whole transform of all slots, canonical residues in and out
   bool plain() const {
     return !galois && !src_b && !galois_pc && !scale && !split_out && !rows_only && !blocks_only && !raw_out && only_class < 0 &&
-           exclude_class < 0;
+           exclude_class < 0 && int_id < 0;
   }
 };
 // Whether a whole transform holds a limb per workgroup (ntt_limb.hip.h): always up to 2^13. A limb of 2^14 takes a compute unit's
@@ -796,6 +800,7 @@ int launch_ntt(const ckks_ctx* c, bool inverse, const u64* src, u64 src_stride, 
     b.src_poly_stride = dst_stride;
     auto cls_of = [&](u32 s) {
       int k = host_class(c, c->mod[ids_from_slot0.id[s]]);
+      if (ids_from_slot0.id[s] == opt.int_id) k = 2;
       if (opt.only_class >= 0 && k != opt.only_class) return -1;
       if (opt.exclude_class >= 0 && k == opt.exclude_class) return -1;
       return k;
@@ -1103,9 +1108,10 @@ u32 conv_shares(u64 groups, u32 wsrc, u32 wtargets, u32 targets) {
   }
   return at;
 }
-// job.a: everything but the tables of the ring, the target lists and nsplit; target_id(slot) = modulus id of a target slot.
+// job.a: everything but the tables of the ring, the target lists and nsplit; target_id(slot) = modulus id of a target slot. int_slot: a
+// double-precision target slot that is to be an integer one (ConvArgs::last_int); int_sources: sources come as integers of any kind.
 template <class TargetId>
-void conv_plan(const ckks_ctx* c, ConvJob& job, TargetId target_id) {
+void conv_plan(const ckks_ctx* c, ConvJob& job, TargetId target_id, u32 int_slot = ~0u, bool int_sources = false) {
   ConvArgs& a = job.a;
   a.tw = c->d_tw_fwd;
   a.twi = c->d_tw_inv;
@@ -1117,16 +1123,17 @@ void conv_plan(const ckks_ctx* c, ConvJob& job, TargetId target_id) {
   for (int fp = 1; fp >= 0; fp--)
     for (u32 s = 0; s < a.ntarget; s++) {
       const u32 id = target_id(s);
-      if ((host_class(c, c->mod[id]) == 0) != (fp == 1)) continue;
+      if ((host_class(c, c->mod[id]) == 0 && s != int_slot) != (fp == 1)) continue;
       const u32 n = a.nfp + a.nint;
       a.target[n] = s | id << 8;
       if (fp) a.nfp++;
       else a.nint++;
     }
   a.first_id = a.src_id0;
-  job.fp = host_class(c, c->mod[a.src_id0]) == 0;
+  a.last_int = int_slot != ~0u;
+  job.fp = !int_sources && host_class(c, c->mod[a.src_id0]) == 0;
   const u32 len = std::min(a.alpha, a.src_nlimbs), own = a.skip_own ? len : 0;   // own limbs: of the sources' kind, not converted
-  const u32 targets = a.nfp + a.nint - own, wtargets = (a.nfp - (job.fp ? own : 0)) * 4 + (a.nint - (job.fp ? 0 : own)) * 7;
+  const u32 targets = a.nfp + a.nint - own, wtargets = (a.nfp - std::min(a.nfp, job.fp ? own : 0)) * 4 + (a.nint - std::min(a.nint, job.fp ? 0 : own)) * 7;
   const u64 groups = (u64)job.npoly * (c->N / CONV_TILE);
   // From 6 sources on, and where one share would take over a tenth longer than several (a quarter with double-precision sources,
   // whose inverse pass is cheaper), the sources' inverse row pass runs by itself before the shares instead of in each of them
@@ -1155,7 +1162,7 @@ int launch_conv_rows(const ckks_ctx* c, const ConvJob& job, hipStream_t st) {
 }
 // ModUp on the two-pass path, from the inverse block pass of the polynomial (in dcoef; its row pass too if the plan says ready)
 // to ext after the row pass.
-ConvJob conv_up_job(const ckks_ctx* c, const LevelTables* lt, const u64* dcoef, u64* ext, u32 B, u32 nlimbs) {
+ConvJob conv_up_job(const ckks_ctx* c, const LevelTables* lt, const u64* dcoef, u64* ext, u32 B, u32 nlimbs, bool last_int = false) {
   ConvJob job;
   ConvArgs& a = job.a;
   a.src = dcoef;
@@ -1172,7 +1179,7 @@ ConvJob conv_up_job(const ckks_ctx* c, const LevelTables* lt, const u64* dcoef, 
   a.direct = lt->up_direct;
   a.scale = lt->up_scale;
   job.npoly = B * lt->beta;
-  conv_plan(c, job, [&](u32 s) { return s < nlimbs ? s : s - nlimbs + c->nq; });
+  conv_plan(c, job, [&](u32 s) { return s < nlimbs ? s : s - nlimbs + c->nq; }, last_int ? nlimbs - 1 : ~0u);
   return job;
 }
 // ModDown: both accumulators' special limbs to tq.
@@ -1283,8 +1290,20 @@ int ks16_moddown_rows(ckks_ctx* c, const LevelTables* lt, u32 B, u32 nlimbs, u64
   return launch_bconv_rows(c, a, B * 2, lt->narrow_dn, [&](u32 s) { return host_class(c, c->mod[s]); }, st);
 }
 
-// The same where the last main limb is divided away with the special ones: it joins them as a source. Sources are of any kind, so they
-// all go through their inverse pass before the conversion, which takes residues.
+// Where the last main limb is divided away with the special ones, it is handled as one of them, with integer bodies (JOINED: it is of an
+// integer class, or becomes an integer target of the digits' conversion), if they are of integer classes and the fused conversion takes
+// one source more. Else (APART) it keeps its kind until its coefficients are known.
+enum DropForm { APART = 0, JOINED, JOINED_FORCED };
+DropForm drop_form(const ckks_ctx* c, const LevelTables* lt, u32 nlimbs) {
+  if (!two_pass(c) || !lt->dm_rows || c->tune[2] != 0) return APART;
+  for (u32 k = 0; k < c->np; k++)
+    if (host_class(c, c->mod[c->nq + k]) == 0) return APART;
+  const u64 q = c->mod[nlimbs - 1];
+  if (host_class(c, q) != 0) return JOINED;
+  return conv_fits(c, 0, nlimbs, c->alpha) && h_bits(q) > CONV_INT_MIN_BITS ? JOINED_FORCED : APART;
+}
+// ModDown's conversion and the first forward pass there: from accumulators (the integer ones after their inverse block pass with
+// int_blocks_done; the last main limb in the form of its class, APART, or of integers) to tq in row-pass form.
 int ks16_drop_rows(ckks_ctx* c, const LevelTables* lt, u32 B, u32 nlimbs, u64* acc, u64* tq, hipStream_t st, bool int_blocks_done) {
   int rc;
   const u32 N = c->N, next = lt->next, K = c->np, keep = nlimbs - 1;
@@ -1296,20 +1315,9 @@ int ks16_drop_rows(ckks_ctx* c, const LevelTables* lt, u32 B, u32 nlimbs, u64* a
   };
   NttOpts o;
   o.scale = lt->dm_scale;
-  if (int_blocks_done) {
-    NttOpts blocks = o, rows = o;
-    blocks.blocks_only = true;
-    if ((rc = inverse(keep, 1, sources, blocks))) return rc;
-    blocks.scale = lt->dm_scale + 1;
-    blocks.only_class = 0;
-    if ((rc = inverse(nlimbs, K, special, blocks))) return rc;
-    rows.rows_only = true;
-    if ((rc = inverse(keep, K + 1, sources, rows))) return rc;
-  } else if ((rc = inverse(keep, K + 1, sources, o))) {
-    return rc;
-  }
-  if (lt->dm_rows && c->tune[2] == 0) {
-    ConvJob job;
+  ConvJob job;
+  const bool conv = lt->dm_rows && c->tune[2] == 0;
+  if (conv) {
     ConvArgs& a = job.a;
     a.src = acc;
     a.dst = tq;
@@ -1322,13 +1330,36 @@ int ks16_drop_rows(ckks_ctx* c, const LevelTables* lt, u32 B, u32 nlimbs, u64* a
     a.skip_own = 0;
     a.ntarget = keep;
     a.pieces = lt->dm_rows;
-    a.scale = lt->dm_scale;
+    a.scale = lt->dm_iscale;
     job.npoly = B * 2;
-    conv_plan(c, job, [](u32 s) { return s; });
+    conv_plan(c, job, [](u32 s) { return s; }, ~0u, true);
     a.first_id = keep;
-    job.fp = false;
-    job.ready = true;
-    a.nsplit = conv_shares((u64)job.npoly * (N / CONV_TILE), K + 1, a.nfp * 4 + a.nint * 7, keep);
+  }
+  if (drop_form(c, lt, nlimbs) != APART) {
+    o.scale = lt->dm_iscale;
+    o.int_id = (int)keep;
+    NttOpts blocks = o, rows = o;
+    blocks.blocks_only = true;
+    rows.rows_only = true;
+    if (!int_blocks_done && (rc = inverse(keep, K + 1, sources, blocks))) return rc;
+    if (job.ready && (rc = inverse(keep, K + 1, sources, rows))) return rc;
+    return launch_conv_rows(c, job, st);
+  }
+  if (int_blocks_done) {
+    NttOpts blocks = o, rows = o;
+    blocks.blocks_only = true;
+    if ((rc = inverse(keep, 1, sources, blocks))) return rc;
+    blocks.scale = lt->dm_scale + 1;
+    blocks.only_class = 0;
+    if ((rc = inverse(nlimbs, K, special, blocks))) return rc;
+    rows.rows_only = true;
+    if ((rc = inverse(keep, K + 1, sources, rows))) return rc;
+  } else if ((rc = inverse(keep, K + 1, sources, o))) {
+    return rc;
+  }
+  if (conv) {
+    job.ready = true;   // (the conversion takes residues of any kind)
+    job.a.nsplit = conv_shares((u64)job.npoly * (N / CONV_TILE), K + 1, job.a.nfp * 4 + job.a.nint * 7, keep);
     return launch_conv_rows(c, job, st);
   }
   {
@@ -1465,7 +1496,9 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
   if (io.galois_pc && B > KS_MULTI_MAX) return fail(CKKS_ESHAPE, "internal: per-ciphertext keys for too many ciphertexts");
   const bool fused_fp = c->tune[3] != 1;
   if ((acc_add || io.more != KS_PLAIN) && !fused_fp) return fail(CKKS_EINVAL, "internal: this needs the default inner kernels");
-  auto ext_class = [&](u32 s) { return host_class(c, c->mod[emap.id[s]]); };
+  const DropForm form = io.drop ? drop_form(c, lt, nlimbs) : APART;
+  auto ext_class = [&](u32 s) { return form == JOINED_FORCED && s + 1 == nlimbs ? 2 : host_class(c, c->mod[emap.id[s]]); };
+  const u32 keep = io.drop ? nlimbs - 1 : nlimbs, first_special = form == APART ? nlimbs : keep;
   bool any_fp = false, any_int = false, special_fp = false;
   for (u32 s_ = 0; s_ < next; s_++) {
     const bool fp = ext_class(s_) == 0;
@@ -1483,7 +1516,7 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
   o1.split_out = fused_up;
   ConvJob up;
   if (conv_up) {
-    up = conv_up_job(c, lt, dcoef, ext, B, nlimbs);
+    up = conv_up_job(c, lt, dcoef, ext, B, nlimbs, form == JOINED_FORCED);
     o1.blocks_only = !up.ready;
   }
   const u64 polyN = (u64)nlimbs * N;
@@ -1565,6 +1598,7 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
   ia.next = next;
   ia.map_mode = map_mode_inner(c, io.galois_pc == nullptr);
   ia.galois = io.d_galois;
+  ia.first_special = first_special;
   ia.ext_galois = 0;
   ia.more = io.more_args;
   if (io.galois_pc) {
@@ -1584,7 +1618,7 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
     for (int cls = 1; cls <= 2; cls++) {
       u32 cnt = 0;
       for (u32 s_ = 0; s_ < next; s_++)
-        if (ext_class(s_) == cls && (s_ >= nlimbs ? special : main_slots && !(fin && io.drop && s_ + 1 == nlimbs)))
+        if (ext_class(s_) == cls && (s_ >= first_special ? special : main_slots && s_ < keep))
           a.slots[cnt++] = (unsigned char)s_;
       if (!cnt) continue;
       ProfScope ps(c, PK_INNER8 + cls - 1, st);
@@ -1626,8 +1660,7 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
     if ((rc = launch_inner_fp(true, acc_add || !fused_fp, st))) return rc;
   }
   if (acc_add) return CKKS_OK;
-  const u32 keep = io.drop ? nlimbs - 1 : nlimbs;
-  if (io.drop) {   // the last main limb's accumulators, on top of what lies there
+  if (io.drop && form == APART) {   // the last main limb's accumulators, on top of what lies there
     FwdInnerArgs a = ia;
     a.accumulate = 1;
     a.twi = nullptr;
@@ -1696,8 +1729,9 @@ static FwdInnerArgs hoisted_args(const ckks_ctx* c, const LevelTables* lt, const
 // Shared front of the hoisted rotations: inverse transform, ModUp and forward transform of B polynomials (limb-vector (b, t) at
 // d + b*d_stride + t*N) into the workspace, and the arguments of the streaming inner-product kernels that read them
 // (accumulators default to the workspace's own).
+// last_int: limb nlimbs - 1 in integers (JOINED_FORCED).
 static int hoist_front16(ckks_ctx* c, const LevelTables* lt, const u64* d, u64 d_stride, u32 B, u32 nlimbs, char* ws,
-                         hipStream_t st, FwdInnerArgs& ia) {
+                         hipStream_t st, FwdInnerArgs& ia, bool last_int = false) {
   int rc;
   const u32 N = c->N, next = lt->next, beta = lt->beta;
   const u64 polyN = (u64)nlimbs * N;
@@ -1710,9 +1744,10 @@ static int hoist_front16(ckks_ctx* c, const LevelTables* lt, const u64* d, u64 d
   of.blocks_only = conv_fits(c, 0, nlimbs, c->alpha);
   ConvJob up;
   if (of.blocks_only) {
-    up = conv_up_job(c, lt, dcoef, ext, B, nlimbs);
+    up = conv_up_job(c, lt, dcoef, ext, B, nlimbs, last_int);
     o1.blocks_only = !up.ready;
   }
+  if (last_int) of.int_id = (int)nlimbs - 1;
   if ((rc = launch_ntt(c, true, d, d_stride, dcoef, polyN, B, 0, nlimbs, qmap, 0, 0, st, o1))) return rc;
   if (of.blocks_only) {
     if ((rc = launch_conv_rows(c, up, st))) return rc;

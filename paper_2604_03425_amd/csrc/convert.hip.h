@@ -51,6 +51,7 @@ struct ConvArgs {
   u32 first_id;              // modulus id of source 0 itself (src_id0, or a main prime's before special ones)
   u32 src_nlimbs, alpha, beta;  // digit j = p % beta owns sources j*alpha .. j*alpha + len - 1
   u32 skip_own;              // != 0: target slots j*alpha .. j*alpha + len - 1 are the digit's own limbs: left alone
+  u32 last_int;              // != 0: double-precision sources, but slot src_nlimbs - 1 is the first of the integer targets
   u32 ntarget;               // targets of a digit in the constant tables
   u32 nfp, nint;             // targets by arithmetic kind: tslot[0 .. nfp), tslot[nfp .. nfp + nint)
   u32 nsplit;                // workgroups that share the targets of a (polynomial, tile)
@@ -623,12 +624,13 @@ __global__ void __launch_bounds__(CONV_THREADS) __attribute__((amdgpu_waves_per_
   auto walk = [&](u32 first, u32 count, bool own_kind, u32 n, auto* tables, auto zero, auto transform) {
     typedef decltype(zero) V;
     typedef std::remove_const_t<std::remove_pointer_t<decltype(tables)>> TW;
-    const u32 skip = own_kind && a.skip_own ? len : 0;
+    const u32 apart = a.last_int && lo + len == a.src_nlimbs ? 1 : 0;   // own limbs that are listed with the other kind, ahead of it
+    const u32 skip = a.skip_own ? (own_kind ? len - apart : apart) : 0, from = own_kind ? lo : 0;
     count -= skip;
     if (n >= count) return;
     auto at = [&](u32 i) {
       i = min(i, count - 1);
-      return a.target[first + i + (i >= lo ? skip : 0)];
+      return a.target[first + i + (i >= from ? skip : 0)];
     };
     u32 i0 = at(n), i1 = at(n + a.nsplit), buffer = 0;
     ConvTarget t0, t1, n0, n1;

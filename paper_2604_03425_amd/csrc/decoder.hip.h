@@ -49,13 +49,13 @@ struct ProductOut {
   const ulonglong2* less;   // null: kept = nlimbs; else [nlimbs - 1] Shoup pairs of q_last^-1
   u64* last;                // limb nlimbs - 1 of accumulator c of ciphertext b at last + (2 b + c) * last_stride
   u64 last_stride;
-  u32 nlimbs;
+  u32 nlimbs, last_int;     // != 0: the accumulators of that limb are integer ones (times 2^-64) whatever its class
 };
 template <bool FP>
 __device__ __forceinline__ void store_product(const ProductOut& o, size_t b, int c, u32 l, size_t n, size_t N, ulonglong2 w, const ModInfo& mi) {
   if (o.less && c < 2) {
     if (l + 1 == o.nlimbs) {
-      if (FP) w = {prod_mulmod<true>(w.x, mi.pmod, mi), prod_mulmod<true>(w.y, mi.pmod, mi)};
+      if (FP && !o.last_int) w = {prod_mulmod<true>(w.x, mi.pmod, mi), prod_mulmod<true>(w.y, mi.pmod, mi)};
       else w = {csub(mont_mul63(w.x, mi.pmod, mi.m, mi.minv), mi.m), csub(mont_mul63(w.y, mi.pmod, mi.m, mi.minv), mi.m)};
       *(ulonglong2*)(o.last + (2 * b + c) * o.last_stride + n) = w;
       return;

@@ -94,13 +94,14 @@ struct Decoder {
   bool fused() const { return two_pass(cc) && cc->tune[3] != 1; }
   int product_out(ProductOut* o, u64* out, u32 n, u32 limbs, bool more) const {
     int rc;
-    *o = ProductOut{out, nullptr, nullptr, 0, limbs};
+    *o = ProductOut{out, nullptr, nullptr, 0, limbs, 0};
     if (!more || !fused()) return CKKS_OK;
     const LevelTables* lt;
     if ((rc = get_level(c, limbs, &lt))) return rc;
     o->less = lt->rs_qinv;
     o->last = (u64*)(ks + ks_layout(c, n, limbs).acc) + poly(limbs - 1);
     o->last_stride = poly(lt->next);
+    o->last_int = drop_form(cc, lt, limbs) == JOINED_FORCED;
     return CKKS_OK;
   }
   // Relin of products in three components (at `limbs` limbs); more: dividing by the last prime too.
@@ -118,14 +119,15 @@ struct Decoder {
       return keyswitch_impl(c, io, n, limbs, mult_key, ks, st);
     }
     const KsLayout L = ks_layout(c, n, limbs);
-    if ((rc = ext_digits(c, lt, false, in + 2 * pl, 3 * pl, n, limbs, ks, st))) return rc;
+    const bool last_int = drop_form(c, lt, limbs) == JOINED_FORCED;
+    if ((rc = ext_digits(c, lt, false, in + 2 * pl, 3 * pl, n, limbs, ks, st, last_int))) return rc;
     u64* acc = (u64*)(ks + L.acc);
     RotSumArgs r = rot_sum_args(c, lt, false, limbs, acc, 3 * pl);
     r.base = in;
     r.base_stride = 3 * pl;
     r.nterms = 1;
     r.term[0] = RotTerm{(const u64*)(ks + L.ext), in + 2 * pl, nullptr, mult_key, 1};
-    if ((rc = launch_rot_sum(c, r, n, st))) return rc;
+    if ((rc = launch_rot_sum(c, r, n, st, 1, false, last_int))) return rc;
     return ext_mod_down_more(c, lt, acc, out, n, limbs, ks, st);
   }
   int sum_rotations(u64* out, const u64* in, u32 n, const std::vector<u32>& elements, const u64* const* rot_keys, bool more) {
@@ -133,7 +135,8 @@ struct Decoder {
     const LevelTables* lt;
     if ((rc = get_level(c, nlimbs, &lt))) return rc;
     u64* acc = (u64*)(ks + ks_layout(c, n, nlimbs).acc);
-    if ((rc = rotations_to_ext(c, lt, false, in, n, nlimbs, elements.data(), rot_keys, (u32)elements.size(), nullptr, 1, acc, ks, st)))
+    if ((rc = rotations_to_ext(c, lt, false, in, n, nlimbs, elements.data(), rot_keys, (u32)elements.size(), nullptr, 1, acc, ks, st,
+                               more && drop_form(c, lt, nlimbs) == JOINED_FORCED)))
       return rc;
     return more ? ext_mod_down_more(c, lt, acc, out, n, nlimbs, ks, st) : ext_mod_down(c, lt, false, acc, out, n, nlimbs, ks, st);
   }

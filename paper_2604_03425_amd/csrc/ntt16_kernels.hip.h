@@ -424,6 +424,7 @@ struct FwdInnerArgs {
   // ntt16_fwd_blocks_inner8_kernel only: != null takes the accumulators of the special limbs through the inverse block pass
   // before it stores them (ModDown goes on with the inverse row pass)
   const ulonglong2* twi = nullptr;
+  u32 first_special = 0;     // where those begin: nlimbs, or the last main limb where that is divided away with them; its sums start from acc
   u32 logN, nlimbs, nq, nm, alpha, beta, next, map_mode, galois;
   u32 ext_galois;            // streaming kernels only: != 0 reads ext through the Galois map too (hoisted digits:
                              // ext holds the transform of the un-rotated polynomial, shared by many rotations)
@@ -975,7 +976,18 @@ ntt16_fwd_blocks_inner8_kernel(FwdInnerArgs a) {
     return;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy into LDS may outlive the workgroup
-  if (a.twi && t >= a.nlimbs) {   // uniform
+  if (a.twi && t >= a.first_special) {   // uniform
+    if (t < a.nlimbs) {
+      const u64* s0 = a.acc + ((size_t)b * 2 * a.next + t) * N + posC;
+      u64 v[8];
+#pragma unroll
+      for (int e = 0; e < 2; e++) {
+        u64(&acc)[8] = e ? acc1 : acc0;
+        inner8_load(v, s0 + (size_t)e * a.next * N);
+#pragma unroll
+        for (int c = 0; c < 8; c++) acc[c] = csub(acc[c] + v[c], q2);
+      }
+    }
     u64 y[2][8];
 #pragma unroll
     for (int c = 0; c < 8; c++) y[0][c] = acc0[c], y[1][c] = acc1[c];
