@@ -138,6 +138,8 @@ struct LevelTables {
   ulonglong2* dm_inv = nullptr;    // [K+1]  (D/c_i)^-1 mod c_i, Shoup pairs
   ulonglong2* dm_scale = nullptr;  // [K+1]  the same / N (two-pass rings: in the form of the class, integer ones times 2^64)
   ulonglong2* dm_iscale = nullptr; // [K+1]  the same, all in integer form
+  bool narrow_dm = false;          // ring 2^12 (at most 44 special primes): dm_mat12 and dm_off12 are dn_mat_plain and dn_off there
+  u64 *dm_mat12 = nullptr, *dm_off12 = nullptr;   // [nlimbs-1][K+1], [nlimbs-1]
   ulonglong2* dm_pinv = nullptr;   // [nlimbs-1]  D^-1 mod q_t, Shoup pairs
   ulonglong2* dm_pinv2 = nullptr;  // [nlimbs-1]  the same in the form of pinv2
 };
@@ -482,6 +484,26 @@ LevelTables build_level(const ckks_ctx* c, u32 nlimbs, LevelArena& arena) {
       dm_iscale[i] = ulonglong2{w, h_shoup(w, m)};
       dm_scale[i] = is_fp(m) ? as_fp(v, m) : dm_iscale[i];
     }
+    if (c->logN == 12 && n <= 45) {
+      u32 bs = 0, bt = 0, bt_min = 64;
+      for (u64 m : src) bs = std::max(bs, h_bits(m));
+      for (u32 i = 0; i < keep; i++) bt = std::max(bt, h_bits(c->mod[i])), bt_min = std::min(bt_min, h_bits(c->mod[i]));
+      t.narrow_dm = c->tune[5] == 0 && bconv_narrow_ok(n, bs, bt, bt_min);
+      std::vector<u64> mat((size_t)keep * n), off(keep);
+      for (u32 i = 0; i < keep; i++) {
+        const u64 m = c->mod[i], r64_inv = is_fp(m) ? 1 : h_inv(h_mont(1, m), m);
+        auto scaled = [&](u64 v) { return h_mul(t.narrow_dm ? h_mont90(v, m) : h_mont(v, m), r64_inv, m); };
+        u64 sum = 0;
+        for (u32 k = 0; k < n; k++) {
+          const u64 v = others(k, m);
+          mat[(size_t)i * n + k] = scaled(v);
+          sum = (u64)(((u128)sum + h_mul(v, ((src[k] - 1) / 2) % m, m)) % m);
+        }
+        off[i] = scaled(sum ? m - sum : 0);
+      }
+      t.dm_mat12 = arena.add(mat);
+      t.dm_off12 = arena.add(off);
+    }
     for (u32 t_ = 0; t_ < keep; t_++) {
       const u64 m = c->mod[t_], inv = h_inv(others(n, m), m), w = h_mont(inv, m);
       const u64 less = !is_fp(m) && c->logN >= 13 && c->logN <= 16 ? h_inv(h_mont(1, m), m) : 1;
@@ -563,6 +585,7 @@ int build_levels(ckks_ctx* c) {
     if (nl > 1 && c->np) {
       rebase(t.dm_pieces);
       if (t.dm_rows) rebase(t.dm_rows);
+      if (t.narrow_dm || t.dm_off12) { rebase(t.dm_mat12); rebase(t.dm_off12); }
       rebase(t.dm_inv); rebase(t.dm_scale); rebase(t.dm_iscale); rebase(t.dm_pinv); rebase(t.dm_pinv2);
     }
   }
@@ -1003,7 +1026,7 @@ struct KsIo {
   // ciphertexts [B][2][nlimbs][N], whose other two product terms are the addends
   const u64 *prod_a = nullptr, *prod_b = nullptr;
   bool steps = false;          // ring 2^12: one kernel per step (whole_limb said no)
-  // two-pass rings with knob 3 at its default, addends add2 only: division by the last main prime too, so that out has a limb less. The
+  // ring 2^12, and two-pass rings with knob 3 at its default, addends add2 only: division by the last main prime too, so that out has a limb less. The
   // addends come divided by that prime, and P times their last limb (on integer moduli times 2^-64) lies in the accumulators already.
   bool drop = false;
   int more = KS_PLAIN;         // two-pass rings with knob 3 at its default: KS_WEIGHTED or KS_MAPPED with these arguments
@@ -1897,7 +1920,7 @@ Ks12Args ks12_args(const ckks_ctx* c, const LevelTables* lt, u32 B, u32 nlimbs, 
   a.dn_off = lt->dn_off;
   a.up_pitch = lt->up_pitch;
   a.dn_pitch = lt->dn_pitch;
-  a.nlimbs = nlimbs;
+  a.nlimbs = a.keep = nlimbs;
   a.nq = c->nq;
   a.nm = c->nm;
   a.alpha = c->alpha;
@@ -1908,6 +1931,15 @@ Ks12Args ks12_args(const ckks_ctx* c, const LevelTables* lt, u32 B, u32 nlimbs, 
   for (u32 i = 0; i < c->nm; i++)
     if (host_class(c, c->mod[i]) == 0) a.fp_mask[i >> 5] |= 1u << (i & 31);
   return a;
+}
+// The division takes the last main limb too.
+void ks12_drop(Ks12Args& a, const LevelTables* lt) {
+  a.keep = a.nlimbs - 1;
+  a.dn_scale = lt->dm_scale;
+  a.pinv = lt->dm_pinv2;
+  a.dn_mat = lt->dm_mat12;
+  a.dn_off = lt->dm_off12;
+  a.dn_pitch = a.next - a.keep;
 }
 void launch_ks12_digits(const ckks_ctx* c, const LevelTables* lt, u32 B, u32 nlimbs, const Ks12Args& a, hipStream_t st) {
   const dim3 block(WL_THREADS);
@@ -1944,16 +1976,17 @@ int keyswitch_whole12(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
   a.multi = io.galois_pc ? 1u : 0u;
   if (io.galois_pc)
     for (u32 i = 0; i < B; i++) a.galois_pc[i] = io.galois_pc[i], a.evk_pc[i] = io.evk_pc[i];
+  if (io.drop) ks12_drop(a, lt);
   launch_ks12_digits(c, lt, B, nlimbs, a, st);
   const dim3 block(WL_THREADS);
   {
     ProfScope ps(c, PK_KS12_SPECIAL, st);
-    hipLaunchKernelGGL(ks12_special_kernel, dim3(2 * B, c->np), block, 0, st, a);
+    hipLaunchKernelGGL(ks12_special_kernel, dim3(2 * B, a.next - a.keep), block, 0, st, a);
   }
   {
     ProfScope ps(c, PK_KS12_FINAL, st);
-    const dim3 grid(2 * B, nlimbs);
-    if (lt->narrow_dn) hipLaunchKernelGGL(ks12_final_kernel<true>, grid, block, 0, st, a);
+    const dim3 grid(2 * B, a.keep);
+    if (io.drop ? lt->narrow_dm : lt->narrow_dn) hipLaunchKernelGGL(ks12_final_kernel<true>, grid, block, 0, st, a);
     else hipLaunchKernelGGL(ks12_final_kernel<false>, grid, block, 0, st, a);
   }
   HIP_TRY(hipGetLastError());

@@ -7,8 +7,24 @@ namespace {
 
 // ModDown by P q_{nlimbs-1} of both accumulators [B][2][next][N] (what lies from limb nlimbs - 1 on is overwritten) to out
 // [B][2][nlimbs - 1][N]: that limb joins the special ones as a source of the conversion.
-int ext_mod_down_more(ckks_ctx* c, const LevelTables* lt, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
+int ext_mod_down_more(ckks_ctx* c, const LevelTables* lt, bool whole, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
   int rc;
+  if (whole) {
+    Ks12Args a = ks12_args(c, lt, B, nlimbs, ws);
+    a.sums = a.acc = acc;
+    a.out = out;
+    ks12_drop(a, lt);
+    const dim3 block(WL_THREADS), grid(2 * B, a.keep);
+    {
+      ProfScope ps(c, PK_KS12_SPECIAL, st);
+      hipLaunchKernelGGL(ks12_special_sums_kernel, dim3(2 * B, a.next - a.keep), block, 0, st, a);
+    }
+    ProfScope ps(c, PK_KS12_FINAL, st);
+    if (lt->narrow_dm) hipLaunchKernelGGL(ks12_final_sums_kernel<true>, grid, block, 0, st, a);
+    else hipLaunchKernelGGL(ks12_final_sums_kernel<false>, grid, block, 0, st, a);
+    HIP_TRY(hipGetLastError());
+    return CKKS_OK;
+  }
   const u32 N = c->N, next = lt->next, K = c->np, keep = nlimbs - 1;
   u64* tq = (u64*)(ws + ks_layout(c, B, nlimbs).tq);
   if (two_pass(c)) {
@@ -91,13 +107,16 @@ struct Decoder {
   }
   // Whether a relinearisation that divides by the last prime too takes the fused kernels of a key switch; products for one go where it
   // wants them (`more` of product_out).
-  bool fused() const { return two_pass(cc) && cc->tune[3] != 1; }
+  // Ring 2^12: whether n ciphertexts go through the kernels that hold whole limbs.
+  bool whole(const LevelTables* lt, u32 n, u32 limbs) const { return lt->dm_off12 && whole_limb(cc, n, limbs, false); }
+  bool fused(const LevelTables* lt, u32 n, u32 limbs) const { return two_pass(cc) ? cc->tune[3] != 1 : whole(lt, n, limbs); }
   int product_out(ProductOut* o, u64* out, u32 n, u32 limbs, bool more) const {
     int rc;
     *o = ProductOut{out, nullptr, nullptr, 0, limbs, 0};
-    if (!more || !fused()) return CKKS_OK;
+    if (!more) return CKKS_OK;
     const LevelTables* lt;
     if ((rc = get_level(c, limbs, &lt))) return rc;
+    if (!fused(lt, n, limbs)) return CKKS_OK;
     o->less = lt->rs_qinv;
     o->last = (u64*)(ks + ks_layout(c, n, limbs).acc) + poly(limbs - 1);
     o->last_stride = poly(lt->next);
@@ -111,7 +130,7 @@ struct Decoder {
     const LevelTables* lt;
     if ((rc = get_level(c, limbs, &lt))) return rc;
     const u64 pl = poly(limbs);
-    if (fused()) {
+    if (fused(lt, n, limbs)) {
       KsIo io{in + 2 * pl, 3 * pl, 0, out, {1, 1}, nullptr, 0};
       io.add2 = in;
       io.add2_three = true;
@@ -128,17 +147,19 @@ struct Decoder {
     r.nterms = 1;
     r.term[0] = RotTerm{(const u64*)(ks + L.ext), in + 2 * pl, nullptr, mult_key, 1};
     if ((rc = launch_rot_sum(c, r, n, st, 1, false, last_int))) return rc;
-    return ext_mod_down_more(c, lt, acc, out, n, limbs, ks, st);
+    return ext_mod_down_more(c, lt, false, acc, out, n, limbs, ks, st);
   }
   int sum_rotations(u64* out, const u64* in, u32 n, const std::vector<u32>& elements, const u64* const* rot_keys, bool more) {
     int rc;
     const LevelTables* lt;
     if ((rc = get_level(c, nlimbs, &lt))) return rc;
     u64* acc = (u64*)(ks + ks_layout(c, n, nlimbs).acc);
-    if ((rc = rotations_to_ext(c, lt, false, in, n, nlimbs, elements.data(), rot_keys, (u32)elements.size(), nullptr, 1, acc, ks, st,
+    const bool by_limbs = whole(lt, n, nlimbs);
+    if ((rc = rotations_to_ext(c, lt, by_limbs, in, n, nlimbs, elements.data(), rot_keys, (u32)elements.size(), nullptr, 1, acc, ks, st,
                                more && drop_form(c, lt, nlimbs) == JOINED_FORCED)))
       return rc;
-    return more ? ext_mod_down_more(c, lt, acc, out, n, nlimbs, ks, st) : ext_mod_down(c, lt, false, acc, out, n, nlimbs, ks, st);
+    return more ? ext_mod_down_more(c, lt, by_limbs, acc, out, n, nlimbs, ks, st)
+                : ext_mod_down(c, lt, by_limbs, acc, out, n, nlimbs, ks, st);
   }
   // The sum over the components of a lane of products d (nlimbs limbs), less a limb, in every slot of the lane. In one of y; where is
   // returned in `out`.

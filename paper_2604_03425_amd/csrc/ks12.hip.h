@@ -31,6 +31,8 @@ struct Ks12Args {
   const u64 *up_mat, *up_off, *dn_mat, *dn_off;
   u32 up_pitch, dn_pitch;
   u32 nlimbs, nq, nm, alpha, beta, next, fp_on;
+  u32 keep;                // limbs of out: nlimbs, or one less where the last limb is divided away with the special ones (its sums start
+                           // from acc, the dn_ and pinv constants are for that division)
   u32 fp_mask[4];          // bit id: modulus id is of double-precision class
   u32 mode0, mode1, add2_three;
   u32 d_galois, add_galois;
@@ -243,26 +245,36 @@ __device__ __forceinline__ void ks12_load_sums(typename Ks12Mod<FP>::V (&s)[4], 
   for (int k = 0; k < 4; k++) s[k] = md.settle(md.load(p[wl_elem(2, k)]));
 }
 
-// grid = (2B, special limbs): back to coefficient form, scaled by (P/p_k)^-1 / N (times 2^64 on integer classes)
+// Modulus id of the limb number i that a division takes away.
+__device__ __forceinline__ u32 ks12_source(const Ks12Args& a, u32 i) {
+  const u32 t = a.keep + i;
+  return t < a.nlimbs ? t : t - a.nlimbs + a.nq;
+}
+// grid = (2B, limbs divided away): back to coefficient form, scaled by (P/p_k)^-1 / N (times 2^64 on integer classes)
 template <bool FP, bool SUMS = false>
 __device__ __forceinline__ void ks12_special(const Ks12Args& a, u64* sm) {
-  const u32 bc = blockIdx.x, t = a.nlimbs + blockIdx.y, id = t - a.nlimbs + a.nq;
+  const u32 bc = blockIdx.x, t = a.keep + blockIdx.y, id = ks12_source(a, blockIdx.y);
   const Ks12Mod<FP> md(ks12_mod(a.mods, id));
   typename Ks12Tables<FP>::W w;
   w.load(Ks12Tables<FP>::inv(a, id));
   typename Ks12Mod<FP>::V s[4];
   if (SUMS) ks12_load_sums<FP>(s, a, bc, t, md);
   else ks12_inner<FP>(s, a, bc >> 1, bc & 1, t, id, md);
+  if (!SUMS && t < a.nlimbs) {
+    const u64* start = a.acc + ((size_t)bc * a.next + t) * 4096;
+#pragma unroll
+    for (int k = 0; k < 4; k++) s[k] = md.settle(s[k] + md.load(start[wl_elem(2, k)]));
+  }
   u64 y[4];
   ulonglong2 sc;
-  scalar_fetch(sc, a.dn_scale, t - a.nlimbs);
+  scalar_fetch(sc, a.dn_scale, blockIdx.y);
   md.inverse(y, s, w, sc, sm);
   u64* o = a.acc + ((size_t)bc * a.next + t) * 4096;
 #pragma unroll
   for (int k = 0; k < 4; k++) o[wl_elem(0, k)] = ks12_split(y[k], md.mi.m);
 }
 
-// grid = (2B, nlimbs)
+// grid = (2B, limbs of out)
 template <bool FP, bool NARROW, bool SUMS = false>
 __device__ __forceinline__ void ks12_final(const Ks12Args& a, u64* sm) {
   const u32 bc = blockIdx.x, i = blockIdx.y, b = bc >> 1, c = bc & 1;
@@ -282,7 +294,7 @@ __device__ __forceinline__ void ks12_final(const Ks12Args& a, u64* sm) {
     if (mode & 2) ew[k] = as[galois_src_index(n, g, 12)];
   }
   u64 y[4];
-  ks12_convert<NARROW>(y, a.acc + ((size_t)bc * a.next + a.nlimbs) * 4096, a.next - a.nlimbs,
+  ks12_convert<NARROW>(y, a.acc + ((size_t)bc * a.next + a.keep) * 4096, a.next - a.keep,
                        scalar_words(a.dn_mat + (size_t)i * a.dn_pitch), *scalar_words(a.dn_off + i), md.mi);
   typename Ks12Mod<FP>::V x[4];
 #pragma unroll
@@ -294,7 +306,7 @@ __device__ __forceinline__ void ks12_final(const Ks12Args& a, u64* sm) {
   ulonglong2 pv;
   scalar_fetch(pv, a.pinv, i);
   const size_t o0 = (size_t)b * 2 * pl + lo, o1 = o0 + pl;
-  u64* o = a.out + (size_t)bc * pl + lo;
+  u64* o = a.out + (size_t)bc * a.keep * 4096 + lo;
 #pragma unroll
   for (int k = 0; k < 4; k++) {
     const u32 n = wl_elem(2, k);
@@ -326,10 +338,10 @@ template <bool NARROW>
 KS12_KERNEL(ks12_digits_kernel,
             mod_class(a.mods[blockIdx.y < a.nlimbs ? blockIdx.y : blockIdx.y - a.nlimbs + a.nq].m, a.fp_on) == 0,
             (ks12_digits<true, NARROW>), (ks12_digits<false, NARROW>))
-KS12_KERNEL(ks12_special_kernel, ks12_fp(a, a.nq + blockIdx.y), ks12_special<true>, ks12_special<false>)
+KS12_KERNEL(ks12_special_kernel, ks12_fp(a, ks12_source(a, blockIdx.y)), ks12_special<true>, ks12_special<false>)
 template <bool NARROW>
 KS12_KERNEL(ks12_final_kernel, ks12_fp(a, blockIdx.y), (ks12_final<true, NARROW>), (ks12_final<false, NARROW>))
 // The second half of a key switch from sums that another kernel formed.
-KS12_KERNEL(ks12_special_sums_kernel, ks12_fp(a, a.nq + blockIdx.y), (ks12_special<true, true>), (ks12_special<false, true>))
+KS12_KERNEL(ks12_special_sums_kernel, ks12_fp(a, ks12_source(a, blockIdx.y)), (ks12_special<true, true>), (ks12_special<false, true>))
 template <bool NARROW>
 KS12_KERNEL(ks12_final_sums_kernel, ks12_fp(a, blockIdx.y), (ks12_final<true, NARROW, true>), (ks12_final<false, NARROW, true>))
