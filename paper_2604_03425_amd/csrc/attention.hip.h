@@ -252,6 +252,36 @@ __global__ void __launch_bounds__(256) rot_sum_kernel(RotSumArgs a) {
 // Doubles: digits within q / 2, key words below q < 2^50, so that four products stay within 2^101 of H = 1.5 * 2^102, in whose binade
 // sums are multiples of 2^50 and what a product loses in joining H is exact and goes to L: 4 instructions a term, 6 every fourth.
 #define BLOCK_SUM 256
+#define BLOCK_SUM_AHEAD 4
+// Walks over the terms, digit by digit and rotation by rotation, with the key words requested BLOCK_SUM_AHEAD terms ahead (what a
+// workgroup waits for is their way from memory, which the others that share them wait for too). begin(j) puts digit j into LDS,
+// term(e0, e1, m) multiplies by the words of both components what lies at index m of the block.
+template <class Begin, class Term>
+__device__ __forceinline__ void block_sum_terms(const RotSumArgs& a, size_t at, size_t comp, u32 n, Begin begin, Term term) {
+  const u32 R = a.nterms, total = R * a.beta;
+  u64 k0[BLOCK_SUM_AHEAD], k1[BLOCK_SUM_AHEAD];
+  u32 rr = 0, jj = 0;   // the next term to request
+  auto request = [&](int u) {
+    const u64* e = uniform_ptr(a.term[rr].evk) + (size_t)min(jj, a.beta - 1) * 2 * comp + at;
+    k0[u] = e[0], k1[u] = e[comp];
+    if (++rr == R) rr = 0, jj++;
+  };
+#pragma unroll
+  for (int u = 0; u < BLOCK_SUM_AHEAD; u++) request(u);
+  u32 r = 0, j = 0;
+#pragma nounroll
+  for (u32 i = 0; i < total; i += BLOCK_SUM_AHEAD) {
+#pragma unroll
+    for (int u = 0; u < BLOCK_SUM_AHEAD; u++) {
+      if (i + u >= total) break;   // uniform
+      if (r == 0) begin(j);
+      term(k0[u], k1[u], galois_src_index(n, a.term[r].galois, a.logN) & (BLOCK_SUM - 1));
+      request(u);
+      if (++r == R) r = 0, j++;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
 template <int CB>
 __device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 blk, u32 zi, u64* sm) {
   constexpr double M = 1.5 * 5070602400912917605986812821504.0;   // 1.5 * 2^102
@@ -285,45 +315,39 @@ __device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 
   };
   const u32 R = a.nterms;
   request(0);
-  u64 k0, k1;
-  {
-    const u64* e = a.term[0].evk + (size_t)id * N + n;
-    k0 = e[0], k1 = e[comp];
-  }
   u32 count = 0;
-  for (u32 j = 0; j < a.beta; j++) {
-    const u64 bias = j == jo ? 0x4330000000000000ull : 0ull;   // residues become doubles, doubles stay what they are
-    const double less = __longlong_as_double((long long)bias);
+  block_sum_terms(
+      a, (size_t)id * N + n, comp, n,
+      [&](u32 j) {
+        const u64 bias = j == jo ? 0x4330000000000000ull : 0ull;   // residues become doubles, doubles stay what they are
+        const double less = __longlong_as_double((long long)bias);
+        if (j) tile = (double*)sm + (tile == (double*)sm ? CB * BLOCK_SUM : 0);
 #pragma unroll
-    for (int k = 0; k < CB; k++) {
-      const double v = __longlong_as_double((long long)(ahead[k] | bias)) - less;
-      tile[k * BLOCK_SUM + tid] = j == jo ? fp_reduce(v, qinv, q) : v;
-    }
-    lds_barrier();   // the other tile's readers are past it, since they have written this one
-    if (j + 1 < a.beta) request(j + 1);
-    for (u32 r = 0; r < R; r++) {
-      const double e0 = u2d(k0), e1 = u2d(k1);
-      const u32 rn = r + 1 < R ? r + 1 : 0, jn = min(r + 1 < R ? j : j + 1, a.beta - 1);
-      const u64* e = a.term[rn].evk + (size_t)jn * 2 * comp + (size_t)id * N + n;
-      k0 = e[0], k1 = e[comp];
-      const u32 m = galois_src_index(n, a.term[r].galois, a.logN) & (BLOCK_SUM - 1);
+        for (int k = 0; k < CB; k++) {
+          const double v = __longlong_as_double((long long)(ahead[k] | bias)) - less;
+          tile[k * BLOCK_SUM + tid] = j == jo ? fp_reduce(v, qinv, q) : v;
+        }
+        lds_barrier();   // the other tile's readers are past it, since they have written this one
+        if (j + 1 < a.beta) request(j + 1);
+      },
+      [&](u64 k0, u64 k1, u32 m) {
+        const double e0 = u2d(k0), e1 = u2d(k1);
 #pragma unroll
-      for (int k = 0; k < CB; k++) {
-        const double x = tile[k * BLOCK_SUM + m];
-        const double p0 = __builtin_fma(x, e0, H0[k]), h0 = p0 - H0[k];
-        L0[k] += __builtin_fma(x, e0, -h0);
-        H0[k] = p0;
-        const double p1 = __builtin_fma(x, e1, H1[k]), h1 = p1 - H1[k];
-        L1[k] += __builtin_fma(x, e1, -h1);
-        H1[k] = p1;
-      }
-      if ((++count & 3) == 0) {
+        for (int k = 0; k < CB; k++) {
+          const double x = tile[k * BLOCK_SUM + m];
+          const double p0 = __builtin_fma(x, e0, H0[k]), h0 = p0 - H0[k];
+          L0[k] += __builtin_fma(x, e0, -h0);
+          H0[k] = p0;
+          const double p1 = __builtin_fma(x, e1, H1[k]), h1 = p1 - H1[k];
+          L1[k] += __builtin_fma(x, e1, -h1);
+          H1[k] = p1;
+        }
+        if ((++count & 3) == 0) {
 #pragma unroll
-        for (int k = 0; k < CB; k++) settle(H0[k], L0[k]), settle(H1[k], L1[k]);
-      }
-    }
-    tile = (double*)sm + (tile == (double*)sm ? CB * BLOCK_SUM : 0);
-  }
+          for (int k = 0; k < CB; k++) settle(H0[k], L0[k]), settle(H1[k], L1[k]);
+        }
+      });
+  tile = (double*)sm + (tile == (double*)sm ? CB * BLOCK_SUM : 0);
   if (main_prime) {   // P (base + sum of the rotated first components), P base
     const u64* c0 = a.term[0].c0 + (size_t)t * N + n;
     double v[CB];
@@ -391,11 +415,6 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
   };
   const u32 R = a.nterms;
   request(0);
-  u64 k0, k1;
-  {
-    const u64* e = a.term[0].evk + (size_t)id * N + n;
-    k0 = e[0], k1 = e[comp];
-  }
   u32 count = 0;
   auto carry = [&] {
     if (++count < 11) return;
@@ -403,28 +422,27 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
 #pragma unroll
     for (int k = 0; k < CB; k++) dot30_settle(s0[k], mi.mu64, nm), dot30_settle(s1[k], mi.mu64, nm);
   };
-  for (u32 j = 0; j < a.beta; j++) {
+  block_sum_terms(
+      a, (size_t)id * N + n, comp, n,
+      [&](u32 j) {
+        if (j) tile = sm + (tile == sm ? CB * BLOCK_SUM : 0);
 #pragma unroll
-    for (int k = 0; k < CB; k++) tile[k * BLOCK_SUM + tid] = ahead[k];
-    lds_barrier();
-    if (j + 1 < a.beta) request(j + 1);
-    for (u32 r = 0; r < R; r++) {
-      const u32 e00 = (u32)k0 & M30, e01 = (u32)(k0 >> 30), e10 = (u32)k1 & M30, e11 = (u32)(k1 >> 30);
-      const u32 rn = r + 1 < R ? r + 1 : 0, jn = min(r + 1 < R ? j : j + 1, a.beta - 1);
-      const u64* e = a.term[rn].evk + (size_t)jn * 2 * comp + (size_t)id * N + n;
-      k0 = e[0], k1 = e[comp];
-      const u32 m = galois_src_index(n, a.term[r].galois, a.logN) & (BLOCK_SUM - 1);
+        for (int k = 0; k < CB; k++) tile[k * BLOCK_SUM + tid] = ahead[k];
+        lds_barrier();
+        if (j + 1 < a.beta) request(j + 1);
+      },
+      [&](u64 k0, u64 k1, u32 m) {
+        const u32 e00 = (u32)k0 & M30, e01 = (u32)(k0 >> 30), e10 = (u32)k1 & M30, e11 = (u32)(k1 >> 30);
 #pragma unroll
-      for (int k = 0; k < CB; k++) {
-        const u64 x = tile[k * BLOCK_SUM + m];
-        const u32 x0 = (u32)x & M30, x1 = (u32)(x >> 30);
-        dot30_mac(s0[k], x0, x1, e00, e01);
-        dot30_mac(s1[k], x0, x1, e10, e11);
-      }
-      carry();
-    }
-    tile = sm + (tile == sm ? CB * BLOCK_SUM : 0);
-  }
+        for (int k = 0; k < CB; k++) {
+          const u64 x = tile[k * BLOCK_SUM + m];
+          const u32 x0 = (u32)x & M30, x1 = (u32)(x >> 30);
+          dot30_mac(s0[k], x0, x1, e00, e01);
+          dot30_mac(s1[k], x0, x1, e10, e11);
+        }
+        carry();
+      });
+  tile = sm + (tile == sm ? CB * BLOCK_SUM : 0);
   if (main_prime) {
     const u64* c0 = a.term[0].c0 + (size_t)t * N + n;
     const u32 p0 = (u32)mi.pmod & M30, p1 = (u32)(mi.pmod >> 30);
