@@ -10,4 +10,5 @@ from .binding import (Context, CkksError, ckks_ntt, ckks_intt, ckks_automorph, c
                       OP_LINATTN_CHUNK, ckks_rope, ckks_linattn_step, ckks_linattn_chunk,
                       ckks_linattn_workspace_bytes, attn_pairs, ckks_kv_append, ckks_attn_workspace_bytes, ckks_attn_paged,
                       ckks_rmsnorm_workspace_bytes, ckks_rmsnorm)
+from .norm import rmsnorm_plan
 from .rope import rope_frequencies, rope_tables
