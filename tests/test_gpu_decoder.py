@@ -182,3 +182,305 @@ def test_norm_with_numbers_at_the_ends_of_their_range(numbers):
 def test_the_residual_sum_in_place():
     run_norm("ring10", 4, 2, 2, 1, 1, True, True, in_place=True)
     run_norm("ring13", 4, 2, 2, 1, 1, True, True, in_place=True)
+
+
+def test_more_pairs_than_a_key_switch_takes():
+    """Slices that end inside a row: the slice of 2^16 is 128 pairs, rows of 50 and 51 tokens, launches of 128 pairs; and a row that begins in
+    one slice, fills the next and ends in a third (1024 pairs on 2^10)."""
+    run_attention("ring16", 2, (51,), (3,), 7, 0, 0, 0, 1, 1)
+    run_attention("ring10", 2, (2100, 3), (1, 1), 100, 0, 0, 0, 1, 2)
+    run_attention("ring10", 3, (1030,), (2,), 64, 1025, 2, 1, 1, 1)
+
+
+def test_the_norm_of_more_than_a_key_switch_takes():
+    run_norm("ring16", 4, 65, 2, 1, 1, True, True, check=[0, 63, 64])
+    run_norm("ring10", 4, 520, 1, 2, 1, True, False, check=[0, 511, 512, 519])
+
+
+def test_ring_12_in_both_forms():
+    """By whole limbs, and from some 20 ciphertexts of 12 limbs on one kernel per step."""
+    PARAMS.setdefault("ring12_steps", lambda: make_params(12, 12, 50, 4, 60, 3))
+    run_attention("ring12_steps", 12, (66,), (1,), 9, 0, 0, 1, 2, 2)
+    run_attention("ring12_steps", 12, (3,), (1,), 9, 0, 0, 2, 2, 2)
+    run_norm("ring12_steps", 12, 66, 2, 1, 1, True, True, check=[0, 65])
+    run_norm("ring12_steps", 11, 2, 2, 2, 2, True, True)
+
+
+@pytest.mark.parametrize("name", ["ring10", "ring13_mixed", "ring14"])
+@pytest.mark.parametrize("n1,n2,stride", [(33, 1, 1), (40, 2, 2), (34, 1, 8), (2, 35, 4), (3, 5, 7), (4, 4, 16), (64, 4, 2), (8, 8, 64)])
+def test_sums_of_rotations_near_and_far(name, n1, n2, stride):
+    """Rotations that stay in blocks of 256 positions and that do not, more of them than a launch takes, digits in several tiles."""
+    import paper_2604_03425_amd as ck
+    p, rc, ctx = contexts(name)
+    nl, rows = 3, 5
+    s = attention_ref.Shape(p, rc, 1, 1, 1, seed=n1)
+    elements = [pow(5, i * stride, 2 * p.N) for i in range(1, n1)], [pow(5, i * n1 * stride % (p.N // 2), 2 * p.N) for i in range(1, n2)]
+    few = [s.key() for _ in range(3)]
+    s.baby, s.giant = elements
+    s.baby_keys, s.giant_keys = ([few[i % 3] for i in range(len(e))] for e in elements)
+    dev = [to_dev(k) for k in few]
+    keys = to_dev(s.mult_key), [dev[i % 3] for i in range(n1 - 1)], [dev[i % 3] for i in range(n2 - 1)]
+    q, k, v = s.cts((rows,), nl), [s.cts((1,), nl) for _ in range(rows)], [s.cts((1,), nl) for _ in range(rows)]
+    want = decoder_ref.attention(s, q, k, v, [1] * rows, 0, 0, 3, 0)
+    out = torch.empty((rows, 2, nl - 1, p.N), dtype=torch.int64, device="cuda")
+    ck.ckks_attn_paged(ctx, out, to_dev(q), nl, [1] * rows, [1] * rows, [to_dev(x) for x in k], [to_dev(x) for x in v], 1, nl, nl, 0, 0, 3, 0,
+                       n1, n2, stride, *keys, ctx.attn_workspace(rows, rows, nl, n1, n2, 0))
+    assert_same(to_host(out), want, "sums")
+
+
+def test_residues_at_the_ends_of_their_range():
+    """Every input at its largest value, or that and zero in turn: what the lazy ranges of the kernels are argued from."""
+    import paper_2604_03425_amd as ck
+    for name in ("ring10", "ring12", "ring13", "ring13_int", "ring13_mixed", "ring13_fp", "ring16"):
+        p, rc, ctx = contexts(name)
+        n1 = n2 = 2
+        nl, rows = 4, 3
+        s = attention_ref.Shape(p, rc, n1, n2, p.N // 8)
+        top = np.array(p.moduli, dtype=np.uint64)[:, None] - np.uint64(1)
+        for step in (1, 2):
+            full = np.zeros((len(p.moduli), p.N), dtype=np.uint64)
+            full[:, ::step] = top
+            key = np.broadcast_to(full, (p.dnum, 2) + full.shape).copy()
+            s.mult_key, s.baby_keys, s.giant_keys = key, [key], [key]
+            ct = np.broadcast_to(full[:nl], (rows, 2, nl, p.N)).copy()
+            dk = to_dev(key), [to_dev(key)], [to_dev(key)]
+            want = decoder_ref.attention(s, ct, [ct], [ct], [1], 0, 0, -1, 1)
+            out = torch.empty((1, 2, nl - 2, p.N), dtype=torch.int64, device="cuda")
+            pages = [to_dev(ct)]
+            ck.ckks_attn_paged(ctx, out, to_dev(ct), nl, [1], [rows], pages, pages, rows, nl, nl, 0, 0, -1, 1, n1, n2, p.N // 8, *dk,
+                               ctx.attn_workspace(1, 3, nl, n1, n2, 1))
+            assert_same(to_host(out), want, "attention " + name)
+            want, _ = decoder_ref.rmsnorm(s, ct, ct, full[:2], -1, -1, -1, [-1])
+            out = torch.empty((rows, 2, 1, p.N), dtype=torch.int64, device="cuda")
+            ck.ckks_rmsnorm(ctx, out, None, to_dev(ct), to_dev(ct), to_dev(full[:2]), -1, -1, -1, [-1], rows, nl, n1, n2, p.N // 8, *dk,
+                            ctx.rmsnorm_workspace(rows, nl, n1, n2, 1))
+            assert_same(to_host(out), want, "norm " + name)
+
+
+def test_a_prompt_then_tokens_then_the_norm():
+    """As a model runs them: chunks and single tokens on the same cache, pages handed out as it grows and given back as the window leaves
+    them, a shared prefix, the norm of the result with the stream of residuals. A chunk and its tokens one by one agree."""
+    import paper_2604_03425_amd as ck
+    p, rc, ctx = contexts("ring13")
+    n1, n2, nl, page, window, sinks, T = 2, 2, 5, 2, 3, 1, 9
+    L = nl - 2
+    s = attention_ref.Shape(p, rc, n1, n2, p.N // 8, seed=77)
+    q, k, v = (s.cts((T,), nl) for _ in range(3))
+    keys = device_keys(s)
+    dq, dk, dv = (to_dev(x) for x in (q, k, v))
+    want = decoder_ref.attention(s, q, [k], [v], [T], window, sinks, 9, 1)
+
+    def run(chunks, seqs):
+        pages = {}
+        outs, done = [], 0
+        for n in chunks:
+            lens, new = [done + n] * seqs, [n] + [0] * (seqs - 1)
+            for i in range(done // page, -(-(done + n) // page)):
+                pages.setdefault(i, (torch.full((page, 2, nl, p.N), -1, dtype=torch.int64, device="cuda"),
+                                     torch.full((page, 2, L, p.N), -1, dtype=torch.int64, device="cuda")))
+            table = [pages.get(i, (None, None)) for i in range(-(-(done + n) // page))] * seqs    # the other sequences share all of it
+            kp, vp = [x for x, _ in table], [x for _, x in table]
+            ck.ckks_kv_append(ctx, dk[done:done + n], dv[done:done + n], nl, new, lens, kp, vp, page, nl, L)
+            o = torch.empty((n, 2, L, p.N), dtype=torch.int64, device="cuda")
+            ck.ckks_attn_paged(ctx, o, dq[done:done + n], nl, new, lens, kp, vp, page, nl, L, window, sinks, 9, 1, n1, n2, p.N // 8, *keys,
+                               ctx.attn_workspace(n, ck.attn_pairs(new, lens, window, sinks), nl, n1, n2, 1))
+            outs.append(o)
+            done += n
+            for i in list(pages):
+                if i * page >= sinks and (i + 1) * page <= done - window + 1:      # no later token sees it
+                    del pages[i]
+        assert len(pages) < -(-T // page)
+        return torch.cat(outs)
+
+    for chunks, seqs in (([T], 1), ([1] * T, 1), ([4, 1, 1, 3], 2), ([2, 5, 2], 1)):
+        if chunks == [T]:
+            assert_same(to_host(run([5, 4], 1)), want, "chunks")
+        else:
+            assert_same(to_host(run(chunks, seqs)), want, "tokens")
+    o = run([6, 3], 1)
+    x = s.cts((T,), L)
+    w = s.draw(p.q[:L], ())
+    # a norm that takes the attention's limbs, without steps: L - 1 limbs, the gain at L
+    ref_out, ref_h = decoder_ref.rmsnorm(s, x, want, w, 3, 4, 5, [])
+    out, h = torch.empty((T, 2, L - 1, p.N), dtype=torch.int64, device="cuda"), torch.empty_like(o)
+    ck.ckks_rmsnorm(ctx, out, h, to_dev(x), o, to_dev(w), 3, 4, 5, [], T, L, n1, n2, p.N // 8, *keys, ctx.rmsnorm_workspace(T, L, n1, n2, 0))
+    assert_same(to_host(out), ref_out, "norm")
+    assert_same(to_host(h), ref_h, "sum")
+
+
+def test_on_another_stream_and_in_graphs():
+    """The calls enqueue on the current stream alone and allocate nothing; two captured graphs that share a workspace, replayed in turn on new
+    inputs with eager work between them, give what eager calls give."""
+    import paper_2604_03425_amd as ck
+    for name in ("ring12", "ring13", "ring10"):
+        p, rc, ctx = contexts(name)
+        n1 = n2 = 2
+        nl, page, lens, new = 4, 2, [3, 2], [1, 1]
+        s = attention_ref.Shape(p, rc, n1, n2, p.N // 8, seed=9)
+        keys = device_keys(s)
+        table = [torch.empty((page, 2, nl, p.N), dtype=torch.int64, device="cuda") for _ in range(6)]
+        kp, vp = table[:3], table[3:]
+        need = max(ck.ckks_attn_workspace_bytes(ctx, 2, 5, nl, n1, n2, 1), ck.ckks_rmsnorm_workspace_bytes(ctx, 2, nl, n1, n2, 1))
+        ws = torch.empty(need // 8, dtype=torch.int64, device="cuda")
+        q, k, v, x = (torch.empty((2, 2, nl, p.N), dtype=torch.int64, device="cuda") for _ in range(4))
+        o, out, h = (torch.empty((2, 2, n, p.N), dtype=torch.int64, device="cuda") for n in (nl - 2, 1, nl))
+
+        def attend():
+            ck.ckks_kv_append(ctx, k, v, nl, new, lens, kp, vp, page, nl, nl)
+            ck.ckks_attn_paged(ctx, o, q, nl, new, lens, kp, vp, page, nl, nl, 0, 0, 7, 1, n1, n2, p.N // 8, *keys, ws)
+
+        def norm():
+            ck.ckks_rmsnorm(ctx, out, h, x, q, None, 3, 4, 5, [6], 2, nl, n1, n2, p.N // 8, *keys, ws)
+
+        def fill(seed):
+            s.seed = 1000 * seed
+            for t in (q, k, v, x):
+                t.copy_(to_dev(s.cts((2,), nl)))
+            for t in table:
+                t.copy_(to_dev(s.cts((page,), nl)))
+            for t in (o, out, h):
+                t.fill_(-1)
+            ws.random_()
+            torch.cuda.synchronize()
+
+        def expected(seed):
+            fill(seed)
+            attend(), norm()
+            torch.cuda.synchronize()
+            return [t.clone() for t in (o, out, h, *table)]
+
+        def check(want, what):
+            torch.cuda.synchronize()
+            for a, b in zip((o, out, h, *table), want):
+                assert torch.equal(a, b), (name, what)
+
+        want = expected(1)
+        fill(1)
+        side = torch.cuda.Stream()
+        before = torch.cuda.memory_allocated()
+        with torch.cuda.stream(side):
+            attend(), norm()
+        check(want, "side stream")
+        assert torch.cuda.memory_allocated() == before
+        graphs = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graphs[0]):
+            attend()
+        with torch.cuda.graph(graphs[1]):
+            norm()
+        for trial in range(2, 5):
+            want = expected(trial)          # eager calls between the replays
+            fill(trial)
+            graphs[trial % 2].replay()
+            graphs[1 - trial % 2].replay()
+            check(want, trial)
+
+
+@pytest.mark.parametrize("knob,value", [(0, 0), (1, 1), (2, 1), (2, 2), (3, 1), (4, 0), (5, 1)])
+@pytest.mark.parametrize("name", ["ring12", "ring13_mixed", "ring16"])
+def test_tuning_knobs_change_no_result(name, knob, value):
+    import paper_2604_03425_amd as ck
+    p, rc, ctx = contexts(name)
+    default = {0: -1, 1: 0, 2: 0, 3: 2, 4: 1, 5: 0}[knob]
+    ck.ckks_tune_set(ctx, knob, value)
+    try:
+        run_attention(name, 4, (3,), (1,), 2, 0, 0, 1, 2, 2)
+        run_norm(name, 4, 2, 2, 2, 1, True, True)
+    finally:
+        ck.ckks_tune_set(ctx, knob, default)
+
+
+def test_small_primes_as_integers():
+    """Main primes below 2^36, which knob 1 gives integer bodies: the divisions' conversion leaves the fused kernel then."""
+    import paper_2604_03425_amd as ck
+    PARAMS.setdefault("ring13_small", lambda: make_params(13, 4, 34, 2, 40, 2))
+    p, rc, ctx = contexts("ring13_small")
+    for value in (0, 1, 0):
+        ck.ckks_tune_set(ctx, 1, value)
+        run_attention("ring13_small", 4, (3,), (1,), 2, 0, 0, 1, 2, 2, bias=1 << 60)
+        run_norm("ring13_small", 4, 2, 2, 2, 1, True, True)
+
+
+def test_a_cache_beyond_2_to_32_words():
+    """One allocation of 40 GB for all pages: tokens at its end alone give the same as in a small cache."""
+    import paper_2604_03425_amd as ck
+    p, rc, ctx = contexts("ring16")
+    nl, page, N = 5, 64, p.N
+    pages = 120
+    k = torch.empty((pages, page, 2, nl, N), dtype=torch.int64, device="cuda")
+    assert k.numel() > 1 << 32
+    gen = torch.Generator(device="cuda").manual_seed(3)
+
+    def residues(lead, moduli):
+        x = torch.empty(tuple(lead) + (len(moduli), N), dtype=torch.int64, device="cuda")
+        for i, m in enumerate(moduli):
+            x[..., i, :].random_(0, m, generator=gen)
+        return x
+
+    key = residues((p.dnum, 2), p.moduli)
+    last = residues((2, 2), p.q)
+    first = residues((1, 2), p.q)
+    v = residues((3, 2), p.q)
+    q = residues((1, 2), p.q)
+    # a sequence as long as the cache; sinks on its first page, the window on its last
+    n = pages * page
+    vt = torch.empty((page, 2, nl, N), dtype=torch.int64, device="cuda")
+    ve = torch.empty_like(vt)
+    kp, vp = [None] * pages, [None] * pages
+    kp[0], kp[-1], vp[0], vp[-1] = k[0], k[-1], vt, ve
+    k[0, 0], vt[0], k[-1, -2], ve[-2] = first[0], v[0], last[0], v[1]
+    ck.ckks_kv_append(ctx, last[1:], v[2:], nl, [1], [n], kp, vp, page, nl, nl)
+    assert torch.equal(k[-1, -1], last[1]) and torch.equal(ve[-1], v[2])
+    args = (9, 1, 1, 1, 1, key, [], [], ctx.attn_workspace(1, 3, nl, 1, 1, 1))
+    o, small = (torch.empty((1, 2, nl - 2, N), dtype=torch.int64, device="cuda") for _ in range(2))
+    ck.ckks_attn_paged(ctx, o, q, nl, [1], [n], kp, vp, page, nl, nl, 2, 1, *args)
+    few = torch.cat([first, last]).contiguous()
+    ck.ckks_attn_paged(ctx, small, q, nl, [1], [3], [few], [v], 3, nl, nl, 2, 1, *args)
+    torch.cuda.synchronize()
+    assert torch.equal(o, small)
+    # and as one flat page, whose last tokens lie beyond 2^32 words
+    flat = k.view(1, n, 2, nl, N)[0]
+    ck.ckks_attn_paged(ctx, small, q, nl, [1], [n], [flat], [flat], n, nl, nl, 2, 1, *args)
+    tail = torch.cat([flat[:1], flat[-2:]]).contiguous()
+    ck.ckks_attn_paged(ctx, o, q, nl, [1], [3], [tail], [tail], 3, nl, nl, 2, 1, *args)
+    torch.cuda.synchronize()
+    assert torch.equal(o, small)
+    del k, kp, flat
+    torch.cuda.empty_cache()
+
+
+def test_the_binding_refuses():
+    import paper_2604_03425_amd as ck
+    p, rc, ctx = contexts("ring10")
+    N, nl = p.N, 4
+    new = lambda *shape: torch.zeros(shape, dtype=torch.int64, device="cuda")   # noqa: E731
+    key = new(p.dnum, 2, len(p.moduli), N)
+    page, ct = new(2, 2, nl, N), new(1, 2, nl, N)
+    ws = ctx.attn_workspace(1, 3, nl, 1, 2, 1)
+    good = dict(o_out=new(1, 2, 2, N), q=ct, nlimbs=nl, new_lens=[1], lens=[3], k_pages=[page, page], v_pages=[page, page], page_tokens=2,
+                k_limbs=nl, v_limbs=nl, window=0, sinks=0, bias=1, squarings=1, n1=1, n2=2, stride=N // 4, evk_mult=key, evk_baby=[],
+                evk_giant=[key], ws=ws)
+    ck.ckks_attn_paged(ctx, **good)
+    for error, change in ((ValueError, dict(k_pages=[page])), (ValueError, dict(evk_baby=[key])), (ValueError, dict(new_lens=[1, 0])),
+                          (ValueError, dict(k_pages=[page, page[:1]])), (ValueError, dict(o_out=new(1, 2, 1, N))), (ValueError, dict(lens=[-1])),
+                          (ValueError, dict(q=ct[:, :1].contiguous())), (TypeError, dict(q=ct.cpu())), (TypeError, dict(v_pages=[page, page.float()])),
+                          (TypeError, dict(k_pages=[page, page.transpose(0, 1)])), (ValueError, dict(evk_mult=key[:1])), (ValueError, dict(page_tokens=0)),
+                          (ck.CkksError, dict(k_pages=[None, page])), (ck.CkksError, dict(squarings=3, o_out=new(1, 2, 2, N)))):
+        with pytest.raises(error):
+            ck.ckks_attn_paged(ctx, **dict(good, **change))
+    with pytest.raises(ck.CkksError):
+        ctx.attn_workspace(1, 0, nl, 1, 2, 1)
+    with pytest.raises(ck.CkksError):
+        ctx.rmsnorm_workspace(1, 3, 1, 2, 1)
+    app = dict(k=ct, v=ct, in_limbs=nl, new_lens=[1], lens=[3], k_pages=[None, page], v_pages=[None, new(2, 2, nl, N)], page_tokens=2, k_limbs=nl, v_limbs=nl)
+    ck.ckks_kv_append(ctx, **app)
+    for error, change in ((ValueError, dict(k=ct[:, :1].contiguous())), (ck.CkksError, dict(v_pages=[None, page])), (ck.CkksError, dict(k=page)),
+                          (TypeError, dict(v=None))):
+        with pytest.raises(error):
+            ck.ckks_kv_append(ctx, **dict(app, **change))
+    norm = dict(ct_out=new(1, 2, 1, N), h_out=new(1, 2, nl, N), ct_x=ct, ct_res=new(1, 2, nl, N), gain=new(2, N), square=1, eps=0, start=5, factors=[3],
+                B=1, nlimbs=nl, n1=1, n2=2, stride=N // 4, evk_mult=key, evk_baby=[], evk_giant=[key], ws=ctx.rmsnorm_workspace(1, nl, 1, 2, 1))
+    ck.ckks_rmsnorm(ctx, **norm)
+    for error, change in ((ValueError, dict(ct_out=new(1, 2, 1, N // 2))), (ValueError, dict(gain=new(1, N))), (ValueError, dict(evk_giant=[])),
+                          (ck.CkksError, dict(factors=[3, 3])), (TypeError, dict(ct_res=ct.cpu())), (ck.CkksError, dict(ct_out=norm["h_out"]))):
+        with pytest.raises(error):
+            ck.ckks_rmsnorm(ctx, **dict(norm, **change))
