@@ -2,6 +2,7 @@
 // sums, the giant steps of a state's read) and sums of ciphertext products (scores, the state's update and read).
 #pragma once
 #include "ntt16_kernels.hip.h"
+#include "radix4.hip.h"
 
 #define ROT_SUM_TERMS 32   // terms per launch (they travel in the kernel's arguments)
 
@@ -27,6 +28,10 @@ struct RotSumArgs {
   u64 d_stride;
   u32 logN, nlimbs, nq, nm, alpha, beta, next, B, nterms, w_first, w_terms, per_set, accumulate, nfp;
   u32 doubles;          // != 0: ext holds doubles on moduli below 2^50
+  // block_sum_kernel, FUSED: twiddles; integer slots from first_special on go through their inverse block pass if `inverse` says so
+  const ulonglong2 *tw = nullptr, *twi = nullptr;
+  const double* twfp = nullptr;
+  u32 first_special = 0, inverse = 0;
   unsigned char slots[128];
   RotTerm term[ROT_SUM_TERMS];
 };
@@ -252,38 +257,170 @@ __global__ void __launch_bounds__(256) rot_sum_kernel(RotSumArgs a) {
 // Doubles: digits within q / 2, key words below q < 2^50, so that four products stay within 2^101 of H = 1.5 * 2^102, in whose binade
 // sums are multiples of 2^50 and what a product loses in joining H is exact and goes to L: 4 instructions a term, 6 every fourth.
 #define BLOCK_SUM 256
+// The last 8 stages of a transform on a block of 256 elements in one wave, four values a lane: round K (stages 2K, 2K + 1 of the block)
+// holds in lane l the elements (l / S) 4S + i S + l % S, S = 64 >> 2K.
+__device__ __forceinline__ u32 block_lane() {   // hidden, so that what is derived from it is not kept in registers from digit to digit
+  u32 l = threadIdx.x & 63;
+  asm volatile("" : "+v"(l));
+  return l;
+}
+__device__ __forceinline__ u32 block_elem(int K, u32 i, u32 l) {
+  const u32 s = 6 - 2 * K;
+  return ((l >> s) << (s + 2)) + (i << s) + (l & ((1u << s) - 1));
+}
+template <int FROM, int TO, class T>
+__device__ __forceinline__ void block_exchange(T (&x)[4], T* blk) {
+  const u32 l = block_lane();
+#pragma unroll
+  for (int i = 0; i < 4; i++) blk[wl_word(block_elem(FROM, i, l))] = x[i];
+  wave_lds_sync();
+#pragma unroll
+  for (int i = 0; i < 4; i++) x[i] = blk[wl_word(block_elem(TO, i, l))];
+  wave_lds_sync();
+  __builtin_amdgcn_sched_barrier(0);
+}
+// Twiddles of block h of R, stage s, group g at (1 << s) - 1 + g.
+template <class TW>
+__device__ __forceinline__ void block_twiddles_fetch(TW* tws, const TW* __restrict__ tw, u32 h, u32 R) {
+  const u32 t = min(threadIdx.x, 254u), s = 31 - __clz(t + 1);
+  tws[t] = tw[(R << s) + (h << s) + (t + 1 - (1u << s))];
+}
+template <class TW>
+__device__ __forceinline__ void block_twiddles(TW (&w)[3], const TW* tws, int K) {
+  const u32 g = block_lane() >> (6 - 2 * K);
+  w[0] = tws[(1u << (2 * K)) - 1 + g];
+  w[1] = tws[(2u << (2 * K)) - 1 + 2 * g];
+  w[2] = tws[(2u << (2 * K)) + 2 * g];
+}
+// In: round 0's elements, at most 2.64 q (integers: below 16q, SMALL 33q). Out: round 3's, reduced (canonical).
+__device__ __forceinline__ void block_forward(double (&x)[4], const double* tws, double q, double qinv, double* blk) {
+  double w[3];
+  block_twiddles(w, tws, 0);
+  radix4_fwd(x, w, q, qinv);
+  block_exchange<0, 1>(x, blk);
+  block_twiddles(w, tws, 1);
+  radix4_fwd(x, w, q, qinv);
+  reduce4(x, q, qinv);
+  block_exchange<1, 2>(x, blk);
+  block_twiddles(w, tws, 2);
+  radix4_fwd(x, w, q, qinv);
+  block_exchange<2, 3>(x, blk);
+  block_twiddles(w, tws, 3);
+  radix4_fwd(x, w, q, qinv);
+  reduce4(x, q, qinv);
+}
+template <bool BIG>
+__device__ __forceinline__ void block_forward(u64 (&x)[4], const ulonglong2* tws, u64 q, u64 mu, u64* blk) {
+  const u64 q2 = lazy_const<BIG>(q);
+  ulonglong2 w[3];
+  block_twiddles(w, tws, 0);
+  radix4_fwd<BIG>(x, w, q, q2);
+  block_exchange<0, 1>(x, blk);
+  block_twiddles(w, tws, 1);
+  radix4_fwd<BIG>(x, w, q, q2);
+  block_exchange<1, 2>(x, blk);
+  block_twiddles(w, tws, 2);
+  radix4_fwd<BIG>(x, w, q, q2);
+  block_exchange<2, 3>(x, blk);
+  block_twiddles(w, tws, 3);
+  radix4_fwd<BIG>(x, w, q, q2);
+#pragma unroll
+  for (int i = 0; i < 4; i++) x[i] = csub(fwd_settle<BIG>(x[i], mu, q), q);
+}
+// In: round 3's elements, canonical. Out: round 0's, below 8q (SMALL 2q).
+template <bool BIG>
+__device__ __forceinline__ void block_inverse(u64 (&x)[4], const ulonglong2* tws, u64 q, u64 mu, u64* blk) {
+  const u64 q2 = lazy_const<BIG>(q);
+  ulonglong2 w[3];
+  block_twiddles(w, tws, 3);
+  radix4_inv<BIG>(x, w, q, q2);
+  block_exchange<3, 2>(x, blk);
+  block_twiddles(w, tws, 2);
+  radix4_inv<BIG>(x, w, q, BIG ? q2 : q2 << 2);
+  block_exchange<2, 1>(x, blk);
+  block_twiddles(w, tws, 1);
+  radix4_inv<BIG>(x, w, q, BIG ? q2 : q2 << 4);
+  block_exchange<1, 0>(x, blk);
+  block_twiddles(w, tws, 0);
+  radix4_inv<BIG>(x, w, q, BIG ? q2 : q2 << 6);
+  if (!BIG) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) x[i] = barrett_lazy(x[i], mu, q);
+  }
+}
 #define BLOCK_SUM_AHEAD 4
-// Walks over the terms, digit by digit and rotation by rotation, with the key words requested BLOCK_SUM_AHEAD terms ahead (what a
-// workgroup waits for is their way from memory, which the others that share them wait for too). begin(j) puts digit j into LDS,
-// term(e0, e1, m) multiplies by the words of both components what lies at index m of the block.
+// Walks over the terms, digit by digit and rotation by rotation, with the key words requested BLOCK_SUM_AHEAD rotations ahead, across the
+// digits' ends (what a workgroup waits for is their way from memory, which the others that share them wait for too). begin(j) puts
+// digit j into LDS, term(e0, e1, m) multiplies by the words of both components what lies at index m of the block.
 template <class Begin, class Term>
 __device__ __forceinline__ void block_sum_terms(const RotSumArgs& a, size_t at, size_t comp, u32 n, Begin begin, Term term) {
-  const u32 R = a.nterms, total = R * a.beta;
+  const u32 R = a.nterms;
   u64 k0[BLOCK_SUM_AHEAD], k1[BLOCK_SUM_AHEAD];
-  u32 rr = 0, jj = 0;   // the next term to request
-  auto request = [&](int u) {
-    const u64* e = uniform_ptr(a.term[rr].evk) + (size_t)min(jj, a.beta - 1) * 2 * comp + at;
+  auto request = [&](int u, u32 r, u32 j) {
+    if (r >= R || j >= a.beta) return;   // uniform
+    const u64* e = uniform_ptr(a.term[r].evk) + (size_t)j * 2 * comp + at;
     k0[u] = e[0], k1[u] = e[comp];
-    if (++rr == R) rr = 0, jj++;
   };
 #pragma unroll
-  for (int u = 0; u < BLOCK_SUM_AHEAD; u++) request(u);
-  u32 r = 0, j = 0;
+  for (int u = 0; u < BLOCK_SUM_AHEAD; u++) request(u, u, 0);
 #pragma nounroll
-  for (u32 i = 0; i < total; i += BLOCK_SUM_AHEAD) {
+  for (u32 j = 0; j < a.beta; j++) {
+    begin(j);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma nounroll
+    for (u32 r = 0; r < R; r += BLOCK_SUM_AHEAD) {
+      const bool more = r + BLOCK_SUM_AHEAD < R;
 #pragma unroll
-    for (int u = 0; u < BLOCK_SUM_AHEAD; u++) {
-      if (i + u >= total) break;   // uniform
-      if (r == 0) begin(j);
-      term(k0[u], k1[u], galois_src_index(n, a.term[r].galois, a.logN) & (BLOCK_SUM - 1));
-      request(u);
-      if (++r == R) r = 0, j++;
-      __builtin_amdgcn_sched_barrier(0);
+      for (int u = 0; u < BLOCK_SUM_AHEAD; u++) {
+        if (r + u >= R) break;   // uniform
+        term(k0[u], k1[u], galois_src_index(n, a.term[r + u].galois, a.logN) & (BLOCK_SUM - 1));
+        request(u, more ? r + BLOCK_SUM_AHEAD + u : u, more ? j : j + 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (more) {   // places that the last rotations of a digit leave: the next one's
+#pragma unroll
+        for (int u = 0; u < BLOCK_SUM_AHEAD; u++)
+          if (r + BLOCK_SUM_AHEAD + u >= R) request(u, u, j + 1);
+      }
     }
   }
 }
-template <int CB>
-__device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 blk, u32 zi, u64* sm) {
+// FUSED: ext comes from the first pass of the digits' transform. A wave takes a block of a ciphertext's digit through the second one on
+// its way into LDS, as many digits at a time as there are waves for.
+template <int CB, bool FUSED>
+constexpr u32 block_sum_fill() { return !FUSED ? 1 : CB == 1 ? 4 : CB == 2 ? 2 : 1; }
+// The words of a fill that a lane moves: with FUSED four of its wave's block, else one of each ciphertext.
+template <int CB, bool FUSED>
+struct BlockFill {
+  static constexpr u32 DIGITS = block_sum_fill<CB, FUSED>(), WORDS = FUSED ? 4 : CB;
+  u64 w[WORDS];
+  u32 b;         // FUSED: the wave's ciphertext, and its digit among those of a fill
+  u32 digit;
+  bool active;
+  __device__ __forceinline__ BlockFill(u32 b0, u32 B) {
+    const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    digit = wave / CB;
+    active = wave < DIGITS * CB;
+    b = min(b0 + wave % CB, B - 1);
+  }
+  // ext, d: at the block's first word of ciphertext and digit 0
+  __device__ __forceinline__ void request(const RotSumArgs& a, const u64* ext, const u64* d, const u32 (&bb)[CB], u32 j, u32 jo) {
+    const size_t N = (size_t)1 << a.logN;
+    if (FUSED) {
+      const u32 jj = min(j + digit, a.beta - 1);
+      const u32 l = block_lane();
+      const u64* p = uniform_ptr(jj == jo ? d + (size_t)b * a.d_stride : ext + ((size_t)b * a.beta + jj) * a.next * N);
+#pragma unroll
+      for (u32 i = 0; i < 4; i++) w[i % WORDS] = p[block_elem(0, i, l)];
+    } else {
+#pragma unroll
+      for (int k = 0; k < CB; k++)
+        w[k % WORDS] = (j == jo ? d + (size_t)bb[k] * a.d_stride : ext + ((size_t)bb[k] * a.beta + j) * a.next * N)[threadIdx.x];
+    }
+  }
+};
+template <int CB, bool FUSED>
+__device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 blk, u32 zi, u64* sm, ulonglong2* tws_) {
   constexpr double M = 1.5 * 5070602400912917605986812821504.0;   // 1.5 * 2^102
   const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, comp = (size_t)a.nm * N;
   const u32 tid = threadIdx.x, n = blk * BLOCK_SUM + tid, t = a.slots[zi], b0 = what * CB;
@@ -291,7 +428,7 @@ __device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 
   const u32 id = main_prime ? t : t - a.nlimbs + a.nq;
   const ModInfo mi = a.mods[id];
   const double q = mi.qd, qinv = mi.qinv;
-  const u64 *ext = a.term[0].ext + (size_t)t * N + n, *d = a.term[0].d + (size_t)t * N + n;
+  const u64 *ext = a.term[0].ext + (size_t)t * N + blk * BLOCK_SUM, *d = a.term[0].d + (size_t)t * N + blk * BLOCK_SUM;
   const u32 jo = main_prime ? t / a.alpha : 0xFFFFFFFFu;   // the digit that holds limb t itself
   u32 bb[CB];   // surplus places repeat the last ciphertext and store nothing
   double H0[CB], L0[CB], H1[CB], L1[CB];
@@ -306,35 +443,56 @@ __device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 
     L = __builtin_fma(-__builtin_rint(__builtin_fma(L, qinv, h * qinv)), q, h) + L;   // at most 1.3 q
     H = M;
   };
-  double* tile = (double*)sm;
-  u64 ahead[CB];
-  auto request = [&](u32 j) {
-#pragma unroll
-    for (int k = 0; k < CB; k++)
-      ahead[k] = j == jo ? d[(size_t)bb[k] * a.d_stride] : ext[((size_t)bb[k] * a.beta + j) * a.next * N];
-  };
+  typedef BlockFill<CB, FUSED> Fill;
+  double *tile = (double*)sm, *digit = tile;
+  Fill fill(b0, a.B);
+  double* const tws = (double*)tws_;
+  if (FUSED) block_twiddles_fetch(tws, a.twfp + (size_t)id * N, blk, (u32)(N / BLOCK_SUM));
   const u32 R = a.nterms;
-  request(0);
+  fill.request(a, ext, d, bb, 0, jo);
+  if (FUSED) lds_barrier();
   u32 count = 0;
   block_sum_terms(
       a, (size_t)id * N + n, comp, n,
       [&](u32 j) {
-        const u64 bias = j == jo ? 0x4330000000000000ull : 0ull;   // residues become doubles, doubles stay what they are
-        const double less = __longlong_as_double((long long)bias);
-        if (j) tile = (double*)sm + (tile == (double*)sm ? CB * BLOCK_SUM : 0);
+        const u32 place = j % Fill::DIGITS;
+        if (place == 0) {
+          if (j) tile = (double*)sm + (tile == (double*)sm ? Fill::DIGITS * CB * BLOCK_SUM : 0);
+          if (FUSED) {
+            if (fill.active) {
+              double* to = tile + (threadIdx.x >> 6) * BLOCK_SUM;
+              double x[4];
+              const u32 l = block_lane();
+              if (j + fill.digit == jo) {   // uniform
 #pragma unroll
-        for (int k = 0; k < CB; k++) {
-          const double v = __longlong_as_double((long long)(ahead[k] | bias)) - less;
-          tile[k * BLOCK_SUM + tid] = j == jo ? fp_reduce(v, qinv, q) : v;
+                for (u32 i = 0; i < 4; i++) to[block_elem(0, i, l)] = fp_reduce(u2d(fill.w[i % Fill::WORDS]), qinv, q);
+              } else {
+#pragma unroll
+                for (u32 i = 0; i < 4; i++) x[i] = __longlong_as_double((long long)fill.w[i % Fill::WORDS]);
+                block_forward(x, tws, q, qinv, to);
+#pragma unroll
+                for (u32 i = 0; i < 4; i++) to[block_elem(3, i, l)] = x[i];
+              }
+            }
+          } else {
+            const u64 bias = j == jo ? 0x4330000000000000ull : 0ull;   // residues become doubles, doubles stay what they are
+            const double less = __longlong_as_double((long long)bias);
+#pragma unroll
+            for (int k = 0; k < CB; k++) {
+              const double v = __longlong_as_double((long long)(fill.w[k % Fill::WORDS] | bias)) - less;
+              tile[k * BLOCK_SUM + tid] = j == jo ? fp_reduce(v, qinv, q) : v;
+            }
+          }
+          lds_barrier();   // the other tile's readers are past it, since they have written this one
+          if (j + Fill::DIGITS < a.beta) fill.request(a, ext, d, bb, j + Fill::DIGITS, jo);
         }
-        lds_barrier();   // the other tile's readers are past it, since they have written this one
-        if (j + 1 < a.beta) request(j + 1);
+        digit = tile + place * CB * BLOCK_SUM;
       },
       [&](u64 k0, u64 k1, u32 m) {
         const double e0 = u2d(k0), e1 = u2d(k1);
 #pragma unroll
         for (int k = 0; k < CB; k++) {
-          const double x = tile[k * BLOCK_SUM + m];
+          const double x = digit[k * BLOCK_SUM + m];
           const double p0 = __builtin_fma(x, e0, H0[k]), h0 = p0 - H0[k];
           L0[k] += __builtin_fma(x, e0, -h0);
           H0[k] = p0;
@@ -347,7 +505,7 @@ __device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 
           for (int k = 0; k < CB; k++) settle(H0[k], L0[k]), settle(H1[k], L1[k]);
         }
       });
-  tile = (double*)sm + (tile == (double*)sm ? CB * BLOCK_SUM : 0);
+  tile = (double*)sm + (tile == (double*)sm ? Fill::DIGITS * CB * BLOCK_SUM : 0);
   if (main_prime) {   // P (base + sum of the rotated first components), P base
     const u64* c0 = a.term[0].c0 + (size_t)t * N + n;
     double v[CB];
@@ -388,15 +546,15 @@ __device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 
   }
 }
 // Integer moduli (PLAIN: all of them, acc without the factor 2^-64): 30-bit halves, 4 multiply-adds a term and carries every 11.
-template <int CB, bool PLAIN>
-__device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32 blk, u32 zi, u64* tile) {
+template <int CB, bool PLAIN, bool FUSED>
+__device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32 blk, u32 zi, u64* tile, ulonglong2* tws) {
   const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, comp = (size_t)a.nm * N;
   const u32 tid = threadIdx.x, n = blk * BLOCK_SUM + tid, t = a.slots[zi], b0 = what * CB;
   const bool main_prime = t < a.nlimbs;
   const u32 id = main_prime ? t : t - a.nlimbs + a.nq;
   const ModInfo mi = a.mods[id];
   const u64 q = mi.m, nm = neg_opaque(q);
-  const u64 *ext = a.term[0].ext + (size_t)t * N + n, *d = a.term[0].d + (size_t)t * N + n;
+  const u64 *ext = a.term[0].ext + (size_t)t * N + blk * BLOCK_SUM, *d = a.term[0].d + (size_t)t * N + blk * BLOCK_SUM;
   const u32 jo = main_prime ? t / a.alpha : 0xFFFFFFFFu;
   u64* const sm = tile;
   u32 bb[CB];
@@ -407,14 +565,14 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
     dot30_init(s0[k]);
     dot30_init(s1[k]);
   }
-  u64 ahead[CB];
-  auto request = [&](u32 j) {
-#pragma unroll
-    for (int k = 0; k < CB; k++)
-      ahead[k] = j == jo ? d[(size_t)bb[k] * a.d_stride] : ext[((size_t)bb[k] * a.beta + j) * a.next * N];
-  };
+  typedef BlockFill<CB, FUSED> Fill;
+  u64* digit = tile;
+  Fill fill(b0, a.B);
+  const bool big = (q >> 52) != 0;   // uniform
+  if (FUSED) block_twiddles_fetch(tws, a.tw + (size_t)id * N, blk, (u32)(N / BLOCK_SUM));
   const u32 R = a.nterms;
-  request(0);
+  fill.request(a, ext, d, bb, 0, jo);
+  if (FUSED) lds_barrier();
   u32 count = 0;
   auto carry = [&] {
     if (++count < 11) return;
@@ -425,24 +583,46 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
   block_sum_terms(
       a, (size_t)id * N + n, comp, n,
       [&](u32 j) {
-        if (j) tile = sm + (tile == sm ? CB * BLOCK_SUM : 0);
+        const u32 place = j % Fill::DIGITS;
+        if (place == 0) {
+          if (j) tile = sm + (tile == sm ? Fill::DIGITS * CB * BLOCK_SUM : 0);
+          if (FUSED) {
+            if (fill.active) {
+              u64 *to = tile + (threadIdx.x >> 6) * BLOCK_SUM, x[4];
+              const u32 l = block_lane();
 #pragma unroll
-        for (int k = 0; k < CB; k++) tile[k * BLOCK_SUM + tid] = ahead[k];
-        lds_barrier();
-        if (j + 1 < a.beta) request(j + 1);
+              for (u32 i = 0; i < 4; i++) x[i] = fill.w[i % Fill::WORDS];
+              if (j + fill.digit == jo) {   // uniform
+#pragma unroll
+                for (u32 i = 0; i < 4; i++) to[block_elem(0, i, l)] = x[i];
+              } else {
+                if (big) block_forward<true>(x, tws, q, mi.mu64, to);
+                else block_forward<false>(x, tws, q, mi.mu64, to);
+#pragma unroll
+                for (u32 i = 0; i < 4; i++) to[block_elem(3, i, l)] = x[i];
+              }
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < CB; k++) tile[k * BLOCK_SUM + tid] = fill.w[k % Fill::WORDS];
+          }
+          lds_barrier();
+          if (j + Fill::DIGITS < a.beta) fill.request(a, ext, d, bb, j + Fill::DIGITS, jo);
+        }
+        digit = tile + place * CB * BLOCK_SUM;
       },
       [&](u64 k0, u64 k1, u32 m) {
         const u32 e00 = (u32)k0 & M30, e01 = (u32)(k0 >> 30), e10 = (u32)k1 & M30, e11 = (u32)(k1 >> 30);
 #pragma unroll
         for (int k = 0; k < CB; k++) {
-          const u64 x = tile[k * BLOCK_SUM + m];
+          const u64 x = digit[k * BLOCK_SUM + m];
           const u32 x0 = (u32)x & M30, x1 = (u32)(x >> 30);
           dot30_mac(s0[k], x0, x1, e00, e01);
           dot30_mac(s1[k], x0, x1, e10, e11);
         }
         carry();
       });
-  tile = sm + (tile == sm ? CB * BLOCK_SUM : 0);
+  tile = sm + (tile == sm ? Fill::DIGITS * CB * BLOCK_SUM : 0);
   if (main_prime) {
     const u64* c0 = a.term[0].c0 + (size_t)t * N + n;
     const u32 p0 = (u32)mi.pmod & M30, p1 = (u32)(mi.pmod >> 30);
@@ -467,9 +647,13 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
       }
     }
   }
+  const bool back = FUSED && a.inverse && t >= a.first_special;   // uniform
+  if (back) {
+    lds_barrier();   // the tiles and the twiddles have been read
+    block_twiddles_fetch(tws, a.twi + (size_t)id * N, blk, (u32)(N / BLOCK_SUM));
+  }
 #pragma unroll
   for (int k = 0; k < CB; k++) {
-    if (b0 + k >= a.B) break;
     u64* to = a.acc + ((size_t)bb[k] * 2 * a.next + t) * N + n;
 #pragma unroll
     for (int c = 0; c < 2; c++) {
@@ -477,19 +661,36 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
       dot30_settle(s, mi.mu64, nm);
       u64 v = PLAIN ? reduce128(dot30_value(s), mi) : csub(csub(redc(dot30_value(s), q, mi.minv), q), q);
       u64* o = to + (size_t)c * a.next * N;
-      if (a.accumulate) v = addmod(v, *o, q);
-      *o = v;
+      if (a.accumulate && b0 + k < a.B) v = addmod(v, *o, q);
+      if (back) sm[(2 * k + c) * BLOCK_SUM + tid] = v;
+      else if (b0 + k < a.B) *o = v;
     }
+  }
+  if (!back) return;
+  lds_barrier();
+  for (u32 u = threadIdx.x >> 6; u < 2 * CB; u += 4) {   // a wave for each accumulator of a ciphertext
+    if (b0 + u / 2 >= a.B) break;
+    u64 *blk_sm = sm + u * BLOCK_SUM, x[4];
+    const u32 l = block_lane();
+#pragma unroll
+    for (u32 i = 0; i < 4; i++) x[i] = blk_sm[block_elem(3, i, l)];
+    wave_lds_sync();
+    if (big) block_inverse<true>(x, tws, q, mi.mu64, blk_sm);
+    else block_inverse<false>(x, tws, q, mi.mu64, blk_sm);
+    u64* o = a.acc + (((size_t)(b0 + u / 2) * 2 + u % 2) * a.next + t) * N + blk * BLOCK_SUM;
+#pragma unroll
+    for (u32 i = 0; i < 4; i++) o[block_elem(0, i, l)] = x[i];
   }
 }
 // Kinds as for rot_sum_kernel. grid = (ceil(B / CB), N / 256, slots)
-template <int KIND, int CB>
+template <int KIND, int CB, bool FUSED>
 __global__ void __launch_bounds__(BLOCK_SUM) block_sum_kernel(RotSumArgs a) {
-  __shared__ u64 sm[2 * CB * BLOCK_SUM];
+  __shared__ __attribute__((aligned(16))) u64 sm[2 * block_sum_fill<CB, FUSED>() * CB * BLOCK_SUM];
+  __shared__ ulonglong2 tws[FUSED ? BLOCK_SUM - 1 : 1];
   u32 what, blk, zi;
   attention_map(what, blk, zi);
-  if (KIND == 0 && zi < a.nfp) block_sum_fp<CB>(a, what, blk, zi, sm);
-  else block_sum_int<CB, KIND == 2>(a, what, blk, zi, sm);
+  if (KIND == 0 && zi < a.nfp) block_sum_fp<CB, FUSED>(a, what, blk, zi, sm, tws);
+  else block_sum_int<CB, KIND == 2, FUSED>(a, what, blk, zi, sm, tws);
 }
 
 // out[i][j][b] = sum_{s < ns} x(j, s)[b] * y(i, s)[b] in three components (+ add in the first two, or in all three), for i0 <= i < i1 and

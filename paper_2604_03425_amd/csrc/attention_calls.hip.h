@@ -31,12 +31,12 @@ u32 rotation_element(const ckks_ctx* c, u64 steps) {   // 5^steps mod 2N
 // in 3 digits 1012 and 880.
 // Digits of B polynomials in the extended basis, evaluation domain, at L.ext of the key-switch workspace: (b, limb t) is at
 // d + b * d_stride + t * N. Doubles on the double-precision moduli of the two-pass rings and of whole limbs, canonical residues elsewhere.
-// last_int (two-pass rings): limb nlimbs - 1 in residues whatever its class.
+// last_int (two-pass rings): limb nlimbs - 1 in residues whatever its class; rows_only (there): after the first pass of the transform.
 int ext_digits(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* d, u64 d_stride, u32 B, u32 nlimbs, char* ws, hipStream_t st,
-               bool last_int = false) {
+               bool last_int = false, bool rows_only = false) {
   int rc;
   FwdInnerArgs unused;
-  if (two_pass(c)) return hoist_front16(c, lt, d, d_stride, B, nlimbs, ws, st, unused, last_int);
+  if (two_pass(c)) return hoist_front16(c, lt, d, d_stride, B, nlimbs, ws, st, unused, last_int, rows_only);
   if (whole) {
     Ks12Args a = ks12_args(c, lt, B, nlimbs, ws);
     a.d = d;
@@ -59,11 +59,12 @@ int ext_digits(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* d, u64
 }
 
 // ModDown of both accumulators [B][2][next][N] (their special limbs are overwritten) to out [B][2][nlimbs][N].
-int ext_mod_down(ckks_ctx* c, const LevelTables* lt, bool whole, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
+int ext_mod_down(ckks_ctx* c, const LevelTables* lt, bool whole, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st,
+                 bool blocks_done = false) {
   int rc;
   if (two_pass(c)) {
     KsIo io{nullptr, 0, 0, out, {0, 0}, nullptr, 0};
-    return ks16_finish(c, lt, io, B, nlimbs, ws, st, acc);
+    return ks16_finish(c, lt, io, B, nlimbs, ws, st, acc, blocks_done);
   }
   if (whole) {
     Ks12Args a = ks12_args(c, lt, B, nlimbs, ws);
@@ -129,9 +130,11 @@ void launch_rot_sum_of(u32 outs, u32 slots, const RotSumArgs& a, hipStream_t st)
 template <int CB>
 void launch_block_sum_of(u32 slots, const RotSumArgs& a, hipStream_t st) {
   const dim3 grid((a.B + CB - 1) / CB, (1u << a.logN) / BLOCK_SUM, slots), block(BLOCK_SUM);
-  if (!a.doubles) hipLaunchKernelGGL((block_sum_kernel<2, CB>), grid, block, 0, st, a);
-  else if (a.nfp == 0) hipLaunchKernelGGL((block_sum_kernel<1, CB>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((block_sum_kernel<0, CB>), grid, block, 0, st, a);
+  if (a.tw && a.nfp) hipLaunchKernelGGL((block_sum_kernel<0, CB, true>), grid, block, 0, st, a);
+  else if (a.tw) hipLaunchKernelGGL((block_sum_kernel<1, CB, true>), grid, block, 0, st, a);
+  else if (!a.doubles) hipLaunchKernelGGL((block_sum_kernel<2, CB, false>), grid, block, 0, st, a);
+  else if (a.nfp == 0) hipLaunchKernelGGL((block_sum_kernel<1, CB, false>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((block_sum_kernel<0, CB, false>), grid, block, 0, st, a);
 }
 // Whether all rotations keep the blocks that block_sum_kernel holds.
 bool rotations_near(const ckks_ctx* c, const u32* galois, u32 R) {
@@ -164,12 +167,17 @@ int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 
   return CKKS_OK;
 }
 
-// acc = P w_0 ct + sum_r w_{r+1} (accumulators of the rotation of ct by galois[r]); ws: a key-switch workspace for B.
+// acc = P w_0 ct + sum_r w_{r+1} (accumulators of the rotation of ct by galois[r]); ws: a key-switch workspace for B. Returns in
+// *blocks_done (where given) whether the integer special limbs (and the last main one, where it goes with them: last_int, or an integer
+// one with `drop`) have been through their inverse block pass, which unweighted near rotations on two-pass rings do in their kernel.
 int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* ct, u32 B, u32 nlimbs, const u32* galois,
-                     const u64* const* evks, u32 R, const u64* w, u32 per_set, u64* acc, char* ws, hipStream_t st, bool last_int = false) {
+                     const u64* const* evks, u32 R, const u64* w, u32 per_set, u64* acc, char* ws, hipStream_t st, bool* blocks_done = nullptr,
+                     DropForm form = APART) {
   int rc;
   const u64 pl = (u64)nlimbs * c->N;
-  if (R && (rc = ext_digits(c, lt, whole, ct + pl, 2 * pl, B, nlimbs, ws, st, last_int))) return rc;
+  const bool last_int = form == JOINED_FORCED, near = !w && rotations_near(c, galois, R), fused = near && blocks_done && two_pass(c);
+  if (blocks_done) *blocks_done = fused;
+  if (R && (rc = ext_digits(c, lt, whole, ct + pl, 2 * pl, B, nlimbs, ws, st, last_int, fused))) return rc;
   const u64* ext = (const u64*)(ws + ks_layout(c, B, nlimbs).ext);
   RotSumArgs a = rot_sum_args(c, lt, whole, nlimbs, acc, 2 * pl);
   a.base = ct;
@@ -177,9 +185,10 @@ int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* 
   a.w = w;
   a.w_terms = R + 1;
   a.per_set = per_set;
-  const bool near = !w && rotations_near(c, galois, R);
+  if (fused) a.tw = c->d_tw_fwd, a.twi = c->d_tw_inv, a.twfp = c->d_twfp_fwd, a.first_special = form == APART ? nlimbs : nlimbs - 1;
   for (u32 r0 = 0; r0 == 0 || r0 < R; r0 += ROT_SUM_TERMS) {
     a.nterms = std::min<u32>(ROT_SUM_TERMS, R - r0);
+    a.inverse = fused && r0 + a.nterms == R;
     a.w_first = r0;
     for (u32 r = 0; r < a.nterms; r++) a.term[r] = RotTerm{ext, ct + pl, ct, evks[r0 + r], galois[r0 + r]};
     if ((rc = launch_rot_sum(c, a, B, st, 1, near, last_int))) return rc;
@@ -497,8 +506,10 @@ struct LinAttn {
   int sum_rotations(u64* out, const u64* in, u32 n, const std::vector<u32>& elements, const u64* const* keys) {
     int rc;
     u64* acc = (u64*)(ks + ks_layout(c, n, nlimbs).acc);
-    if ((rc = rotations_to_ext(c, lt, whole, in, n, nlimbs, elements.data(), keys, (u32)elements.size(), nullptr, 1, acc, ks, st))) return rc;
-    return ext_mod_down(c, lt, whole, acc, out, n, nlimbs, ks, st);
+    bool done;
+    if ((rc = rotations_to_ext(c, lt, whole, in, n, nlimbs, elements.data(), keys, (u32)elements.size(), nullptr, 1, acc, ks, st, &done)))
+      return rc;
+    return ext_mod_down(c, lt, whole, acc, out, n, nlimbs, ks, st, done);
   }
 
   // d = sum_{s <= t} p_ts * v_s for tokens [t0, t0 + T)

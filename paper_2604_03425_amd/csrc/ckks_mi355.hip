@@ -1434,12 +1434,12 @@ int ks16_assemble(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B, u32
 // Second half of a key switch on the two-pass path: from the accumulators (all slots) to the assembled output.
 // acc_in: accumulators held outside the workspace ([B][2][next][N]; their special-prime slots are overwritten).
 int ks16_finish(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B, u32 nlimbs, char* ws, hipStream_t st,
-                u64* acc_in = nullptr) {
+                u64* acc_in = nullptr, bool int_blocks_done = false) {
   int rc;
   KsLayout L = ks_layout(c, B, nlimbs);
   u64* acc = acc_in ? acc_in : (u64*)(ws + L.acc);
   u64* tq = (u64*)(ws + L.tq);
-  if ((rc = ks16_moddown_rows(c, lt, B, nlimbs, acc, tq, st))) return rc;
+  if ((rc = ks16_moddown_rows(c, lt, B, nlimbs, acc, tq, st, int_blocks_done))) return rc;
   return ks16_assemble(c, lt, io, B, nlimbs, acc, tq, st);
 }
 
@@ -1752,9 +1752,9 @@ static FwdInnerArgs hoisted_args(const ckks_ctx* c, const LevelTables* lt, const
 // Shared front of the hoisted rotations: inverse transform, ModUp and forward transform of B polynomials (limb-vector (b, t) at
 // d + b*d_stride + t*N) into the workspace, and the arguments of the streaming inner-product kernels that read them
 // (accumulators default to the workspace's own).
-// last_int: limb nlimbs - 1 in integers (JOINED_FORCED).
+// last_int: limb nlimbs - 1 in integers (JOINED_FORCED). rows_only: only the first pass of the forward transform.
 static int hoist_front16(ckks_ctx* c, const LevelTables* lt, const u64* d, u64 d_stride, u32 B, u32 nlimbs, char* ws,
-                         hipStream_t st, FwdInnerArgs& ia, bool last_int = false) {
+                         hipStream_t st, FwdInnerArgs& ia, bool last_int = false, bool rows_only = false) {
   int rc;
   const u32 N = c->N, next = lt->next, beta = lt->beta;
   const u64 polyN = (u64)nlimbs * N;
@@ -1781,7 +1781,9 @@ static int hoist_front16(ckks_ctx* c, const LevelTables* lt, const u64* d, u64 d
     HIP_TRY(hipGetLastError());
   }
   of.raw_out = true;  // reduced doubles on double-precision moduli, canonical residues elsewhere
-  if ((rc = launch_ntt(c, false, ext, (u64)next * N, ext, (u64)next * N, B * beta, 0, next, emap, beta, nlimbs, st, of)))
+  of.rows_only = rows_only;
+  if (!(rows_only && of.blocks_only) &&
+      (rc = launch_ntt(c, false, ext, (u64)next * N, ext, (u64)next * N, B * beta, 0, next, emap, beta, nlimbs, st, of)))
     return rc;
   ia = hoisted_args(c, lt, d, d_stride, ext, nlimbs);
   ia.acc = (u64*)(ws + L.acc);

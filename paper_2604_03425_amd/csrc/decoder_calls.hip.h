@@ -7,7 +7,8 @@ namespace {
 
 // ModDown by P q_{nlimbs-1} of both accumulators [B][2][next][N] (what lies from limb nlimbs - 1 on is overwritten) to out
 // [B][2][nlimbs - 1][N]: that limb joins the special ones as a source of the conversion.
-int ext_mod_down_more(ckks_ctx* c, const LevelTables* lt, bool whole, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
+int ext_mod_down_more(ckks_ctx* c, const LevelTables* lt, bool whole, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st,
+                      bool blocks_done = false) {
   int rc;
   if (whole) {
     Ks12Args a = ks12_args(c, lt, B, nlimbs, ws);
@@ -28,7 +29,7 @@ int ext_mod_down_more(ckks_ctx* c, const LevelTables* lt, bool whole, u64* acc, 
   const u32 N = c->N, next = lt->next, K = c->np, keep = nlimbs - 1;
   u64* tq = (u64*)(ws + ks_layout(c, B, nlimbs).tq);
   if (two_pass(c)) {
-    if ((rc = ks16_drop_rows(c, lt, B, nlimbs, acc, tq, st, false))) return rc;
+    if ((rc = ks16_drop_rows(c, lt, B, nlimbs, acc, tq, st, blocks_done))) return rc;
     FwdFinalArgs a;
     a.tq = tq;
     a.acc = acc;
@@ -155,11 +156,12 @@ struct Decoder {
     if ((rc = get_level(c, nlimbs, &lt))) return rc;
     u64* acc = (u64*)(ks + ks_layout(c, n, nlimbs).acc);
     const bool by_limbs = whole(lt, n, nlimbs);
+    bool done;
     if ((rc = rotations_to_ext(c, lt, by_limbs, in, n, nlimbs, elements.data(), rot_keys, (u32)elements.size(), nullptr, 1, acc, ks, st,
-                               more && drop_form(c, lt, nlimbs) == JOINED_FORCED)))
+                               &done, more ? drop_form(c, lt, nlimbs) : APART)))
       return rc;
-    return more ? ext_mod_down_more(c, lt, by_limbs, acc, out, n, nlimbs, ks, st)
-                : ext_mod_down(c, lt, by_limbs, acc, out, n, nlimbs, ks, st);
+    return more ? ext_mod_down_more(c, lt, by_limbs, acc, out, n, nlimbs, ks, st, done)
+                : ext_mod_down(c, lt, by_limbs, acc, out, n, nlimbs, ks, st, done);
   }
   // The sum over the components of a lane of products d (nlimbs limbs), less a limb, in every slot of the lane. In one of y; where is
   // returned in `out`.
