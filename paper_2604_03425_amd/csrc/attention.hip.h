@@ -545,7 +545,8 @@ __device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 
     to[(size_t)a.next * N] = d2u_canon(fp_reduce(L1[k], qinv, q), q);
   }
 }
-// Integer moduli (PLAIN: all of them, acc without the factor 2^-64): 30-bit halves, 4 multiply-adds a term and carries every 11.
+// Integer moduli (PLAIN: all of them, acc without the factor 2^-64): 30-bit halves, 4 multiply-adds a term and carries every
+// seventh.
 template <int CB, bool PLAIN, bool FUSED>
 __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32 blk, u32 zi, u64* tile, ulonglong2* tws) {
   const size_t N = (size_t)1 << a.logN, pl = (size_t)a.nlimbs * N, comp = (size_t)a.nm * N;
@@ -558,12 +559,12 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
   const u32 jo = main_prime ? t / a.alpha : 0xFFFFFFFFu;
   u64* const sm = tile;
   u32 bb[CB];
-  Dot30 s0[CB], s1[CB];
+  Dot30N s0[CB], s1[CB];
 #pragma unroll
   for (int k = 0; k < CB; k++) {
     bb[k] = min(b0 + k, a.B - 1);
-    dot30_init(s0[k]);
-    dot30_init(s1[k]);
+    dot30n_init(s0[k]);
+    dot30n_init(s1[k]);
   }
   typedef BlockFill<CB, FUSED> Fill;
   u64* digit = tile;
@@ -575,10 +576,10 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
   if (FUSED) lds_barrier();
   u32 count = 0;
   auto carry = [&] {
-    if (++count < 11) return;
+    if (++count < 7) return;
     count = 0;
 #pragma unroll
-    for (int k = 0; k < CB; k++) dot30_settle(s0[k], mi.mu64, nm), dot30_settle(s1[k], mi.mu64, nm);
+    for (int k = 0; k < CB; k++) dot30n_settle(s0[k], mi.mu64, nm), dot30n_settle(s1[k], mi.mu64, nm);
   };
   block_sum_terms(
       a, (size_t)id * N + n, comp, n,
@@ -617,8 +618,8 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
         for (int k = 0; k < CB; k++) {
           const u64 x = digit[k * BLOCK_SUM + m];
           const u32 x0 = (u32)x & M30, x1 = (u32)(x >> 30);
-          dot30_mac(s0[k], x0, x1, e00, e01);
-          dot30_mac(s1[k], x0, x1, e10, e11);
+          dot30n_mac(s0[k], x0, x1, e00, e01);
+          dot30n_mac(s1[k], x0, x1, e10, e11);
         }
         carry();
       });
@@ -634,7 +635,7 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
 #pragma unroll
       for (int k = 0; k < CB; k++) {
         const u64 x = tile[k * BLOCK_SUM + m];
-        dot30_mac(s0[k], (u32)x & M30, (u32)(x >> 30), p0, p1);
+        dot30n_mac(s0[k], (u32)x & M30, (u32)(x >> 30), p0, p1);
       }
       carry();
     }
@@ -642,8 +643,8 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
 #pragma unroll
       for (int k = 0; k < CB; k++) {
         const u64* x = a.base + (size_t)bb[k] * a.base_stride + (size_t)t * N + n;
-        dot30_mac(s0[k], (u32)x[0] & M30, (u32)(x[0] >> 30), p0, p1);
-        dot30_mac(s1[k], (u32)x[pl] & M30, (u32)(x[pl] >> 30), p0, p1);
+        dot30n_mac(s0[k], (u32)x[0] & M30, (u32)(x[0] >> 30), p0, p1);
+        dot30n_mac(s1[k], (u32)x[pl] & M30, (u32)(x[pl] >> 30), p0, p1);
       }
     }
   }
@@ -657,9 +658,9 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
     u64* to = a.acc + ((size_t)bb[k] * 2 * a.next + t) * N + n;
 #pragma unroll
     for (int c = 0; c < 2; c++) {
-      Dot30& s = c ? s1[k] : s0[k];
-      dot30_settle(s, mi.mu64, nm);
-      u64 v = PLAIN ? reduce128(dot30_value(s), mi) : csub(csub(redc(dot30_value(s), q, mi.minv), q), q);
+      Dot30N& s = c ? s1[k] : s0[k];
+      dot30n_settle(s, mi.mu64, nm);
+      u64 v = PLAIN ? reduce128(dot30n_value(s), mi) : csub(csub(redc(dot30n_value(s), q, mi.minv), q), q);
       u64* o = to + (size_t)c * a.next * N;
       if (a.accumulate && b0 + k < a.B) v = addmod(v, *o, q);
       if (back) sm[(2 * k + c) * BLOCK_SUM + tid] = v;
@@ -684,7 +685,7 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
 }
 // Kinds as for rot_sum_kernel. grid = (ceil(B / CB), N / 256, slots)
 template <int KIND, int CB, bool FUSED>
-__global__ void __launch_bounds__(BLOCK_SUM) block_sum_kernel(RotSumArgs a) {
+__global__ void __launch_bounds__(BLOCK_SUM) __attribute__((amdgpu_waves_per_eu(4))) block_sum_kernel(RotSumArgs a) {
   __shared__ __attribute__((aligned(16))) u64 sm[2 * block_sum_fill<CB, FUSED>() * CB * BLOCK_SUM];
   __shared__ ulonglong2 tws[FUSED ? BLOCK_SUM - 1 : 1];
   u32 what, blk, zi;

@@ -171,6 +171,19 @@ __device__ __forceinline__ void dot30n_mac(Dot30N& d, u32 y0, u32 y1, u32 c0, u3
   d.b += (u64)y1 * c0;
   d.c += (u64)y1 * c1;
 }
+// The same value with a and b below 2^30 and c below 4m (as dot30_settle); 7 products of operands below 2^60 fit on top of that.
+__device__ __forceinline__ void dot30n_settle(Dot30N& d, u64 mu64, u64 nm) {
+  d.b += d.a >> 30;
+  d.c += d.b >> 30;
+  d.a = (u32)d.a & 0x3FFFFFFFu;
+  d.b = (u32)d.b & 0x3FFFFFFFu;
+  const u32 x0 = (u32)d.c, x1 = (u32)(d.c >> 32), p0 = (u32)mu64, p1 = (u32)(mu64 >> 32);
+  const u64 qt = (u64)x1 * p1 + __umulhi(x1, p0) + __umulhi(x0, p1);
+  const u32 q0 = (u32)qt, q1 = (u32)(qt >> 32), n0 = (u32)nm, n1 = (u32)(nm >> 32);
+  const u64 t = d.c + (u64)q0 * n0;
+  d.c = (u64)((u32)(t >> 32) + q0 * n1 + q1 * n0) << 32 | (u32)t;
+}
+__device__ __forceinline__ Acc128 dot30n_value(const Dot30N& d) { return dot30_value(Dot30{d.a, d.b, 0, d.c}); }
 // minv = -m^-1 mod 2^64 (its low 30 bits are -m^-1 mod 2^30).
 __device__ __forceinline__ u64 dot30n_redc90(const Dot30N& d, u64 m, u64 minv) {
   const u32 q0 = (u32)m & 0x3FFFFFFFu, q1 = (u32)(m >> 30), qi = (u32)minv & 0x3FFFFFFFu;
