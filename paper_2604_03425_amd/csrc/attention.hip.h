@@ -32,6 +32,11 @@ struct RotSumArgs {
   const ulonglong2 *tw = nullptr, *twi = nullptr;
   const double* twfp = nullptr;
   u32 first_special = 0, inverse = 0;
+  // fin_tq != null: main limbs are finished, out = (sum - NTT(tq)) pinv, instead of stored; tq after the first pass of its transform
+  const u64* fin_tq = nullptr;   // [B][2][fin_limbs][N]
+  u64* fin_out = nullptr;        // [B][2][fin_limbs][N]
+  const ulonglong2* fin_pinv = nullptr;
+  u32 fin_limbs = 0;
   unsigned char slots[128];
   RotTerm term[ROT_SUM_TERMS];
 };
@@ -385,6 +390,23 @@ __device__ __forceinline__ void block_sum_terms(const RotSumArgs& a, size_t at, 
     }
   }
 }
+// The corrections of CB ciphertexts' accumulators at a block, transformed, to sm[2 k + c][256].
+template <int CB, class Forward>
+__device__ __forceinline__ void block_corrections(const RotSumArgs& a, u32 b0, u32 blk, u32 t, u64* sm, Forward forward) {
+  const size_t N = (size_t)1 << a.logN;
+  lds_barrier();   // what was there has been read
+  for (u32 u = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); u < 2 * CB; u += 4) {
+    const u32 l = block_lane();
+    const u64* p = uniform_ptr(a.fin_tq + (((size_t)min(b0 + u / 2, a.B - 1) * 2 + u % 2) * a.fin_limbs + t) * N + blk * BLOCK_SUM);
+    u64 x[4];
+#pragma unroll
+    for (u32 i = 0; i < 4; i++) x[i] = p[block_elem(0, i, l)];
+    forward(x, sm + u * BLOCK_SUM);
+#pragma unroll
+    for (u32 i = 0; i < 4; i++) sm[u * BLOCK_SUM + block_elem(3, i, l)] = x[i];
+  }
+  lds_barrier();
+}
 // FUSED: ext comes from the first pass of the digits' transform. A wave takes a block of a ciphertext's digit through the second one on
 // its way into LDS, as many digits at a time as there are waves for.
 template <int CB, bool FUSED>
@@ -534,6 +556,16 @@ __device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 
       L0[k] += fp_mulmod_var(fp_reduce(v[k], qinv, q), pm, qinv, q);
     }
   }
+  const bool finish = FUSED && main_prime && a.fin_tq;   // uniform
+  if (finish)
+    block_corrections<CB>(a, b0, blk, t, sm, [&](u64 (&v)[4], u64* to) {
+      double y[4];
+#pragma unroll
+      for (int i = 0; i < 4; i++) y[i] = __longlong_as_double((long long)v[i]);
+      block_forward(y, tws, q, qinv, (double*)to);
+#pragma unroll
+      for (int i = 0; i < 4; i++) v[i] = (u64)__double_as_longlong(y[i]);
+    });
 #pragma unroll
   for (int k = 0; k < CB; k++) {
     if (b0 + k >= a.B) break;
@@ -541,8 +573,15 @@ __device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 
     settle(H1[k], L1[k]);
     u64* to = a.acc + ((size_t)bb[k] * 2 * a.next + t) * N + n;
     if (a.accumulate) L0[k] += u2d(to[0]), L1[k] += u2d(to[(size_t)a.next * N]);
-    to[0] = d2u_canon(fp_reduce(L0[k], qinv, q), q);
-    to[(size_t)a.next * N] = d2u_canon(fp_reduce(L1[k], qinv, q), q);
+    double r0 = fp_reduce(L0[k], qinv, q), r1 = fp_reduce(L1[k], qinv, q);
+    if (finish) {
+      const double2 pv = ((const double2*)a.fin_pinv)[t];
+      r0 = fp_mulmod_const(r0 - __longlong_as_double((long long)sm[2 * k * BLOCK_SUM + tid]), pv.x, pv.y, q);
+      r1 = fp_mulmod_const(r1 - __longlong_as_double((long long)sm[(2 * k + 1) * BLOCK_SUM + tid]), pv.x, pv.y, q);
+      to = a.fin_out + ((size_t)bb[k] * 2 * a.fin_limbs + t) * N + n;
+    }
+    to[0] = d2u_canon(r0, q);
+    to[(finish ? a.fin_limbs : a.next) * N] = d2u_canon(r1, q);
   }
 }
 // Integer moduli (PLAIN: all of them, acc without the factor 2^-64): 30-bit halves, 4 multiply-adds a term and carries every
@@ -649,6 +688,12 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
     }
   }
   const bool back = FUSED && a.inverse && t >= a.first_special;   // uniform
+  const bool finish = FUSED && main_prime && !back && a.fin_tq;
+  if (finish)
+    block_corrections<CB>(a, b0, blk, t, sm, [&](u64 (&v)[4], u64* to) {
+      if (big) block_forward<true>(v, tws, q, mi.mu64, to);
+      else block_forward<false>(v, tws, q, mi.mu64, to);
+    });
   if (back) {
     lds_barrier();   // the tiles and the twiddles have been read
     block_twiddles_fetch(tws, a.twi + (size_t)id * N, blk, (u32)(N / BLOCK_SUM));
@@ -663,6 +708,11 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
       u64 v = PLAIN ? reduce128(dot30n_value(s), mi) : csub(csub(redc(dot30n_value(s), q, mi.minv), q), q);
       u64* o = to + (size_t)c * a.next * N;
       if (a.accumulate && b0 + k < a.B) v = addmod(v, *o, q);
+      if (finish) {
+        const ulonglong2 pv = a.fin_pinv[t];
+        v = shoup(submod(v, sm[(2 * k + c) * BLOCK_SUM + tid], q), pv.x, pv.y, q);
+        o = a.fin_out + (((size_t)bb[k] * 2 + c) * a.fin_limbs + t) * N + n;
+      }
       if (back) sm[(2 * k + c) * BLOCK_SUM + tid] = v;
       else if (b0 + k < a.B) *o = v;
     }

@@ -59,12 +59,11 @@ int ext_digits(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* d, u64
 }
 
 // ModDown of both accumulators [B][2][next][N] (their special limbs are overwritten) to out [B][2][nlimbs][N].
-int ext_mod_down(ckks_ctx* c, const LevelTables* lt, bool whole, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st,
-                 bool blocks_done = false) {
+int ext_mod_down(ckks_ctx* c, const LevelTables* lt, bool whole, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
   int rc;
   if (two_pass(c)) {
     KsIo io{nullptr, 0, 0, out, {0, 0}, nullptr, 0};
-    return ks16_finish(c, lt, io, B, nlimbs, ws, st, acc, blocks_done);
+    return ks16_finish(c, lt, io, B, nlimbs, ws, st, acc);
   }
   if (whole) {
     Ks12Args a = ks12_args(c, lt, B, nlimbs, ws);
@@ -142,12 +141,14 @@ bool rotations_near(const ckks_ctx* c, const u32* galois, u32 R) {
     if (galois[r] % (2 * c->N / BLOCK_SUM) != 1) return false;
   return R != 0;
 }
-int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 outs = 1, bool near = false, bool last_int = false) {
+// near: block_sum_kernel (rotations_near); last_int: limb nlimbs - 1 in integers; extended limbs from `from` to `to` only.
+int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 outs = 1, bool near = false, bool last_int = false,
+                   u32 from = 0, u32 to = ~0u) {
   a.B = B;
   const LimbMap emap = ext_map(c, a.nlimbs);
   u32 cnt = 0;
   for (int fp = 1; fp >= 0; fp--) {   // double-precision slots first
-    for (u32 s = 0; s < a.next; s++)
+    for (u32 s = from; s < std::min(to, a.next); s++)
       if ((a.doubles && host_class(c, c->mod[emap.id[s]]) == 0 && !(last_int && s + 1 == a.nlimbs)) == (fp == 1)) a.slots[cnt++] = (unsigned char)s;
     if (fp) a.nfp = cnt;
   }
@@ -167,17 +168,13 @@ int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 
   return CKKS_OK;
 }
 
-// acc = P w_0 ct + sum_r w_{r+1} (accumulators of the rotation of ct by galois[r]); ws: a key-switch workspace for B. Returns in
-// *blocks_done (where given) whether the integer special limbs (and the last main one, where it goes with them: last_int, or an integer
-// one with `drop`) have been through their inverse block pass, which unweighted near rotations on two-pass rings do in their kernel.
+// acc = P w_0 ct + sum_r w_{r+1} (accumulators of the rotation of ct by galois[r]); ws: a key-switch workspace for B.
 int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* ct, u32 B, u32 nlimbs, const u32* galois,
-                     const u64* const* evks, u32 R, const u64* w, u32 per_set, u64* acc, char* ws, hipStream_t st, bool* blocks_done = nullptr,
-                     DropForm form = APART) {
+                     const u64* const* evks, u32 R, const u64* w, u32 per_set, u64* acc, char* ws, hipStream_t st, bool last_int = false) {
   int rc;
   const u64 pl = (u64)nlimbs * c->N;
-  const bool last_int = form == JOINED_FORCED, near = !w && rotations_near(c, galois, R), fused = near && blocks_done && two_pass(c);
-  if (blocks_done) *blocks_done = fused;
-  if (R && (rc = ext_digits(c, lt, whole, ct + pl, 2 * pl, B, nlimbs, ws, st, last_int, fused))) return rc;
+  const bool near = !w && rotations_near(c, galois, R);
+  if (R && (rc = ext_digits(c, lt, whole, ct + pl, 2 * pl, B, nlimbs, ws, st, last_int))) return rc;
   const u64* ext = (const u64*)(ws + ks_layout(c, B, nlimbs).ext);
   RotSumArgs a = rot_sum_args(c, lt, whole, nlimbs, acc, 2 * pl);
   a.base = ct;
@@ -185,10 +182,8 @@ int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* 
   a.w = w;
   a.w_terms = R + 1;
   a.per_set = per_set;
-  if (fused) a.tw = c->d_tw_fwd, a.twi = c->d_tw_inv, a.twfp = c->d_twfp_fwd, a.first_special = form == APART ? nlimbs : nlimbs - 1;
   for (u32 r0 = 0; r0 == 0 || r0 < R; r0 += ROT_SUM_TERMS) {
     a.nterms = std::min<u32>(ROT_SUM_TERMS, R - r0);
-    a.inverse = fused && r0 + a.nterms == R;
     a.w_first = r0;
     for (u32 r = 0; r < a.nterms; r++) a.term[r] = RotTerm{ext, ct + pl, ct, evks[r0 + r], galois[r0 + r]};
     if ((rc = launch_rot_sum(c, a, B, st, 1, near, last_int))) return rc;
@@ -196,6 +191,67 @@ int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* 
     a.accumulate = 1;
   }
   return CKKS_OK;
+}
+
+// out = ct + its rotations by galois[r] with one ModDown, by P or (drop) by P q_{nlimbs-1}; R > 0, ws: a key-switch workspace for B.
+// Unweighted near rotations on two-pass rings: digits go through their last stages and the special limbs through their first inverse ones
+// in the sums' kernel, which comes first for the special limbs and then for the main ones, whose sums it finishes: neither the
+// transformed digits nor the main limbs' sums reach memory. Where all workgroups are one round (BLOCK_SUM_ROUND) the limbs go together and
+// the assembly is a kernel of its own. us, together | apart: attention of four ragged sequences at 2^13, 672 workgroups, 318 | 336; norms of 5
+// ciphertexts at 2^14, 1280, 604 | 611, of one of 12 limbs at 2^16, 4096, 1151 | 1161; 26 pairs of 64 components there 3829 | 3579. Otherwise
+// *done is false and nothing happens.
+#define BLOCK_SUM_ROUND 4096
+int sum_near_rotations(ckks_ctx* c, const LevelTables* lt, u64* out, const u64* ct, u32 B, u32 nlimbs, const u32* galois,
+                       const u64* const* evks, u32 R, bool drop, char* ws, hipStream_t st, bool* done) {
+  int rc;
+  *done = two_pass(c) && rotations_near(c, galois, R);
+  if (!*done) return CKKS_OK;
+  const u64 pl = (u64)nlimbs * c->N;
+  const KsLayout L = ks_layout(c, B, nlimbs);
+  u64 *acc = (u64*)(ws + L.acc), *tq = (u64*)(ws + L.tq);
+  const u64* ext = (const u64*)(ws + L.ext);
+  const DropForm form = drop ? drop_form(c, lt, nlimbs) : APART;
+  const bool last_int = form == JOINED_FORCED;
+  const u32 keep = drop ? nlimbs - 1 : nlimbs;
+  if ((rc = ext_digits(c, lt, false, ct + pl, 2 * pl, B, nlimbs, ws, st, last_int, true))) return rc;
+  RotSumArgs a = rot_sum_args(c, lt, false, nlimbs, acc, 2 * pl);
+  a.base_stride = 2 * pl;
+  a.tw = c->d_tw_fwd;
+  a.twi = c->d_tw_inv;
+  a.twfp = c->d_twfp_fwd;
+  a.first_special = form == APART ? nlimbs : keep;
+  a.fin_out = out;
+  a.fin_pinv = drop ? lt->dm_pinv2 : lt->pinv2;
+  a.fin_limbs = keep;
+  auto sums = [&](u32 from, u32 to) {
+    a.base = ct;
+    a.accumulate = 0;
+    for (u32 r0 = 0; r0 < R; r0 += ROT_SUM_TERMS) {
+      a.nterms = std::min<u32>(ROT_SUM_TERMS, R - r0);
+      a.inverse = r0 + a.nterms == R;
+      a.fin_tq = to <= keep && a.inverse ? tq : nullptr;
+      for (u32 r = 0; r < a.nterms; r++) a.term[r] = RotTerm{ext, ct + pl, ct, evks[r0 + r], galois[r0 + r]};
+      if (int e = launch_rot_sum(c, a, B, st, 1, true, last_int, from, to)) return e;
+      a.base = nullptr;
+      a.accumulate = 1;
+    }
+    return CKKS_OK;
+  };
+  const u32 groups = (B + 3) / 4;
+  if ((u64)groups * (c->N / BLOCK_SUM) * lt->next <= BLOCK_SUM_ROUND) {
+    if ((rc = sums(0, lt->next))) return rc;
+    if (drop) rc = ks16_drop_rows(c, lt, B, nlimbs, acc, tq, st, true);
+    else rc = ks16_moddown_rows(c, lt, B, nlimbs, acc, tq, st, true);
+    if (rc) return rc;
+    if (drop) return ks16_drop_assemble(c, lt, out, B, nlimbs, acc, tq, st);
+    KsIo io{nullptr, 0, 0, out, {0, 0}, nullptr, 0};
+    return ks16_assemble(c, lt, io, B, nlimbs, acc, tq, st);
+  }
+  if ((rc = sums(keep, lt->next))) return rc;
+  if (drop) rc = ks16_drop_rows(c, lt, B, nlimbs, acc, tq, st, true);
+  else rc = ks16_moddown_rows(c, lt, B, nlimbs, acc, tq, st, true);
+  if (rc) return rc;
+  return sums(0, keep);
 }
 
 // ---- linear attention ----
@@ -505,11 +561,12 @@ struct LinAttn {
   // out = in + its rotations by the elements, one ModDown for all of them; n <= slice ciphertexts
   int sum_rotations(u64* out, const u64* in, u32 n, const std::vector<u32>& elements, const u64* const* keys) {
     int rc;
-    u64* acc = (u64*)(ks + ks_layout(c, n, nlimbs).acc);
     bool done;
-    if ((rc = rotations_to_ext(c, lt, whole, in, n, nlimbs, elements.data(), keys, (u32)elements.size(), nullptr, 1, acc, ks, st, &done)))
+    if ((rc = sum_near_rotations(c, lt, out, in, n, nlimbs, elements.data(), keys, (u32)elements.size(), false, ks, st, &done)) || done)
       return rc;
-    return ext_mod_down(c, lt, whole, acc, out, n, nlimbs, ks, st, done);
+    u64* acc = (u64*)(ks + ks_layout(c, n, nlimbs).acc);
+    if ((rc = rotations_to_ext(c, lt, whole, in, n, nlimbs, elements.data(), keys, (u32)elements.size(), nullptr, 1, acc, ks, st))) return rc;
+    return ext_mod_down(c, lt, whole, acc, out, n, nlimbs, ks, st);
   }
 
   // d = sum_{s <= t} p_ts * v_s for tokens [t0, t0 + T)

@@ -1431,15 +1431,40 @@ int ks16_assemble(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B, u32
   return CKKS_OK;
 }
 
+// The same after ks16_drop_rows, without addends: out [B][2][nlimbs - 1][N].
+int ks16_drop_assemble(ckks_ctx* c, const LevelTables* lt, u64* out, u32 B, u32 nlimbs, const u64* acc, const u64* tq, hipStream_t st) {
+  FwdFinalArgs a;
+  a.tq = tq;
+  a.acc = acc;
+  a.out = out;
+  a.add_src = nullptr;
+  a.add2 = nullptr;
+  a.tw = c->d_tw_fwd;
+  a.twfp = c->d_twfp_fwd;
+  a.mods = c->d_mods;
+  a.pinv = lt->dm_pinv2;
+  a.logN = c->logN;
+  a.nlimbs = nlimbs - 1;
+  a.next = lt->next;
+  a.mode0 = a.mode1 = 0;
+  a.galois = 0;
+  a.map_mode = map_mode_pass(c);
+  auto cls_of = [&](u32 s) { return host_class(c, c->mod[s]); };
+  launch_by_class(c, PK_FWD_FINAL, a, B * 2, nlimbs - 1, cls_of, st,
+                  [&](int cls, dim3 grid) { LAUNCH_CLASS_KERNEL(ntt16_fwd_blocks_final_kernel, cls, grid, st, a); });
+  HIP_TRY(hipGetLastError());
+  return CKKS_OK;
+}
+
 // Second half of a key switch on the two-pass path: from the accumulators (all slots) to the assembled output.
 // acc_in: accumulators held outside the workspace ([B][2][next][N]; their special-prime slots are overwritten).
 int ks16_finish(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B, u32 nlimbs, char* ws, hipStream_t st,
-                u64* acc_in = nullptr, bool int_blocks_done = false) {
+                u64* acc_in = nullptr) {
   int rc;
   KsLayout L = ks_layout(c, B, nlimbs);
   u64* acc = acc_in ? acc_in : (u64*)(ws + L.acc);
   u64* tq = (u64*)(ws + L.tq);
-  if ((rc = ks16_moddown_rows(c, lt, B, nlimbs, acc, tq, st, int_blocks_done))) return rc;
+  if ((rc = ks16_moddown_rows(c, lt, B, nlimbs, acc, tq, st))) return rc;
   return ks16_assemble(c, lt, io, B, nlimbs, acc, tq, st);
 }
 

@@ -7,8 +7,7 @@ namespace {
 
 // ModDown by P q_{nlimbs-1} of both accumulators [B][2][next][N] (what lies from limb nlimbs - 1 on is overwritten) to out
 // [B][2][nlimbs - 1][N]: that limb joins the special ones as a source of the conversion.
-int ext_mod_down_more(ckks_ctx* c, const LevelTables* lt, bool whole, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st,
-                      bool blocks_done = false) {
+int ext_mod_down_more(ckks_ctx* c, const LevelTables* lt, bool whole, u64* acc, u64* out, u32 B, u32 nlimbs, char* ws, hipStream_t st) {
   int rc;
   if (whole) {
     Ks12Args a = ks12_args(c, lt, B, nlimbs, ws);
@@ -29,28 +28,8 @@ int ext_mod_down_more(ckks_ctx* c, const LevelTables* lt, bool whole, u64* acc, 
   const u32 N = c->N, next = lt->next, K = c->np, keep = nlimbs - 1;
   u64* tq = (u64*)(ws + ks_layout(c, B, nlimbs).tq);
   if (two_pass(c)) {
-    if ((rc = ks16_drop_rows(c, lt, B, nlimbs, acc, tq, st, blocks_done))) return rc;
-    FwdFinalArgs a;
-    a.tq = tq;
-    a.acc = acc;
-    a.out = out;
-    a.add_src = nullptr;
-    a.add2 = nullptr;
-    a.tw = c->d_tw_fwd;
-    a.twfp = c->d_twfp_fwd;
-    a.mods = c->d_mods;
-    a.pinv = lt->dm_pinv2;
-    a.logN = c->logN;
-    a.nlimbs = keep;
-    a.next = next;
-    a.mode0 = a.mode1 = 0;
-    a.galois = 0;
-    a.map_mode = map_mode_pass(c);
-    auto cls_of = [&](u32 s) { return host_class(c, c->mod[s]); };
-    launch_by_class(c, PK_FWD_FINAL, a, B * 2, keep, cls_of, st,
-                    [&](int cls, dim3 grid) { LAUNCH_CLASS_KERNEL(ntt16_fwd_blocks_final_kernel, cls, grid, st, a); });
-    HIP_TRY(hipGetLastError());
-    return CKKS_OK;
+    if ((rc = ks16_drop_rows(c, lt, B, nlimbs, acc, tq, st, false))) return rc;
+    return ks16_drop_assemble(c, lt, out, B, nlimbs, acc, tq, st);
   }
   LimbMap sources = identity_map(0);
   sources.id[0] = (unsigned char)keep;
@@ -154,14 +133,16 @@ struct Decoder {
     int rc;
     const LevelTables* lt;
     if ((rc = get_level(c, nlimbs, &lt))) return rc;
+    bool done;
+    if ((rc = sum_near_rotations(c, lt, out, in, n, nlimbs, elements.data(), rot_keys, (u32)elements.size(), more, ks, st, &done)) || done)
+      return rc;
     u64* acc = (u64*)(ks + ks_layout(c, n, nlimbs).acc);
     const bool by_limbs = whole(lt, n, nlimbs);
-    bool done;
     if ((rc = rotations_to_ext(c, lt, by_limbs, in, n, nlimbs, elements.data(), rot_keys, (u32)elements.size(), nullptr, 1, acc, ks, st,
-                               &done, more ? drop_form(c, lt, nlimbs) : APART)))
+                               more && drop_form(c, lt, nlimbs) == JOINED_FORCED)))
       return rc;
-    return more ? ext_mod_down_more(c, lt, by_limbs, acc, out, n, nlimbs, ks, st, done)
-                : ext_mod_down(c, lt, by_limbs, acc, out, n, nlimbs, ks, st, done);
+    return more ? ext_mod_down_more(c, lt, by_limbs, acc, out, n, nlimbs, ks, st)
+                : ext_mod_down(c, lt, by_limbs, acc, out, n, nlimbs, ks, st);
   }
   // The sum over the components of a lane of products d (nlimbs limbs), less a limb, in every slot of the lane. In one of y; where is
   // returned in `out`.
