@@ -138,22 +138,50 @@ __global__ void __launch_bounds__(256) weighted_values_kernel(ValueArgs a) {
   else weighted_values<false>(a, mi);
 }
 
-// factor (x[b] + bias) * (y[b] + bias) + (z_factor z[b], 0) for ciphertext b; the biases are added to every slot. z may be null.
-// second != 0: also x2[b] * y[b], as ciphertext second + b.
+// A ciphertext as a product takes it: itself or its negative, plus the number add - sub in every slot.
+struct Affine {
+  long long add, sub;
+  u32 negative;
+};
+__device__ __forceinline__ void apply(const Affine& f, ulonglong2 (&v)[2], const ModInfo& mi) {
+  const u64 m = mi.m, number = submod(signed_residue(f.add, mi), signed_residue(f.sub, mi), m);
+  if (f.negative) {   // uniform
+    v[0] = {submod(number, v[0].x, m), submod(number, v[0].y, m)};
+    v[1] = {submod(0, v[1].x, m), submod(0, v[1].y, m)};
+  } else {
+    v[0] = plus_number(v[0], number, m);
+  }
+}
+// factor X * Y + (z_factor Z, 0) for ciphertext b, X, Y and Z what fx, fy and fz make of x, y and z. y null: the same words as x; z null:
+// none. plus: x + plus in the place of x, written to `sum` too where that is given (layout of x). second != 0: also Y * Y, as
+// ciphertext second + b.
 struct ProductArgs {
-  CtRef x, y, x2, z;
+  CtRef x, y, z;
+  Affine fx, fy, fz;
+  const u64* plus;
+  u64* sum;
   ProductOut o;
   const ModInfo* mods;
-  long long factor, bias, z_factor;
+  long long factor, z_factor;
   u32 logN, fp_on, second;
 };
 template <bool FP>
 __device__ __forceinline__ void ct_products(const ProductArgs& a, const ModInfo& mi) {
   const size_t N = (size_t)1 << a.logN, n = (blockIdx.x * 256 + threadIdx.x) * 2, l = blockIdx.y, b = blockIdx.z;
-  const u64 *px = a.x.at + b * a.x.stride + l * N + n, *py = a.y.at + b * a.y.stride + l * N + n;
-  const u64 bias = signed_residue(a.bias, mi);
-  ulonglong2 x[2] = {plus_number(word_pair(px), bias, mi.m), word_pair(px + a.x.comp)};
-  const ulonglong2 y[2] = {plus_number(word_pair(py), bias, mi.m), word_pair(py + a.y.comp)};
+  ulonglong2 x[2], y[2];
+#pragma unroll
+  for (int c = 0; c < 2; c++) {
+    const size_t at = b * a.x.stride + c * a.x.comp + l * N + n;
+    x[c] = word_pair(a.x.at + at);
+    if (a.plus) {
+      const ulonglong2 p = word_pair(a.plus + at);
+      x[c] = {addmod(x[c].x, p.x, mi.m), addmod(x[c].y, p.y, mi.m)};
+      if (a.sum) *(ulonglong2*)(a.sum + at) = x[c];
+    }
+    y[c] = a.y.at ? word_pair(a.y.at + b * a.y.stride + c * a.y.comp + l * N + n) : x[c];
+  }
+  apply(a.fx, x, mi);
+  apply(a.fy, y, mi);
   if (a.factor != 1) {
     const u64 f = signed_residue(a.factor, mi);
 #pragma unroll
@@ -162,22 +190,24 @@ __device__ __forceinline__ void ct_products(const ProductArgs& a, const ModInfo&
   {
     PairAcc<FP> s;
     s.mac(x, y, mi);
-    const u64 zf = a.z.at ? signed_residue(a.z_factor, mi) : 0;
+    ulonglong2 z[2] = {};
+    u64 zf = 0;
+    if (a.z.at) {
+#pragma unroll
+      for (int c = 0; c < 2; c++) z[c] = word_pair(a.z.at + b * a.z.stride + c * a.z.comp + l * N + n);
+      apply(a.fz, z, mi);
+      zf = signed_residue(a.z_factor, mi);
+    }
 #pragma unroll
     for (int c = 0; c < 3; c++) {
       ulonglong2 w = s.value(c, mi);
-      if (a.z.at && c < 2) {
-        const ulonglong2 z = word_pair(a.z.at + b * a.z.stride + c * a.z.comp + l * N + n);
-        w = {addmod(w.x, prod_mulmod<FP>(z.x, zf, mi), mi.m), addmod(w.y, prod_mulmod<FP>(z.y, zf, mi), mi.m)};
-      }
+      if (a.z.at && c < 2) w = {addmod(w.x, prod_mulmod<FP>(z[c % 2].x, zf, mi), mi.m), addmod(w.y, prod_mulmod<FP>(z[c % 2].y, zf, mi), mi.m)};
       store_product<FP>(a.o, b, c, (u32)l, n, N, w, mi);
     }
   }
   if (a.second) {
-    const u64* p2 = a.x2.at + b * a.x2.stride + l * N + n;
-    const ulonglong2 x2[2] = {word_pair(p2), word_pair(p2 + a.x2.comp)};
     PairAcc<FP> s;
-    s.mac(x2, y, mi);
+    s.mac(y, y, mi);
 #pragma unroll
     for (int c = 0; c < 3; c++) store_product<FP>(a.o, a.second + b, c, (u32)l, n, N, s.value(c, mi), mi);
   }
@@ -187,18 +217,6 @@ __global__ void __launch_bounds__(256) ct_products_kernel(ProductArgs a) {
   const ModInfo mi = a.mods[blockIdx.y];
   if (mod_class(mi.m, a.fp_on) == 0) ct_products<true>(a, mi);
   else ct_products<false>(a, mi);
-}
-
-// m += eps and y = start - m, numbers in every slot. Ciphertexts [B][2][nlimbs][N]; grid = (N / 512, limbs, 2 B).
-__global__ void __launch_bounds__(256) norm_start_kernel(u64* m, u64* y, const ModInfo* mods, long long eps, long long start, u32 logN,
-                                                         u32 nlimbs) {
-  const size_t N = (size_t)1 << logN, at = ((size_t)blockIdx.z * nlimbs + blockIdx.y) * N + (blockIdx.x * 256 + threadIdx.x) * 2;
-  const ModInfo mi = mods[blockIdx.y];
-  const bool first = (blockIdx.z & 1) == 0;
-  const u64 e = first ? signed_residue(eps, mi) : 0, s = first ? signed_residue(start, mi) : 0;
-  const ulonglong2 x = plus_number(word_pair(m + at), e, mi.m);
-  *(ulonglong2*)(m + at) = x;
-  *(ulonglong2*)(y + at) = {submod(s, x.x, mi.m), submod(s, x.y, mi.m)};
 }
 
 // out = pt (.) x on the first nlimbs limbs of ciphertexts, [B][2][nlimbs][N]; grid = (N / 512, limbs, 2 B).

@@ -244,9 +244,9 @@ struct PagedAttn : Decoder {
     long long add = bias;
     for (u32 s = 0; s < squarings; s++) {
       ProductArgs a{};
-      a.x = a.y = cts(u, limbs);
+      a.x = cts(u, limbs);
       a.factor = 1;
-      a.bias = add;
+      a.fx.add = a.fy.add = add;
       if ((rc = products(a, n, limbs, true))) return rc;
       if ((rc = relin(u, d, n, limbs, true))) return rc;
       add = 0;
@@ -340,30 +340,25 @@ struct RmsNorm : Decoder {
   int run(u64* out, u64* h_out, const u64* x, const u64* res, const u64* gain, int64_t square, int64_t eps, int64_t start,
           const int64_t* factors, u32 n) {
     int rc;
-    const u64* in = x;
-    if (res) {
-      u64* to = h_out ? h_out : h;
-      if ((rc = ckks_add(c, (uint64_t*)to, (const uint64_t*)x, (const uint64_t*)res, 2 * n, nlimbs, st))) return rc;
-      in = to;
-    }
+    const u64* in = res ? h_out ? h_out : h : x;
     ProductArgs a{};
-    a.x = a.y = cts(in, nlimbs);
+    a.x = cts(x, nlimbs);
+    a.plus = res;
+    a.sum = res ? const_cast<u64*>(in) : nullptr;
     a.factor = square;
     if ((rc = products(a, n, nlimbs, n1 == 1 && n2 == 1))) return rc;
-    u64* mean;
+    u64* mean;   // without eps, which the products add
     if ((rc = slot_sum(mean, n))) return rc;
     u32 limbs = nlimbs - 1;
-    u64* v = mean == y[0] ? y[1] : y[0];
-    {
-      ProfScope ps(c, PK_NORM_START, st);
-      hipLaunchKernelGGL(norm_start_kernel, dim3(c->N / 512, limbs, 2 * n), dim3(256), 0, st, mean, v, c->d_mods, (long long)eps,
-                         (long long)start, c->logN, limbs);
-      HIP_TRY(hipGetLastError());
-    }
+    // y: start - (mean + eps) until the first step has put it where the mean is not
+    u64 *next = mean == y[0] ? y[1] : y[0], *v = mean;
+    Affine fy{start, eps, 1};
     for (u32 k = 0; k < iterations; k++) {
       ProductArgs p{};
       p.x = cts(mean, nlimbs - 1);
-      p.y = p.x2 = cts(v, limbs);
+      p.fx.add = eps;
+      if (v != mean) p.y = cts(v, limbs);
+      p.fy = fy;
       p.factor = 1;
       p.second = n;
       if ((rc = products(p, n, limbs, true))) return rc;
@@ -373,14 +368,18 @@ struct RmsNorm : Decoder {
       s.y = cts(uw + n * 2 * poly(limbs - 1), limbs - 1);
       s.factor = -1;
       s.z = cts(v, limbs);
+      s.fz = fy;
       s.z_factor = factors[k];
       if ((rc = products(s, n, limbs - 1, true))) return rc;
-      if ((rc = relin(v, d, n, limbs - 1, true))) return rc;
+      if ((rc = relin(next, d, n, limbs - 1, true))) return rc;
+      v = next;
+      fy = Affine{0, 0, 0};
       limbs -= 2;
     }
     ProductArgs e{};
     e.x = cts(in, nlimbs);
     e.y = cts(v, limbs);
+    e.fy = fy;
     e.factor = 1;
     if (gain) {
       {
