@@ -407,6 +407,13 @@ def ckks_linattn_chunk(ctx, o_out, state_out, q, k, v, state_in, decay, tokens, 
                                    ws.numel() * 8, _stream()))
 
 
+def _whole(low, high, **numbers):
+    """Refuses what a C integer would wrap."""
+    for name, v in numbers.items():
+        if not low <= v < high:
+            raise ValueError("%s must be in [%d, %d)" % (name, low, high))
+
+
 def attn_pairs(new_lens, lens, window=0, sinks=0):
     """The number of (query, token) pairs that ckks_attn_paged scores, which its workspace is sized by."""
     total = 0
@@ -449,6 +456,8 @@ def ckks_attn_paged(ctx, o_out, q, nlimbs, new_lens, lens, k_pages, v_pages, pag
                     squarings, n1, n2, stride, evk_mult, evk_baby, evk_giant, ws):
     if len(evk_baby) != n1 - 1 or len(evk_giant) != n2 - 1:
         raise ValueError("need n1-1 baby-step keys and n2-1 giant-step keys")
+    _whole(0, 1 << 32, window=window, sinks=sinks, squarings=squarings)
+    _whole(-(1 << 63), 1 << 63, bias=bias)
     rows = sum(new_lens)
     cache = _cache(ctx, new_lens, lens, k_pages, v_pages, page_tokens, k_limbs, v_limbs)
     _check(_lib.ckks_attn_paged(ctx.handle, _ptr(o_out, "o_out", ctx, max(0, rows * 2 * (nlimbs - 1 - squarings) * ctx.N)),
@@ -466,6 +475,7 @@ def ckks_rmsnorm(ctx, ct_out, h_out, ct_x, ct_res, gain, square, eps, start, fac
                  evk_giant, ws):
     if len(evk_baby) != n1 - 1 or len(evk_giant) != n2 - 1:
         raise ValueError("need n1-1 baby-step keys and n2-1 giant-step keys")
+    _whole(-(1 << 63), 1 << 63, square=square, eps=eps, start=start, **{"factors[%d]" % i: f for i, f in enumerate(factors)})
     e, L = B * 2 * nlimbs * ctx.N, nlimbs - 1 - 2 * len(factors)
     numbers = (C.c_int64 * max(1, len(factors)))(*factors)
     optional = [None if t is None else _ptr(t, name, ctx, n) for t, name, n in

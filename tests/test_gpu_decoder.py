@@ -464,6 +464,8 @@ def test_the_binding_refuses():
                           (ValueError, dict(k_pages=[page, page[:1]])), (ValueError, dict(o_out=new(1, 2, 1, N))), (ValueError, dict(lens=[-1])),
                           (ValueError, dict(q=ct[:, :1].contiguous())), (TypeError, dict(q=ct.cpu())), (TypeError, dict(v_pages=[page, page.float()])),
                           (TypeError, dict(k_pages=[page, page.transpose(0, 1)])), (ValueError, dict(evk_mult=key[:1])), (ValueError, dict(page_tokens=0)),
+                          (ValueError, dict(bias=1 << 63)), (ValueError, dict(bias=-(1 << 63) - 1)), (ValueError, dict(window=-1)), (ValueError, dict(sinks=-1)),
+                          (ValueError, dict(squarings=-1)),
                           (ck.CkksError, dict(k_pages=[None, page])), (ck.CkksError, dict(squarings=3, o_out=new(1, 2, 2, N)))):
         with pytest.raises(error):
             ck.ckks_attn_paged(ctx, **dict(good, **change))
@@ -481,6 +483,7 @@ def test_the_binding_refuses():
                 B=1, nlimbs=nl, n1=1, n2=2, stride=N // 4, evk_mult=key, evk_baby=[], evk_giant=[key], ws=ctx.rmsnorm_workspace(1, nl, 1, 2, 1))
     ck.ckks_rmsnorm(ctx, **norm)
     for error, change in ((ValueError, dict(ct_out=new(1, 2, 1, N // 2))), (ValueError, dict(gain=new(1, N))), (ValueError, dict(evk_giant=[])),
-                          (ck.CkksError, dict(factors=[3, 3])), (TypeError, dict(ct_res=ct.cpu())), (ck.CkksError, dict(ct_out=norm["h_out"]))):
+                          (ck.CkksError, dict(factors=[3, 3])), (ValueError, dict(factors=[1 << 63])), (ValueError, dict(start=1 << 64)),
+                          (TypeError, dict(ct_res=ct.cpu())), (ck.CkksError, dict(ct_out=norm["h_out"]))):
         with pytest.raises(error):
             ck.ckks_rmsnorm(ctx, **dict(norm, **change))
