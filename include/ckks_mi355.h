@@ -388,8 +388,9 @@ int ckks_linattn_chunk(ckks_ctx* ctx, uint64_t* o_out, uint64_t* state_out, cons
  *   q       device [rows][2][nlimbs][N];   o_out device [rows][2][nlimbs - 1 - squarings][N], at the product of u's and v's scale
  *   bias    added to every slot as an integer
  * k_limbs >= nlimbs and v_limbs >= nlimbs - 1 - squarings >= 1; pages that no new token sees may be null. o_out may overlap neither q nor
- * a page that is read. Keys as for ckks_linattn_chunk. Workspace: ckks_attn_workspace_bytes for the number of rows and of (query, token) pairs that see
- * each other, or more of both; beyond a bound that fills the chip it does not grow with the pairs. Rows <= 32767. No rows: nothing is done.
+ * a page that is read. Keys as for ckks_linattn_chunk. Workspace: ckks_attn_workspace_bytes for the number of rows and of (query, token)
+ * pairs that see each other, or more of both; beyond a bound that fills the chip it does not grow with the pairs. Rows <= 32767. No rows:
+ * nothing is done.
  *
  * ckks_rmsnorm: with h = ct_x + ct_res (ct_res NULL: ct_x; the sum is written to h_out if that is given),
  *   m = slotsum'(square h * h) + eps;   y = start - m;

@@ -261,6 +261,11 @@ __global__ void __launch_bounds__(256) rot_sum_kernel(RotSumArgs a) {
 // position and shares the key words among its ciphertexts.
 // Doubles: digits within q / 2, key words below q < 2^50, so that four products stay within 2^101 of H = 1.5 * 2^102, in whose binade
 // sums are multiples of 2^50 and what a product loses in joining H is exact and goes to L: 4 instructions a term, 6 every fourth.
+// 26 ciphertexts of 8 + 3 limbs at 2^16 by 7 rotations and by 7 again took 1337 us in rot_sum_kernel, which fetches a digit's words from
+// the caches once for every rotation, and the digits' last passes; in here 981, with the key words requested 4 rotations ahead 850 (6: the
+// same; moved through registers instead of an unrolled walk: slower). Four ciphertexts a lane share the key words and take 119 registers:
+// two a lane in the integer launches cost 1345 us where four take 1303, and 580 for 552 (64 scores of 7 limbs); tiles of four digits at a
+// time (178 registers) 1088 for 981. What bounds it is issue: 8 double-precision instructions a term beside the butterflies, at 2 to 3 TB/s.
 #define BLOCK_SUM 256
 // The last 8 stages of a transform on a block of 256 elements in one wave, four values a lane: round K (stages 2K, 2K + 1 of the block)
 // holds in lane l the elements (l / S) 4S + i S + l % S, S = 64 >> 2K.

@@ -1026,8 +1026,9 @@ struct KsIo {
   // ciphertexts [B][2][nlimbs][N], whose other two product terms are the addends
   const u64 *prod_a = nullptr, *prod_b = nullptr;
   bool steps = false;          // ring 2^12: one kernel per step (whole_limb said no)
-  // ring 2^12, and two-pass rings with knob 3 at its default, addends add2 only: division by the last main prime too, so that out has a limb less. The
-  // addends come divided by that prime, and P times their last limb (on integer moduli times 2^-64) lies in the accumulators already.
+  // ring 2^12, and two-pass rings with knob 3 at its default, addends add2 only: division by the last main prime too, so that out has a
+  // limb less. The addends come divided by that prime, and P times their last limb (on integer moduli times 2^-64) lies in the
+  // accumulators already.
   bool drop = false;
   int more = KS_PLAIN;         // two-pass rings with knob 3 at its default: KS_WEIGHTED or KS_MAPPED with these arguments
   KsMore more_args = {};
@@ -1315,7 +1316,8 @@ int ks16_moddown_rows(ckks_ctx* c, const LevelTables* lt, u32 B, u32 nlimbs, u64
 
 // Where the last main limb is divided away with the special ones, it is handled as one of them, with integer bodies (JOINED: it is of an
 // integer class, or becomes an integer target of the digits' conversion), if they are of integer classes and the fused conversion takes
-// one source more. Else (APART) it keeps its kind until its coefficients are known.
+// one source more. Else (APART) it keeps its kind until its coefficients are known. A norm of one ciphertext of 12 limbs at 2^16, 3 steps:
+// 1193 us and 70 launches JOINED_FORCED, 1308 and 97 APART.
 enum DropForm { APART = 0, JOINED, JOINED_FORCED };
 DropForm drop_form(const ckks_ctx* c, const LevelTables* lt, u32 nlimbs) {
   if (!two_pass(c) || !lt->dm_rows || c->tune[2] != 0) return APART;

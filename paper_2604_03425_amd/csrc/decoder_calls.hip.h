@@ -85,10 +85,11 @@ struct Decoder {
     for (u32 i = 1; i < n1; i++) baby.push_back(rotation_element(c, (u64)i * stride % slots));
     for (u32 i = 1; i < n2; i++) giant.push_back(rotation_element(c, (u64)i * n1 % slots * stride % slots));
   }
-  // Whether a relinearisation that divides by the last prime too takes the fused kernels of a key switch; products for one go where it
-  // wants them (`more` of product_out).
   // Ring 2^12: whether n ciphertexts go through the kernels that hold whole limbs.
   bool whole(const LevelTables* lt, u32 n, u32 limbs) const { return lt->dm_off12 && whole_limb(cc, n, limbs, false); }
+  // Whether a relinearisation that divides by the last prime too takes the fused kernels of a key switch; products for one go where it
+  // wants them (`more` of product_out). Against a step of sums and a division of their own, us: a norm of 8 ciphertexts of 20 limbs at 2^16
+  // 10 498 -> 9 100, 64 scores of 7 limbs squared twice 2 524 -> 2 370; 2^12: a token of 4 pairs 166 -> 156.
   bool fused(const LevelTables* lt, u32 n, u32 limbs) const { return two_pass(cc) ? cc->tune[3] != 1 : whole(lt, n, limbs); }
   int product_out(ProductOut* o, u64* out, u32 n, u32 limbs, bool more) const {
     int rc;

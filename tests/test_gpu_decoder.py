@@ -487,3 +487,62 @@ def test_the_binding_refuses():
                           (TypeError, dict(ct_res=ct.cpu())), (ck.CkksError, dict(ct_out=norm["h_out"]))):
         with pytest.raises(error):
             ck.ckks_rmsnorm(ctx, **dict(norm, **change))
+
+
+def test_calls_in_flight_on_two_streams():
+    """Two calls at once: the same context, keys and cache, a stream and a workspace each."""
+    import paper_2604_03425_amd as ck
+    for name in ("ring12", "ring13"):
+        p, rc, ctx = contexts(name)
+        nl, n, page = 4, 5, 2
+        s = attention_ref.Shape(p, rc, 2, 2, p.N // 8, seed=31)
+        keys = device_keys(s)
+        k, v, q, x = (s.cts((m,), nl) for m in (n, n, 2, 3))
+        cache = Cache([n], [0], page, nl, nl, p.N, [k], [v])
+        want = [decoder_ref.attention(s, q[i:i + 1], [k], [v], [1], 0, 0, 5 + i, 1) for i in range(2)]
+        want += decoder_ref.rmsnorm(s, x, None, None, 2, 3, 4, [5])[:1]
+        q, x = to_dev(q), to_dev(x)
+        outs = [torch.empty((m, 2, limbs, p.N), dtype=torch.int64, device="cuda") for m, limbs in ((1, nl - 2), (1, nl - 2), (3, 1))]
+        spaces = [ctx.attn_workspace(1, n, nl, 2, 2, 1) for _ in range(2)] + [ctx.rmsnorm_workspace(3, nl, 2, 2, 1)]
+        streams = [torch.cuda.Stream() for _ in range(3)]
+        for trial in range(3):
+            for t in outs + spaces:
+                t.fill_(-1)
+            torch.cuda.synchronize()
+            for i in range(2):
+                with torch.cuda.stream(streams[i]):
+                    ck.ckks_attn_paged(ctx, outs[i], q[i:i + 1], nl, [1], [n], *cache.args, 0, 0, 5 + i, 1, 2, 2, p.N // 8, *keys, spaces[i])
+            with torch.cuda.stream(streams[2]):
+                ck.ckks_rmsnorm(ctx, outs[2], None, x, None, None, 2, 3, 4, [5], 3, nl, 2, 2, p.N // 8, *keys, spaces[2])
+            torch.cuda.synchronize()
+            for got, ref in zip(outs, want):
+                assert_same(to_host(got), ref, "%s, trial %d" % (name, trial))
+
+
+def test_tensors_that_begin_on_an_odd_word():
+    """Rows, pages and a gain 8 bytes behind an aligned place."""
+    import paper_2604_03425_amd as ck
+
+    def odd(x):
+        t = torch.empty(x.size + 1, dtype=torch.int64, device="cuda")[1:].view(x.shape)
+        return t.copy_(to_dev(x))
+
+    for name in ("ring10", "ring12", "ring13"):
+        p, rc, ctx = contexts(name)
+        nl, n = 4, 3
+        s = attention_ref.Shape(p, rc, 2, 1, p.N // 4, seed=41)
+        keys = device_keys(s)
+        k, v, q, x, r = (s.cts((m,), nl) for m in (n, n, 1, 2, 2))
+        gain = s.draw(p.q[:2], ())
+        want = decoder_ref.attention(s, q, [k], [v], [1], 0, 0, 5, 1)
+        kp, vp = ([odd(np.zeros((n, 2, nl, p.N), dtype=np.uint64))] for _ in range(2))
+        assert kp[0].data_ptr() % 16 == 8
+        o = odd(np.zeros((1, 2, nl - 2, p.N), dtype=np.uint64))
+        ck.ckks_kv_append(ctx, odd(k), odd(v), nl, [n], [n], kp, vp, n, nl, nl)
+        ck.ckks_attn_paged(ctx, o, odd(q), nl, [1], [n], kp, vp, n, nl, nl, 0, 0, 5, 1, 2, 1, p.N // 4, *keys, ctx.attn_workspace(1, n, nl, 2, 1, 1))
+        assert_same(to_host(o), want, "attention " + name)
+        want, want_h = decoder_ref.rmsnorm(s, x, r, gain, 2, 3, 4, [5])
+        out, h = odd(np.zeros((2, 2, 1, p.N), dtype=np.uint64)), odd(np.zeros((2, 2, nl, p.N), dtype=np.uint64))
+        ck.ckks_rmsnorm(ctx, out, h, odd(x), odd(r), odd(gain), 2, 3, 4, [5], 2, nl, 2, 1, p.N // 4, *keys, ctx.rmsnorm_workspace(2, nl, 2, 1, 1))
+        assert_same(to_host(out), want, "norm " + name)
+        assert_same(to_host(h), want_h, "sum " + name)
