@@ -152,7 +152,7 @@ int launch_rot_sum(const ckks_ctx* c, RotSumArgs& a, u32 B, hipStream_t st, u32 
       if ((a.doubles && host_class(c, c->mod[emap.id[s]]) == 0 && !(last_int && s + 1 == a.nlimbs)) == (fp == 1)) a.slots[cnt++] = (unsigned char)s;
     if (fp) a.nfp = cnt;
   }
-  ProfScope ps(c, PK_ROT_SUM, st);
+  ProfScope ps(c, near ? PK_BLOCK_SUM : PK_ROT_SUM, st);
   if (near) {
     const u32 groups = (B + 3) / 4;
     switch ((B + groups - 1) / groups) {   // ciphertexts a lane, as even as possible

@@ -18,7 +18,7 @@ q = find_ntt_primes(q_bits, nq, logN)
 p = find_ntt_primes(p_bits, np, logN, exclude=set(q)) if np else []
 lib = C.CDLL(sys.argv[1])
 lib.ckks_attn_workspace_bytes.restype = lib.ckks_rmsnorm_workspace_bytes.restype = lib.ckks_workspace_bytes.restype = C.c_size_t
-lib.ckks_last_error.restype = C.c_char_p
+lib.ckks_last_error.restype = lib.ckks_prof_kind_name.restype = C.c_char_p
 array = lambda v: (C.c_uint64 * max(1, len(v)))(*v)
 u32s = lambda v: None if v is None else (C.c_uint32 * max(1, len(v)))(*v)
 ptrs = lambda v: None if v is None else (C.c_void_p * max(1, len(v)))(*v)
@@ -38,6 +38,8 @@ for j in jobs:
     if kind == "norm_bytes":
         out.append(lib.ckks_rmsnorm_workspace_bytes(ctx, j["B"], j["nl"], j["n1"], j["n2"], j["its"]))
         continue
+    if j.get("profile"):
+        lib.ckks_prof_enable(ctx, 1)
     if kind == "append":
         rc = lib.ckks_kv_append(ctx if j["ctx"] else None, at(j["k"]), at(j["v"]), j["inl"], len(j["lens"] or []), u32s(j["new"]), u32s(j["lens"]),
                                 ptrs(j["kp"]), ptrs(j["vp"]), j["page"], j["kl"], j["vl"], at(1 << 50))
@@ -52,6 +54,15 @@ for j in jobs:
                               C.c_int64(1 << 50), i64s(j["factors"]), j["its"], j["B"], j["nl"], j["n1"], j["n2"], j["stride"],
                               at(j["mult"]), ptrs(j["baby"]), ptrs(j["giant"]), at(j["ws"]), C.c_size_t(n), at(1 << 50))
     out.append([rc, lib.ckks_last_error().decode() if rc else ""])
+    if j.get("profile"):
+        lib.ckks_prof_collect(ctx)
+        lib.ckks_prof_enable(ctx, 0)
+        out[-1].append({})
+        for i in range(lib.ckks_prof_num_kinds()):
+            ms, count = C.c_double(), C.c_uint64()
+            lib.ckks_prof_read(ctx, i, C.byref(ms), C.byref(count))
+            out[-1][-1][lib.ckks_prof_kind_name(i).decode()] = count.value
+        lib.ckks_prof_reset(ctx)
 flush(None)
 print(json.dumps(out), file=sys.stderr)
 """
@@ -179,3 +190,18 @@ def test_launches_of_one_token(shape, most):
     assert [g[0] for g in got] == [0, 0, 0]
     assert len(launched[0]) == 1
     assert len(launched[1]) <= most[0] and len(launched[2]) <= most[1], [len(x) for x in launched]
+
+
+@pytest.mark.parametrize("shape", [(10, 50, 5, 60, 2, 3), (12, 45, 5, 60, 2, 3), (13, 50, 5, 60, 2, 3)])
+@pytest.mark.parametrize("stride", [1, 64])
+def test_the_profile_names_the_kernels_that_ran(shape, stride):
+    """Rotations by 1 leave their blocks of 256 positions, those by 64 stay in them: 5^64 = 1 mod 2N / 256."""
+    change = dict(stride=stride, profile=True)
+    got, launched = answers(shape, [dict(APPEND, profile=True), dict(ATTN, **change), dict(NORM, **change)])
+    for (code, _, counts), names in zip(got, launched):
+        assert code == 0
+        for name in ("pair_products_kernel", "weighted_values_kernel", "ct_products_kernel", "kv_append_kernel", "rot_sum_kernel",
+                     "block_sum_kernel"):
+            assert counts[name] == sum(name in k for k in names), name
+        assert sum(counts.values()) == len(names)
+    assert any("block_sum_kernel" in k for k in launched[2]) == (stride == 64)
