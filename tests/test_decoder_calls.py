@@ -195,7 +195,7 @@ def test_launches_of_one_token(shape, most):
 @pytest.mark.parametrize("shape", [(10, 50, 5, 60, 2, 3), (12, 45, 5, 60, 2, 3), (13, 50, 5, 60, 2, 3)])
 @pytest.mark.parametrize("stride", [1, 64])
 def test_the_profile_names_the_kernels_that_ran(shape, stride):
-    """Rotations by 1 leave their blocks of 256 positions, those by 64 stay in them: 5^64 = 1 mod 2N / 256."""
+    """A rotation by 1 leaves its block of 256 positions, those by multiples of 64 stay in them: 5^64 = 1 mod 2N / 256."""
     change = dict(stride=stride, profile=True)
     got, launched = answers(shape, [dict(APPEND, profile=True), dict(ATTN, **change), dict(NORM, **change)])
     for (code, _, counts), names in zip(got, launched):
@@ -204,4 +204,4 @@ def test_the_profile_names_the_kernels_that_ran(shape, stride):
                      "block_sum_kernel"):
             assert counts[name] == sum(name in k for k in names), name
         assert sum(counts.values()) == len(names)
-    assert any("block_sum_kernel" in k for k in launched[2]) == (stride == 64)
+    assert any("rot_sum_kernel" in k for k in launched[2]) == (stride == 1)
