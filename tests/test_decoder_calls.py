@@ -204,4 +204,4 @@ def test_the_profile_names_the_kernels_that_ran(shape, stride):
                      "block_sum_kernel"):
             assert counts[name] == sum(name in k for k in names), name
         assert sum(counts.values()) == len(names)
-    assert any("rot_sum_kernel" in k for k in launched[2]) == (stride == 1)
+    assert any(("block_sum_kernel" if stride == 64 else "rot_sum_kernel") in k for k in launched[2])
