@@ -534,18 +534,20 @@ __device__ __forceinline__ void block_sum_fp(const RotSumArgs& a, u32 what, u32 
       });
   tile = (double*)sm + (tile == (double*)sm ? Fill::DIGITS * CB * BLOCK_SUM : 0);
   if (main_prime) {   // P (base + sum of the rotated first components), P base
-    const u64* c0 = a.term[0].c0 + (size_t)t * N + n;
-    double v[CB];
+    double v[CB] = {};
+    if (a.term[0].c0) {   // uniform
+      const u64* c0 = a.term[0].c0 + (size_t)t * N + n;
 #pragma unroll
-    for (int k = 0; k < CB; k++) tile[k * BLOCK_SUM + tid] = u2d(c0[(size_t)bb[k] * a.d_stride]), v[k] = 0.0;
-    lds_barrier();
-    for (u32 r = 0; r < R; r++) {
-      const u32 m = galois_src_index(n, a.term[r].galois, a.logN) & (BLOCK_SUM - 1);
+      for (int k = 0; k < CB; k++) tile[k * BLOCK_SUM + tid] = u2d(c0[(size_t)bb[k] * a.d_stride]);
+      lds_barrier();
+      for (u32 r = 0; r < R; r++) {
+        const u32 m = galois_src_index(n, a.term[r].galois, a.logN) & (BLOCK_SUM - 1);
 #pragma unroll
-      for (int k = 0; k < CB; k++) v[k] += tile[k * BLOCK_SUM + m];
-      if ((r & 3) == 3) {
+        for (int k = 0; k < CB; k++) v[k] += tile[k * BLOCK_SUM + m];
+        if ((r & 3) == 3) {
 #pragma unroll
-        for (int k = 0; k < CB; k++) v[k] = fp_reduce(v[k], qinv, q);
+          for (int k = 0; k < CB; k++) v[k] = fp_reduce(v[k], qinv, q);
+        }
       }
     }
     const double pm = u2d(mi.pmod);
@@ -669,19 +671,21 @@ __device__ __forceinline__ void block_sum_int(const RotSumArgs& a, u32 what, u32
       });
   tile = sm + (tile == sm ? Fill::DIGITS * CB * BLOCK_SUM : 0);
   if (main_prime) {
-    const u64* c0 = a.term[0].c0 + (size_t)t * N + n;
     const u32 p0 = (u32)mi.pmod & M30, p1 = (u32)(mi.pmod >> 30);
+    if (a.term[0].c0) {   // uniform
+      const u64* c0 = a.term[0].c0 + (size_t)t * N + n;
 #pragma unroll
-    for (int k = 0; k < CB; k++) tile[k * BLOCK_SUM + tid] = c0[(size_t)bb[k] * a.d_stride];
-    lds_barrier();
-    for (u32 r = 0; r < R; r++) {
-      const u32 m = galois_src_index(n, a.term[r].galois, a.logN) & (BLOCK_SUM - 1);
+      for (int k = 0; k < CB; k++) tile[k * BLOCK_SUM + tid] = c0[(size_t)bb[k] * a.d_stride];
+      lds_barrier();
+      for (u32 r = 0; r < R; r++) {
+        const u32 m = galois_src_index(n, a.term[r].galois, a.logN) & (BLOCK_SUM - 1);
 #pragma unroll
-      for (int k = 0; k < CB; k++) {
-        const u64 x = tile[k * BLOCK_SUM + m];
-        dot30n_mac(s0[k], (u32)x & M30, (u32)(x >> 30), p0, p1);
+        for (int k = 0; k < CB; k++) {
+          const u64 x = tile[k * BLOCK_SUM + m];
+          dot30n_mac(s0[k], (u32)x & M30, (u32)(x >> 30), p0, p1);
+        }
+        carry();
       }
-      carry();
     }
     if (a.base) {
 #pragma unroll

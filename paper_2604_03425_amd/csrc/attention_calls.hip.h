@@ -193,29 +193,33 @@ int rotations_to_ext(ckks_ctx* c, const LevelTables* lt, bool whole, const u64* 
   return CKKS_OK;
 }
 
-// out = ct + its rotations by galois[r] with one ModDown, by P or (drop) by P q_{nlimbs-1}; R > 0, ws: a key-switch workspace for B.
+// What near_sums decomposes (limb t of number b at d + b * d_stride + t * N), rotates beside it (c0, the same stride; null: nothing) and
+// adds as it is (two components, N nlimbs words apart).
+struct NearIn {
+  const u64 *d, *c0;
+  u64 d_stride;
+  const u64* base;
+  u64 base_stride;
+};
+// out = base + the rotations by galois[r] with one ModDown, by P or (drop) by P q_{nlimbs-1}; R > 0, ws: a key-switch workspace for B.
 // Unweighted near rotations on two-pass rings: digits go through their last stages and the special limbs through their first inverse ones
 // in the sums' kernel, which comes first for the special limbs and then for the main ones, whose sums it finishes: neither the
 // transformed digits nor the main limbs' sums reach memory. Where all workgroups are one round (BLOCK_SUM_ROUND) the limbs go together and
 // the assembly is a kernel of its own. us, together | apart: attention of four ragged sequences at 2^13, 672 workgroups, 318 | 336; norms of 5
-// ciphertexts at 2^14, 1280, 604 | 611, of one of 12 limbs at 2^16, 4096, 1151 | 1161; 26 pairs of 64 components there 3829 | 3579. Otherwise
-// *done is false and nothing happens.
+// ciphertexts at 2^14, 1280, 604 | 611, of one of 12 limbs at 2^16, 4096, 1151 | 1161; 26 pairs of 64 components there 3829 | 3579.
 #define BLOCK_SUM_ROUND 4096
-int sum_near_rotations(ckks_ctx* c, const LevelTables* lt, u64* out, const u64* ct, u32 B, u32 nlimbs, const u32* galois,
-                       const u64* const* evks, u32 R, bool drop, char* ws, hipStream_t st, bool* done) {
+int near_sums(ckks_ctx* c, const LevelTables* lt, u64* out, const NearIn& in, u32 B, u32 nlimbs, const u32* galois, const u64* const* evks,
+              u32 R, bool drop, char* ws, hipStream_t st) {
   int rc;
-  *done = two_pass(c) && rotations_near(c, galois, R);
-  if (!*done) return CKKS_OK;
-  const u64 pl = (u64)nlimbs * c->N;
   const KsLayout L = ks_layout(c, B, nlimbs);
   u64 *acc = (u64*)(ws + L.acc), *tq = (u64*)(ws + L.tq);
   const u64* ext = (const u64*)(ws + L.ext);
   const DropForm form = drop ? drop_form(c, lt, nlimbs) : APART;
   const bool last_int = form == JOINED_FORCED;
   const u32 keep = drop ? nlimbs - 1 : nlimbs;
-  if ((rc = ext_digits(c, lt, false, ct + pl, 2 * pl, B, nlimbs, ws, st, last_int, true))) return rc;
-  RotSumArgs a = rot_sum_args(c, lt, false, nlimbs, acc, 2 * pl);
-  a.base_stride = 2 * pl;
+  if ((rc = ext_digits(c, lt, false, in.d, in.d_stride, B, nlimbs, ws, st, last_int, true))) return rc;
+  RotSumArgs a = rot_sum_args(c, lt, false, nlimbs, acc, in.d_stride);
+  a.base_stride = in.base_stride;
   a.tw = c->d_tw_fwd;
   a.twi = c->d_tw_inv;
   a.twfp = c->d_twfp_fwd;
@@ -224,13 +228,13 @@ int sum_near_rotations(ckks_ctx* c, const LevelTables* lt, u64* out, const u64* 
   a.fin_pinv = drop ? lt->dm_pinv2 : lt->pinv2;
   a.fin_limbs = keep;
   auto sums = [&](u32 from, u32 to) {
-    a.base = ct;
+    a.base = in.base;
     a.accumulate = 0;
     for (u32 r0 = 0; r0 < R; r0 += ROT_SUM_TERMS) {
       a.nterms = std::min<u32>(ROT_SUM_TERMS, R - r0);
       a.inverse = r0 + a.nterms == R;
       a.fin_tq = to <= keep && a.inverse ? tq : nullptr;
-      for (u32 r = 0; r < a.nterms; r++) a.term[r] = RotTerm{ext, ct + pl, ct, evks[r0 + r], galois[r0 + r]};
+      for (u32 r = 0; r < a.nterms; r++) a.term[r] = RotTerm{ext, in.d, in.c0, evks[r0 + r], galois[r0 + r]};
       if (int e = launch_rot_sum(c, a, B, st, 1, true, last_int, from, to)) return e;
       a.base = nullptr;
       a.accumulate = 1;
@@ -252,6 +256,14 @@ int sum_near_rotations(ckks_ctx* c, const LevelTables* lt, u64* out, const u64* 
   else rc = ks16_moddown_rows(c, lt, B, nlimbs, acc, tq, st, true);
   if (rc) return rc;
   return sums(0, keep);
+}
+// The sum of a ciphertext and its rotations this way, if they are near ones on a two-pass ring. Otherwise *done is false and nothing happens.
+int sum_near_rotations(ckks_ctx* c, const LevelTables* lt, u64* out, const u64* ct, u32 B, u32 nlimbs, const u32* galois,
+                       const u64* const* evks, u32 R, bool drop, char* ws, hipStream_t st, bool* done) {
+  *done = two_pass(c) && rotations_near(c, galois, R);
+  if (!*done) return CKKS_OK;
+  const u64 pl = (u64)nlimbs * c->N;
+  return near_sums(c, lt, out, NearIn{ct + pl, ct, 2 * pl, ct, 2 * pl}, B, nlimbs, galois, evks, R, drop, ws, st);
 }
 
 // ---- linear attention ----

@@ -90,7 +90,13 @@ struct Decoder {
   // Whether a relinearisation that divides by the last prime too takes the fused kernels of a key switch; products for one go where it
   // wants them (`more` of product_out). Against a step of sums and a division of their own, us: a norm of 8 ciphertexts of 20 limbs at 2^16
   // 10 498 -> 9 100, 64 scores of 7 limbs squared twice 2 524 -> 2 370; 2^12: a token of 4 pairs 166 -> 156.
-  bool fused(const LevelTables* lt, u32 n, u32 limbs) const { return two_pass(cc) ? cc->tune[3] != 1 : whole(lt, n, limbs); }
+  bool fused(const LevelTables* lt, u32 n, u32 limbs) const { return two_pass(cc) ? cc->tune[3] != 1 && !few(lt, n) : whole(lt, n, limbs); }
+  // Two-pass rings: whether n ciphertexts are so few that the sum of one rotation, by nothing, is sooner there than the fused kernels of a
+  // key switch, which end in longer ones. In blocks of 256 words, us fused | as a sum: a norm of one ciphertext at 2^13 (relinearisations
+  // of up to 512) 381 | 331, at 2^14 (up to 1152) 419 | 383, at 2^15 (up to 2816) 527 | 503 (516 without those above 1536), of 3 at 2^14
+  // (up to 1920) 490 | 487; attention of one token with itself at 2^13 186 | 162. Above: 13 ciphertexts at 2^13 (2912, 2496) 312 | 306, 5 at
+  // 2^14 (2560) 601 | 603, 4 of 60-bit primes at 2^15 (4096) 1099 | 1106.
+  bool few(const LevelTables* lt, u32 n) const { return two_pass(cc) && (u64)n * (cc->N / BLOCK_SUM) * lt->next <= 2048; }
   int product_out(ProductOut* o, u64* out, u32 n, u32 limbs, bool more) const {
     int rc;
     *o = ProductOut{out, nullptr, nullptr, 0, limbs, 0};
@@ -107,10 +113,12 @@ struct Decoder {
   // Relin of products in three components (at `limbs` limbs); more: dividing by the last prime too.
   int relin(u64* out, const u64* in, u32 n, u32 limbs, bool more) {
     int rc;
-    if (!more) return ckks_relin(c, (uint64_t*)out, (const uint64_t*)in, n, limbs, (const uint64_t*)mult_key, ks, ks_bytes, st);
     const LevelTables* lt;
     if ((rc = get_level(c, limbs, &lt))) return rc;
     const u64 pl = poly(limbs);
+    const u32 nothing = 1;   // as a Galois element
+    if (few(lt, n)) return near_sums(c, lt, out, NearIn{in + 2 * pl, nullptr, 3 * pl, in, 3 * pl}, n, limbs, &nothing, &mult_key, 1, more, ks, st);
+    if (!more) return ckks_relin(c, (uint64_t*)out, (const uint64_t*)in, n, limbs, (const uint64_t*)mult_key, ks, ks_bytes, st);
     if (fused(lt, n, limbs)) {
       KsIo io{in + 2 * pl, 3 * pl, 0, out, {1, 1}, nullptr, 0};
       io.add2 = in;

@@ -546,3 +546,12 @@ def test_tensors_that_begin_on_an_odd_word():
         ck.ckks_rmsnorm(ctx, out, h, odd(x), odd(r), odd(gain), 2, 3, 4, [5], 2, nl, 2, 1, p.N // 4, *keys, ctx.rmsnorm_workspace(2, nl, 2, 1, 1))
         assert_same(to_host(out), want, "norm " + name)
         assert_same(to_host(h), want_h, "sum " + name)
+
+
+@pytest.mark.parametrize("name,nl,n1,n2,squarings", [
+    ("ring13", 5, 2, 2, 1), ("ring13_int", 5, 1, 1, 1), ("ring13_mixed", 5, 2, 1, 2), ("ring13_fp", 5, 1, 2, 1), ("ring14", 7, 2, 2, 1),
+    ("ring14_wide", 10, 1, 2, 1), ("ring14_eight", 7, 1, 1, 1)])
+def test_relinearisations_of_many_ciphertexts(name, nl, n1, n2, squarings):
+    """34 pairs, and 17 ciphertexts of a norm: the fused kernels of a key switch, where most shapes above are few enough for those of sums."""
+    run_attention(name, nl, (34,), (1,), 7, 0, 0, squarings, n1, n2)
+    run_norm(name, nl, 17, n1, n2, 1, True, True)
