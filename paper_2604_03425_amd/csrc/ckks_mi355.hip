@@ -1529,8 +1529,9 @@ bool int_sums_stored(const ckks_ctx* c, u32 B, u32 nlimbs, bool product) {
 // With knob 3 = 1 the main limbs' accumulators are stored (integer-class ones by step 3, double-precision ones by a plain block
 // pass and a streaming product) and the assembly kernel replaces step 5. With knob 4 = 0 the double-precision row pass of step 2,
 // where it is a kernel of its own, runs on the context's second stream beside the integer-class kernels of step 3 and step 4, which
-// do not depend on it, and is joined before the first kernel that reads what it leaves: step 5's, or with knob 3 = 1 the block
-// pass of step 3.
+// do not depend on it, and is joined before the first kernel that reads what it leaves: step 5's, with knob 3 = 1 the block
+// pass of step 3, and where the division takes a double-precision main prime too (io.drop) the kernel that forms that limb's
+// sums ahead of step 4.
 // acc_add != null (knob 3 at its default only): the sequence stops before ModDown and ADDS the two accumulators, plus
 // P * sigma(io.add_src component 0) on the main primes of the first, to acc_add ([B][2][next][N]).
 int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B, u32 nlimbs, const u64* evk, char* ws,
@@ -1716,6 +1717,7 @@ int keyswitch_fused16(ckks_ctx* c, const LevelTables* lt, const KsIo& io, u32 B,
     a.twi = nullptr;
     a.slots[0] = (unsigned char)keep;
     const int cls = ext_class(keep);
+    if (fork && cls == 0) HIP_TRY(hipStreamWaitEvent(st, c->ev_join, 0));
     ProfScope ps(c, cls == 0 ? (int)PK_INNER_C : PK_INNER8 + cls - 1, st);
     const dim3 grid(B, N / 2048, 1);
     if (cls == 0) launch_inner_c(c, B, 1, a, st);

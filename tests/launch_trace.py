@@ -61,7 +61,7 @@ for bits in q_bits + p_bits:
     primes += find_ntt_primes(bits, 1, logN, exclude=set(primes))
 nq = len(q_bits)
 lib = C.CDLL(sys.argv[1])
-lib.ckks_workspace_bytes.restype = C.c_size_t
+for f in (lib.ckks_workspace_bytes, lib.ckks_attn_workspace_bytes, lib.ckks_rmsnorm_workspace_bytes): f.restype = C.c_size_t
 lib.ckks_last_error.restype = C.c_char_p
 def array(v): return (C.c_uint64 * len(v))(*v)
 def check(rc):
@@ -80,6 +80,14 @@ for call in calls:
     if call == "hmult": check(lib.ckks_hmult_relin(ctx, out, a, b, B, nl, key, ws, n, st))
     if call == "ntt": check(lib.ckks_ntt(ctx, a, B, ids, nl, st))
     if call == "intt": check(lib.ckks_intt(ctx, a, B, ids, nl, st))
+    if call == "attn":      # one new token, its scores squared once
+        n = C.c_size_t(lib.ckks_attn_workspace_bytes(ctx, 1, C.c_uint64(B), nl, 1, 1, 1))
+        check(lib.ckks_attn_paged(ctx, out, a, nl, 1, (C.c_uint32 * 1)(1), (C.c_uint32 * 1)(B), (C.c_void_p * 1)(7 << 40),
+                                  (C.c_void_p * 1)(8 << 40), B, nl, nl, 0, 0, C.c_int64(1), 1, 1, 1, 1, key, None, None, ws, n, st))
+    if call == "norm":      # one step
+        n = C.c_size_t(lib.ckks_rmsnorm_workspace_bytes(ctx, B, nl, 1, 1, 1))
+        check(lib.ckks_rmsnorm(ctx, out, None, a, None, None, C.c_int64(1), C.c_int64(1), C.c_int64(1), (C.c_int64 * 1)(1), 1, B, nl,
+                               1, 1, 1, key, None, None, ws, n, st))
 """
 
 _folder = None
@@ -99,8 +107,8 @@ def _runtime():
 
 
 def trace(shape, knobs, nl=0, B=2, calls=("hrot", "hmult")):
-    """("launch", stream, kernel), ("record" or "wait", stream, event) of `calls` on B ciphertexts (transforms: polynomials)
-    of nl limbs (0: all). shape: logN, sizes of the main primes, of the special primes, digits."""
+    """("launch", stream, kernel), ("record" or "wait", stream, event) of `calls` on B ciphertexts (transforms: polynomials;
+    attention: cached tokens) of nl limbs (0: all). shape: logN, sizes of the main primes, of the special primes, digits."""
     import paper_2604_03425_amd as pkg
     env = dict(os.environ, LD_LIBRARY_PATH=_runtime(), PYTHONPATH=ROOT)
     res = subprocess.run([sys.executable, "-c", CALLS, pkg.library_path(),

@@ -555,3 +555,28 @@ def test_relinearisations_of_many_ciphertexts(name, nl, n1, n2, squarings):
     """34 pairs, and 17 ciphertexts of a norm: the fused kernels of a key switch, where most shapes above are few enough for those of sums."""
     run_attention(name, nl, (34,), (1,), 7, 0, 0, squarings, n1, n2)
     run_norm(name, nl, 17, n1, n2, 1, True, True)
+
+
+@pytest.mark.parametrize("name,knobs", [("ring13", {2: 2, 4: 0}), ("ring13", {2: 1, 4: 0}), ("ring13_two_kinds", {4: 0}), ("ring13_nine", {4: 0})])
+def test_the_second_stream_changes_no_result(name, knobs):
+    """Shapes whose relinearisations by a main prime too run part of a key switch on the context's second stream: 13 pairs and ciphertexts at 2^13
+    are above those that go as sums."""
+    import paper_2604_03425_amd as ck
+
+    def two_kinds():
+        q, p = find_ntt_primes(60, 1, 13) + find_ntt_primes(50, 3, 13), find_ntt_primes(60, 3, 13)[1:]
+        return CkksParams(logN=13, q=q, p=p, dnum=2, psi=[find_psi(m, 13) for m in q + p])
+
+    PARAMS.setdefault("ring13_two_kinds", two_kinds)
+    PARAMS.setdefault("ring13_nine", lambda: make_params(13, 9, 50, 9, 60, 1))
+    p, rc, ctx = contexts(name)
+    nl = min(len(p.q), 5) if name != "ring13_nine" else 9
+    try:
+        for knob, value in knobs.items():
+            ck.ckks_tune_set(ctx, knob, value)
+        for _ in range(3):
+            run_attention(name, nl, (13,), (1,), 5, 0, 0, 1, 1, 1)
+        run_norm(name, nl, 13, 1, 1, 1, False, False)
+    finally:
+        for knob, value in {2: 0, 4: 1}.items():
+            ck.ckks_tune_set(ctx, knob, value)

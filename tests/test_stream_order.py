@@ -44,3 +44,25 @@ def test_second_stream_is_joined_before_its_digits_are_read(shape, knobs):
             assert after >= {k for k in side if k < i}, (name, "is not ordered after the row pass on the second stream")
     assert readers >= 2
     assert launches[-1][2] >= set(side)   # and the caller's stream goes on only after it
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("knobs", [{4: 0}, {2: 1, 4: 0}, {2: 2, 4: 0}])
+@pytest.mark.parametrize("call", ["attn", "norm"])
+def test_divisions_by_a_main_prime_too_read_joined_digits(shape, knobs, call):
+    """Relinearisations of 40 ciphertexts and more, which take the fused kernels of a key switch: the last main limb's sums are formed before
+    the division and read converted digits like the others'."""
+    steps = trace(shape, knobs, B=40, calls=(call,))
+    launches = _before(steps)
+    main = launches[0][1]
+    side = [i for i, (_, stream, _) in enumerate(launches) if stream != main]
+    fused = shape[1] == [50] * 4 and 2 not in knobs
+    assert bool(side) != fused
+    readers = 0
+    for i, (name, stream, after) in enumerate(launches):
+        assert stream == main or "rows_kernelILi0E" in name
+        if "blocks_inner_c_kernel" in name:
+            readers += 1
+            assert after >= {k for k in side if k < i}, (name, "is not ordered after the row pass on the second stream")
+    assert readers >= 2
+    assert launches[-1][2] >= set(side)
