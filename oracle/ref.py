@@ -63,6 +63,11 @@ def set_threads(n):
     lib().ref_set_threads(C.c_int(int(n)))
 
 
+def set_team(n):
+    """Threads that a call may use in all: where it has fewer ciphertexts, the others share the limbs and coefficients of each."""
+    lib().ref_set_team(C.c_int(int(n)))
+
+
 class RefContext:
     """Oracle context for one parameter set (ckks_inputs.CkksParams)."""
 

@@ -40,7 +40,36 @@ typedef unsigned __int128 u128;
 namespace {
 
 thread_local std::string g_err;
-int g_threads = 1;
+int g_threads = 1;            // ciphertexts worked on at a time
+int g_team = 1;               // threads that a call may use in all, where it has fewer ciphertexts: the others share their limbs
+thread_local int t_team = 1;  // those of this ciphertext
+
+template <class F>
+void run_threads(size_t n, int nt, int team, F f) {
+  std::vector<std::thread> th;
+  for (int t = 0; t < nt; t++)
+    th.emplace_back([=]() {
+      t_team = team;
+      for (size_t i = t; i < n; i += nt) f(i);
+    });
+  for (auto& x : th) x.join();
+}
+// f(i) for i < n, ciphertexts or limb-vectors of a batch.
+template <class F>
+void parallel_for(size_t n, F f) {
+  const int nt = std::max(1, (int)std::min<size_t>(std::max(g_threads, g_team), n)), team = std::max(1, g_team / nt);
+  if (nt > 1) return run_threads(n, nt, team, f);
+  t_team = team;
+  for (size_t i = 0; i < n; i++) f(i);
+  t_team = 1;
+}
+// f(i) for i < n parts of one ciphertext of `words` coefficients each; small ones are not worth a thread.
+template <class F>
+void parts_for(size_t n, size_t words, F f) {
+  const int nt = (int)std::min<size_t>({(size_t)t_team, n, n * words / 4096});
+  if (nt > 1) return run_threads(n, nt, 1, f);
+  for (size_t i = 0; i < n; i++) f(i);
+}
 
 inline u64 addm(u64 a, u64 b, u64 m) { u128 s = (u128)a + b; return (u64)(s % m); }
 inline u64 subm(u64 a, u64 b, u64 m) { return (u64)(((u128)a + m - (b % m)) % m); }
@@ -229,38 +258,25 @@ BConvPlan make_bconv(const std::vector<u64>& src, const std::vector<u64>& dst) {
 }
 // in: nsrc pointers (coefficient domain), out: ndst pointers; n coefficients.
 void bconv_apply(const BConvPlan& p, const std::vector<const u64*>& in, const std::vector<u64*>& out, size_t n) {
-  const size_t ns = p.src.size(), nd = p.dst.size();
-  for (size_t k = 0; k < n; k++) {
-    Big pos(1, 0), neg(1, 0);
-    for (size_t i = 0; i < ns; i++) {
-      u64 ci = p.src[i];
-      u64 y = mulm(in[i][k] % ci, p.chat_inv[i], ci);
-      bool negative = y > ci / 2;  // centred representative is y - c_i
-      u64 mag = negative ? ci - y : y;
-      Big term = p.chat[i];
-      big_mul_word(term, mag);
-      big_add(negative ? neg : pos, term);
+  const size_t ns = p.src.size(), nd = p.dst.size(), piece = 1024;
+  parts_for((n + piece - 1) / piece, piece, [&](size_t part) {
+    for (size_t k = part * piece; k < std::min(n, (part + 1) * piece); k++) {
+      Big pos(1, 0), neg(1, 0);
+      for (size_t i = 0; i < ns; i++) {
+        u64 ci = p.src[i];
+        u64 y = mulm(in[i][k] % ci, p.chat_inv[i], ci);
+        bool negative = y > ci / 2;  // centred representative is y - c_i
+        u64 mag = negative ? ci - y : y;
+        Big term = p.chat[i];
+        big_mul_word(term, mag);
+        big_add(negative ? neg : pos, term);
+      }
+      for (size_t t = 0; t < nd; t++) {
+        u64 m = p.dst[t];
+        out[t][k] = subm(big_mod_word(pos, m), big_mod_word(neg, m), m);
+      }
     }
-    for (size_t t = 0; t < nd; t++) {
-      u64 m = p.dst[t];
-      out[t][k] = subm(big_mod_word(pos, m), big_mod_word(neg, m), m);
-    }
-  }
-}
-
-template <class F>
-void parallel_for(size_t n, F f) {
-  int nt = std::max(1, std::min<int>(g_threads, (int)n));
-  if (nt == 1) {
-    for (size_t i = 0; i < n; i++) f(i);
-    return;
-  }
-  std::vector<std::thread> th;
-  for (int t = 0; t < nt; t++)
-    th.emplace_back([=]() {
-      for (size_t i = t; i < n; i += nt) f(i);
-    });
-  for (auto& x : th) x.join();
+  });
 }
 
 int fail(const std::string& s) {
@@ -288,7 +304,7 @@ std::vector<u64> keyswitch_accumulate(const RefCtx* c, const u64* d, int nlimbs,
 
   // coefficient form of d
   std::vector<u64> dc(d, d + (size_t)nlimbs * N);
-  for (int i = 0; i < nlimbs; i++) intt_fast(c, &dc[(size_t)i * N], i);
+  parts_for(nlimbs, N, [&](size_t i) { intt_fast(c, &dc[i * N], (int)i); });
 
   std::vector<u64> acc((size_t)2 * next * N, 0);
   std::vector<u64> dig((size_t)next * N);
@@ -308,10 +324,10 @@ std::vector<u64> keyswitch_accumulate(const RefCtx* c, const u64* d, int nlimbs,
     }
     BConvPlan plan = make_bconv(src, dst);
     bconv_apply(plan, in, out, N);
-    for (int t = 0; t < next; t++) {
+    parts_for(next, N, [&](size_t t) {
       int id = ext_id[t];
       u64 m = c->mod[id];
-      u64* x = &dig[(size_t)t * N];
+      u64* x = &dig[t * N];
       ntt_fast(c, x, id);
       const u64* kb = evk + (((size_t)j * 2 + 0) * nm + id) * N;
       const u64* ka = evk + (((size_t)j * 2 + 1) * nm + id) * N;
@@ -321,7 +337,7 @@ std::vector<u64> keyswitch_accumulate(const RefCtx* c, const u64* d, int nlimbs,
         ab[n] = addm(ab[n], mulm(x[n], kb[n] % m, m), m);
         aa[n] = addm(aa[n], mulm(x[n], ka[n] % m, m), m);
       }
-    }
+    });
   }
   return acc;
 }
@@ -342,22 +358,22 @@ void moddown_pair(const RefCtx* c, u64* ks, std::vector<u64>& acc, int nlimbs, b
   BConvPlan down = make_bconv(psrc, qdst);
   for (int comp = 0; comp < 2; comp++) {
     u64* x = &acc[(size_t)comp * next * N];
-    for (int t = 0; t < next; t++) intt_fast(c, x + (size_t)t * N, ext_id[t]);
+    parts_for(next, N, [&](size_t t) { intt_fast(c, x + t * N, ext_id[t]); });
     std::vector<u64> tq((size_t)nlimbs * N);
     std::vector<const u64*> in;
     std::vector<u64*> out;
     for (int k = 0; k < K; k++) in.push_back(x + (size_t)(nlimbs + k) * N);
     for (int i = 0; i < nlimbs; i++) out.push_back(&tq[(size_t)i * N]);
     bconv_apply(down, in, out, N);
-    for (int i = 0; i < nlimbs; i++) {
+    parts_for(nlimbs, N, [&](size_t i) {
       u64 m = c->mod[i];
       u64 pinv = 1;
       for (int k = 0; k < K; k++) pinv = mulm(pinv, psrc[k] % m, m);
       pinv = invm(pinv, m);
       u64* o = ks + ((size_t)comp * nlimbs + i) * N;
-      for (size_t n = 0; n < N; n++) o[n] = mulm(subm(x[(size_t)i * N + n], tq[(size_t)i * N + n], m), pinv, m);
-      ntt_fast(c, o, i);
-    }
+      for (size_t n = 0; n < N; n++) o[n] = mulm(subm(x[i * N + n], tq[i * N + n], m), pinv, m);
+      ntt_fast(c, o, (int)i);
+    });
   }
 }
 
@@ -377,13 +393,19 @@ void automorph_eval(const RefCtx* c, u64* out, const u64* in, int id, u64 g) {
   std::copy(b.begin(), b.end(), out);
 }
 
+// The same on the nlimbs limbs of both components of a ciphertext.
+void automorph_ct(const RefCtx* c, std::vector<u64>& r0, std::vector<u64>& r1, const u64* ct, int nlimbs, u64 g) {
+  const size_t N = c->N;
+  parts_for(2 * (size_t)nlimbs, N, [&](size_t u) {
+    const int i = (int)(u % nlimbs);
+    automorph_eval(c, &(u < (size_t)nlimbs ? r0 : r1)[(size_t)i * N], ct + u * N, i, g);
+  });
+}
+
 void hrot_one(const RefCtx* c, u64* out, const u64* ct, int nlimbs, u64 g, const u64* evk) {
   const size_t N = c->N;
   std::vector<u64> r0((size_t)nlimbs * N), r1((size_t)nlimbs * N), ks((size_t)2 * nlimbs * N);
-  for (int i = 0; i < nlimbs; i++) {
-    automorph_eval(c, &r0[(size_t)i * N], ct + (size_t)i * N, i, g);
-    automorph_eval(c, &r1[(size_t)i * N], ct + ((size_t)nlimbs + i) * N, i, g);
-  }
+  automorph_ct(c, r0, r1, ct, nlimbs, g);
   keyswitch_one(c, ks.data(), r1.data(), nlimbs, evk);
   for (int i = 0; i < nlimbs; i++) {
     u64 m = c->mod[i];
@@ -400,6 +422,7 @@ extern "C" {
 
 const char* ref_last_error() { return g_err.c_str(); }
 void ref_set_threads(int n) { g_threads = n < 1 ? 1 : n; }
+void ref_set_team(int n) { g_team = n < 1 ? 1 : n; }
 int ref_get_threads() { return g_threads; }
 
 int ref_ctx_create(RefCtx** out, uint32_t logN, const u64* q, uint32_t nq, const u64* p, uint32_t np, uint32_t dnum,
@@ -509,14 +532,16 @@ int ref_pointwise(const RefCtx* c, u64* out, const u64* a, const u64* b, uint32_
                   const uint32_t* limb_ids, uint32_t nlimbs, int op /*0 add,1 sub,2 mul*/) {
   if (!check_ids(c, limb_ids, nlimbs)) return fail("bad limb id");
   const size_t N = c->N;
-  for (size_t u = 0; u < (size_t)npoly * nlimbs; u++) {
+  t_team = g_team;
+  parts_for((size_t)npoly * nlimbs, N, [&](size_t u) {
     u64 m = c->mod[limb_ids[u % nlimbs]];
     const u64* bb = b + (b_npoly == 1 ? (u % nlimbs) : u) * N;
     for (size_t n = 0; n < N; n++) {
       u64 x = a[u * N + n] % m, y = bb[n] % m;
       out[u * N + n] = op == 0 ? addm(x, y, m) : op == 1 ? subm(x, y, m) : mulm(x, y, m);
     }
-  }
+  });
+  t_team = 1;
   return 0;
 }
 
@@ -619,10 +644,10 @@ int ref_tensor_acc(const RefCtx* c, u64* d_out, const u64* ct_a, const u64* ct_b
     const u64 *a0 = ct_a + b * 2 * pl, *a1 = a0 + pl, *b0 = ct_b + b * 2 * pl, *b1 = b0 + pl;
     u64* d = d_out + b * 3 * pl;
     const u64* e = d_acc ? d_acc + b * 3 * pl : nullptr;
-    for (uint32_t i = 0; i < nlimbs; i++) {
+    parts_for(nlimbs, N, [&](size_t i) {
       u64 m = c->mod[i];
       for (size_t n = 0; n < N; n++) {
-        size_t k = (size_t)i * N + n;
+        size_t k = i * N + n;
         u64 t0 = mulm(a0[k] % m, b0[k] % m, m);
         u64 t1 = addm(mulm(a0[k] % m, b1[k] % m, m), mulm(a1[k] % m, b0[k] % m, m), m);
         u64 t2 = mulm(a1[k] % m, b1[k] % m, m);
@@ -635,7 +660,7 @@ int ref_tensor_acc(const RefCtx* c, u64* d_out, const u64* ct_a, const u64* ct_b
         d[pl + k] = t1;
         d[2 * pl + k] = t2;
       }
-    }
+    });
   });
   return 0;
 }
@@ -736,24 +761,17 @@ int ref_hrot_sum(const RefCtx* c, u64* ct_out, const u64* ct_in, uint32_t B, uin
         for (size_t n = 0; n < N; n++)
           T[(size_t)comp * el + (size_t)i * N + n] = mulm(x[(size_t)comp * pl + (size_t)i * N + n] % c->mod[i], pmod[i], c->mod[i]);
     for (uint32_t r = 0; r < R; r++) {
-      for (uint32_t i = 0; i < nlimbs; i++) {
-        automorph_eval(c, &r0[(size_t)i * N], x + (size_t)i * N, i, galois[r]);
-        automorph_eval(c, &r1[(size_t)i * N], x + pl + (size_t)i * N, i, galois[r]);
-      }
+      automorph_ct(c, r0, r1, x, nlimbs, galois[r]);
       std::vector<u64> A = keyswitch_accumulate(c, r1.data(), nlimbs, evks[r]);
       for (uint32_t i = 0; i < nlimbs; i++)
         for (size_t n = 0; n < N; n++) {
           u64& a = A[(size_t)i * N + n];
           a = addm(a, mulm(r0[(size_t)i * N + n], pmod[i], c->mod[i]), c->mod[i]);
         }
-      for (int comp = 0; comp < 2; comp++)
-        for (int t = 0; t < next; t++) {
-          u64 m = ext_mod(t);
-          for (size_t n = 0; n < N; n++) {
-            size_t k = (size_t)comp * el + (size_t)t * N + n;
-            T[k] = addm(T[k], A[k], m);
-          }
-        }
+      parts_for(2 * (size_t)next, N, [&](size_t u) {
+        const u64 m = ext_mod((int)(u % next));
+        for (size_t k = u * N; k < (u + 1) * N; k++) T[k] = addm(T[k], A[k], m);
+      });
     }
     moddown_pair(c, ct_out + bi * sz, T, nlimbs);
   });
@@ -782,10 +800,7 @@ int ref_rope(const RefCtx* c, u64* ct_out, const u64* ct_in, uint32_t B, uint32_
     for (uint32_t r = 0; r <= R; r++) {
       std::vector<u64> A(2 * el, 0);
       if (r) {
-        for (uint32_t i = 0; i < nlimbs; i++) {
-          automorph_eval(c, &r0[(size_t)i * N], x + (size_t)i * N, i, galois[r - 1]);
-          automorph_eval(c, &r1[(size_t)i * N], x + pl + (size_t)i * N, i, galois[r - 1]);
-        }
+        automorph_ct(c, r0, r1, x, nlimbs, galois[r - 1]);
         A = keyswitch_accumulate(c, r1.data(), nlimbs, evks[r - 1]);
       }
       for (int comp = 0; comp < 2; comp++)
@@ -796,13 +811,10 @@ int ref_rope(const RefCtx* c, u64* ct_out, const u64* ct_in, uint32_t B, uint32_
             const u64 v = r ? r0[(size_t)i * N + n] : x[(size_t)comp * pl + (size_t)i * N + n];
             a = addm(a, lifted(v, (int)i), c->mod[i]);
           }
-      for (int comp = 0; comp < 2; comp++)
-        for (int t = 0; t < next; t++)
-          for (size_t n = 0; n < N; n++) {
-            const u64 m = ext_mod(t);
-            const size_t k = (size_t)comp * el + (size_t)t * N + n;
-            T[k] = addm(T[k], mulm(A[k], ws[(size_t)r * el + (size_t)t * N + n], m), m);
-          }
+      parts_for(2 * (size_t)next, N, [&](size_t u) {
+        const u64 m = ext_mod((int)(u % next));
+        for (size_t k = u * N; k < (u + 1) * N; k++) T[k] = addm(T[k], mulm(A[k], ws[(size_t)r * el + k % el], m), m);
+      });
     }
     moddown_pair(c, ct_out + bi * sz, T, nlimbs);
   });
@@ -822,12 +834,10 @@ int ref_relin_rotated(const RefCtx* c, u64* ct_out, const u64* d, const u64* evk
   parallel_for(B, [&](size_t bi) {
     std::vector<u64> T(2 * el, 0), r0(pl), r1(pl);
     auto add = [&](const std::vector<u64>& A) {
-      for (int comp = 0; comp < 2; comp++)
-        for (int t = 0; t < next; t++)
-          for (size_t n = 0; n < N; n++) {
-            const size_t k = (size_t)comp * el + (size_t)t * N + n;
-            T[k] = addm(T[k], A[k], ext_mod(t));
-          }
+      parts_for(2 * (size_t)next, N, [&](size_t u) {
+        const u64 m = ext_mod((int)(u % next));
+        for (size_t k = u * N; k < (u + 1) * N; k++) T[k] = addm(T[k], A[k], m);
+      });
     };
     auto add_main = [&](int comp, const u64* x) {
       for (uint32_t i = 0; i < nlimbs; i++)
@@ -845,10 +855,7 @@ int ref_relin_rotated(const RefCtx* c, u64* ct_out, const u64* d, const u64* evk
     add_main(1, db + pl);
     for (uint32_t g = 0; g < G; g++) {
       const u64* x = y + ((size_t)g * B + bi) * 2 * pl;
-      for (uint32_t i = 0; i < nlimbs; i++) {
-        automorph_eval(c, &r0[(size_t)i * N], x + (size_t)i * N, i, galois[g]);
-        automorph_eval(c, &r1[(size_t)i * N], x + pl + (size_t)i * N, i, galois[g]);
-      }
+      automorph_ct(c, r0, r1, x, nlimbs, galois[g]);
       add(keyswitch_accumulate(c, r1.data(), nlimbs, evks[g]));
       add_main(0, r0.data());
     }
@@ -869,15 +876,20 @@ int ref_switch_sum(const RefCtx* c, u64* out, const u64* base, const u64* evk, c
   parallel_for(B, [&](size_t bi) {
     std::vector<u64> T(2 * el, 0), r0(pl), r1(pl);
     auto add = [&](const std::vector<u64>& A) {
-      for (size_t k = 0; k < 2 * el; k++) T[k] = addm(T[k], A[k], ext_mod((int)(k % el / N)));
+      parts_for(2 * (size_t)next, N, [&](size_t u) {
+        const u64 m = ext_mod((int)(u % next));
+        for (size_t k = u * N; k < (u + 1) * N; k++) T[k] = addm(T[k], A[k], m);
+      });
     };
     auto add_main = [&](int comp, const u64* x) {
-      for (size_t k = 0; k < pl; k++) {
-        const u64 m = c->mod[k / N];
-        u64 v = x[k];
-        for (int i = 0; i < c->np; i++) v = mulm(v, c->mod[c->nq + i] % m, m);
-        T[comp * el + k] = addm(T[comp * el + k], v, m);
-      }
+      parts_for(nlimbs, N, [&](size_t t) {
+        const u64 m = c->mod[t];
+        for (size_t k = t * N; k < (t + 1) * N; k++) {
+          u64 v = x[k];
+          for (int i = 0; i < c->np; i++) v = mulm(v, c->mod[c->nq + i] % m, m);
+          T[comp * el + k] = addm(T[comp * el + k], v, m);
+        }
+      });
     };
     const u64* b = base + bi * comps * pl;
     if (evk) add(keyswitch_accumulate(c, b + 2 * pl, nlimbs, evk));
@@ -885,10 +897,7 @@ int ref_switch_sum(const RefCtx* c, u64* out, const u64* base, const u64* evk, c
     add_main(1, b + pl);
     for (uint32_t g = 0; g < G; g++) {
       const u64* x = y + bi * 2 * pl;
-      for (uint32_t i = 0; i < nlimbs; i++) {
-        automorph_eval(c, &r0[(size_t)i * N], x + (size_t)i * N, i, galois[g]);
-        automorph_eval(c, &r1[(size_t)i * N], x + pl + (size_t)i * N, i, galois[g]);
-      }
+      automorph_ct(c, r0, r1, x, nlimbs, galois[g]);
       add(keyswitch_accumulate(c, r1.data(), nlimbs, evks[g]));
       add_main(0, r0.data());
     }
@@ -937,10 +946,7 @@ int ref_pcmm_bsgs_double_hoisted(const RefCtx* c, u64* ct_out, const u64* ct_in,
     std::vector<u64> r0(pl), r1(pl);
     for (uint32_t r = 1; r < n1; r++) {
       const u64 g = powm(5, (u64)r * stride, twoN);
-      for (uint32_t i = 0; i < nlimbs; i++) {
-        automorph_eval(c, &r0[(size_t)i * N], x + (size_t)i * N, i, g);
-        automorph_eval(c, &r1[(size_t)i * N], x + pl + (size_t)i * N, i, g);
-      }
+      automorph_ct(c, r0, r1, x, nlimbs, g);
       A[r] = keyswitch_accumulate(c, r1.data(), nlimbs, evk_baby[r - 1]);
       for (uint32_t i = 0; i < nlimbs; i++)
         for (size_t n = 0; n < N; n++) {
@@ -953,22 +959,15 @@ int ref_pcmm_bsgs_double_hoisted(const RefCtx* c, u64* ct_out, const u64* ct_in,
       std::fill(S.begin(), S.end(), 0);
       for (uint32_t r = 0; r < n1; r++) {
         const u64* w = pt_ext + ((size_t)g * n1 + r) * el;
-        for (int comp = 0; comp < 2; comp++)
-          for (int t = 0; t < next; t++) {
-            u64 m = ext_mod(t);
-            for (size_t n = 0; n < N; n++) {
-              size_t k = (size_t)comp * el + (size_t)t * N + n;
-              S[k] = addm(S[k], mulm(A[r][k], w[(size_t)t * N + n] % m, m), m);
-            }
-          }
+        parts_for(2 * (size_t)next, N, [&](size_t u) {
+          const u64 m = ext_mod((int)(u % next));
+          for (size_t k = u * N; k < (u + 1) * N; k++) S[k] = addm(S[k], mulm(A[r][k], w[k % el] % m, m), m);
+        });
       }
       if (g > 0) {
         moddown_pair(c, u.data(), S, nlimbs);
         const u64 gg = powm(5, (u64)g * n1 * stride, twoN);
-        for (uint32_t i = 0; i < nlimbs; i++) {
-          automorph_eval(c, &r0[(size_t)i * N], &u[(size_t)i * N], i, gg);
-          automorph_eval(c, &r1[(size_t)i * N], &u[pl + (size_t)i * N], i, gg);
-        }
+        automorph_ct(c, r0, r1, u.data(), nlimbs, gg);
         S = keyswitch_accumulate(c, r1.data(), nlimbs, evk_giant[g - 1]);
         for (uint32_t i = 0; i < nlimbs; i++)
           for (size_t n = 0; n < N; n++) {
@@ -976,14 +975,10 @@ int ref_pcmm_bsgs_double_hoisted(const RefCtx* c, u64* ct_out, const u64* ct_in,
             a = addm(a, mulm(r0[(size_t)i * N + n], pmod[i], c->mod[i]), c->mod[i]);
           }
       }
-      for (int comp = 0; comp < 2; comp++)
-        for (int t = 0; t < next; t++) {
-          u64 m = ext_mod(t);
-          for (size_t n = 0; n < N; n++) {
-            size_t k = (size_t)comp * el + (size_t)t * N + n;
-            T[k] = addm(T[k], S[k], m);
-          }
-        }
+      parts_for(2 * (size_t)next, N, [&](size_t u) {
+        const u64 m = ext_mod((int)(u % next));
+        for (size_t k = u * N; k < (u + 1) * N; k++) T[k] = addm(T[k], S[k], m);
+      });
     }
     moddown_pair(c, ct_out + bi * sz, T, nlimbs);
   });
@@ -1001,18 +996,18 @@ int ref_rescale(const RefCtx* c, u64* out, const u64* ct, uint32_t B, uint32_t n
   parallel_for((size_t)B * 2, [&](size_t p) {
     std::vector<u64> cl(ct + (p * nlimbs + last) * N, ct + (p * nlimbs + last + 1) * N);
     intt_fast(c, cl.data(), last);
-    for (uint32_t i = 0; i < last; i++) {
+    parts_for(last, N, [&](size_t i) {
       const u64 m = c->mod[i], qinv = invm(qL % m, m);
       std::vector<u64> x(ct + (p * nlimbs + i) * N, ct + (p * nlimbs + i + 1) * N);
-      intt_fast(c, x.data(), i);
+      intt_fast(c, x.data(), (int)i);
       for (size_t n = 0; n < N; n++) {
         u64 v = cl[n];
         u64 t = v > qL / 2 ? subm(v % m, qL % m, m) : v % m;  // centred representative of c_L, reduced mod q_i
         x[n] = mulm(subm(x[n], t, m), qinv, m);
       }
-      ntt_fast(c, x.data(), i);
+      ntt_fast(c, x.data(), (int)i);
       std::copy(x.begin(), x.end(), out + (p * last + i) * N);
-    }
+    });
   });
   return 0;
 }

@@ -10,3 +10,10 @@ if ROOT not in sys.path:
 
 def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a real MI355X (run with -m gpu)")
+
+
+@pytest.fixture(scope="session", autouse=True)
+def _oracle_team():
+    """The oracle on all cores, whatever a test's batch: most of the suite's time is its."""
+    from oracle import ref
+    ref.set_team(min(16, os.cpu_count() or 1))
