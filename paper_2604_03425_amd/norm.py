@@ -38,7 +38,8 @@ def rmsnorm_plan(q, nlimbs, scale, components, lo, hi, iterations, eps=0.0):
                    q[nlimbs - 1 - 2 iterations], the prime that its product with the input is rescaled by)
         error      the largest relative error of that factor on the range, without noise
     The scale of the mean square, components scale^2 / q[nlimbs - 1], may be up to about half of the primes' cube root of product: a larger
-    one is refused, since a product can only raise it."""
+    one is refused, since a product can only raise it. The scales stay where they are while a step divides by primes of one size; a chain
+    whose primes grow from step to step shrinks them, and one where an integer would be rounded by more than 2^-17 of itself is refused."""
     if not 0.0 < lo <= hi:
         raise ValueError("need 0 < lo <= hi")
     if iterations < 0 or nlimbs < 2 + 2 * iterations or nlimbs > len(q):
@@ -74,6 +75,9 @@ def rmsnorm_plan(q, nlimbs, scale, components, lo, hi, iterations, eps=0.0):
         numbers["factors"].append(round(3.0 * product / y))
         y = 2.0 * product / q[limbs - 2]
         limbs -= 2
+    # a factor off by e makes the step's result wrong by 3/2 e at most, which a further step squares
+    if min([numbers["start"]] + numbers["factors"]) < 1 << 16:
+        raise ValueError("the scales vanish over the steps: a step's primes are larger than those of the first one")
     if any(abs(v) >= 1 << 63 for v in [numbers["square"], numbers["eps"], numbers["start"]] + numbers["factors"]):
         raise ValueError("these scales take integers beyond 64 bits")
     return dict(numbers, scale=y * math.sqrt(unit), error=1.0 - least)
