@@ -204,10 +204,12 @@ struct NearIn {
 // out = base + the rotations by galois[r] with one ModDown, by P or (drop) by P q_{nlimbs-1}; R > 0, ws: a key-switch workspace for B.
 // Unweighted near rotations on two-pass rings: digits go through their last stages and the special limbs through their first inverse ones
 // in the sums' kernel, which comes first for the special limbs and then for the main ones, whose sums it finishes: neither the
-// transformed digits nor the main limbs' sums reach memory. Where all workgroups are one round (BLOCK_SUM_ROUND) the limbs go together and
-// the assembly is a kernel of its own. us, together | apart: attention of four ragged sequences at 2^13, 672 workgroups, 318 | 336; norms of 5
-// ciphertexts at 2^14, 1280, 604 | 611, of one of 12 limbs at 2^16, 4096, 1151 | 1161; 26 pairs of 64 components there 3829 | 3579.
-#define BLOCK_SUM_ROUND 4096
+// transformed digits nor the main limbs' sums reach memory. Up to BLOCK_SUM_TOGETHER workgroups, four times what the chip holds of them
+// (four to a compute unit), the limbs go together and the assembly is a kernel of its own: a part of a last round twice costs more there
+// than the main limbs' sums in memory. us, together | apart: attention of four ragged sequences at 2^13, 672 workgroups, 318 | 336; norms of
+// 5 ciphertexts at 2^14, 1280, 604 | 611, of one of 12 limbs at 2^16, 4096, 1151 | 1161; 26 pairs of 64 components there, 19 712,
+// 3829 | 3579.
+#define BLOCK_SUM_TOGETHER 4096
 int near_sums(ckks_ctx* c, const LevelTables* lt, u64* out, const NearIn& in, u32 B, u32 nlimbs, const u32* galois, const u64* const* evks,
               u32 R, bool drop, char* ws, hipStream_t st) {
   int rc;
@@ -242,7 +244,7 @@ int near_sums(ckks_ctx* c, const LevelTables* lt, u64* out, const NearIn& in, u3
     return CKKS_OK;
   };
   const u32 groups = (B + 3) / 4;
-  if ((u64)groups * (c->N / BLOCK_SUM) * lt->next <= BLOCK_SUM_ROUND) {
+  if ((u64)groups * (c->N / BLOCK_SUM) * lt->next <= BLOCK_SUM_TOGETHER) {
     if ((rc = sums(0, lt->next))) return rc;
     if (drop) rc = ks16_drop_rows(c, lt, B, nlimbs, acc, tq, st, true);
     else rc = ks16_moddown_rows(c, lt, B, nlimbs, acc, tq, st, true);

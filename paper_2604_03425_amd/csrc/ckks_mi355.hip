@@ -153,7 +153,7 @@ enum ProfKind {
   PK_FWD_FINAL = PK_INV_ROWS + 3,
   PK_AUTOMORPH = PK_FWD_FINAL + 3, PK_MODUP, PK_INNER, PK_INNER16, PK_INNER16_INT, PK_INNER_C, PK_INNER8, PK_INNER8_BIG, PK_BCONV_ROWS, PK_MODDOWN = PK_BCONV_ROWS + 3, PK_FINAL, PK_TENSOR, PK_PMACC, PK_PMACC_FP, PK_ADD,
   PK_KS12_FRONT, PK_KS12_DIGITS, PK_KS12_SPECIAL, PK_KS12_FINAL, PK_CONV_ROWS, PK_COPY, PK_PMACC_STAGED, PK_PMACC_FP_STAGED, PK_ROT_SUM, PK_PROD_SUM, PK_GATHER,
-  PK_PAIR_PRODUCTS, PK_WEIGHTED_VALUES, PK_CT_PRODUCTS, PK_KV_APPEND, PK_BLOCK_SUM, PK_COUNT
+  PK_PAIR_PRODUCTS, PK_WEIGHTED_VALUES, PK_CT_PRODUCTS, PK_KV_APPEND, PK_BLOCK_SUM, PK_CUT_PMULT, PK_COUNT
 };
 static const char* const kProfNames[PK_COUNT] = {
     "ntt_fwd_pass", "ntt_inv_pass",
@@ -167,7 +167,8 @@ static const char* const kProfNames[PK_COUNT] = {
     "pmacc_int_kernel", "pmacc_fp_kernel", "addto_kernel",
     "ks12_front_kernel", "ks12_digits_kernel", "ks12_special_kernel", "ks12_final_kernel", "conv_rows_kernel", "copy",
     "pmacc_int_staged_kernel", "pmacc_fp_staged_kernel", "rot_sum_kernel", "prod_sum_kernel", "gather_kernel",
-    "pair_products_kernel", "weighted_values_kernel", "ct_products_kernel", "kv_append_kernel", "block_sum_kernel"};
+    "pair_products_kernel", "weighted_values_kernel", "ct_products_kernel", "kv_append_kernel", "block_sum_kernel",
+    "cut_pmult_kernel"};
 struct ProfRec {
   int kind;
   hipEvent_t start, stop;

@@ -392,7 +392,7 @@ struct RmsNorm : Decoder {
     e.factor = 1;
     if (gain) {
       {
-        ProfScope ps(c, PK_TENSOR, st);
+        ProfScope ps(c, PK_CUT_PMULT, st);
         hipLaunchKernelGGL(cut_pmult_kernel, dim3(c->N / 512, limbs + 1, 2 * n), dim3(256), 0, st, g_in, e.x, gain, c->d_mods, c->logN,
                            limbs + 1);
         HIP_TRY(hipGetLastError());

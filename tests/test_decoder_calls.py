@@ -205,3 +205,12 @@ def test_the_profile_names_the_kernels_that_ran(shape, stride):
             assert counts[name] == sum(name in k for k in names), name
         assert sum(counts.values()) == len(names)
     assert any(("block_sum_kernel" if stride == 64 else "rot_sum_kernel") in k for k in launched[2])
+
+
+def test_the_profile_names_the_product_with_a_gain():
+    got, launched = answers((13, 50, 5, 60, 2, 3), [dict(NORM, stride=64, profile=True), dict(NORM, stride=64, gain=None, profile=True)])
+    for (code, _, counts), names, gains in zip(got, launched, (1, 0)):
+        assert code == 0 and sum("cut_pmult_kernel" in k for k in names) == gains
+        for name in ("cut_pmult_kernel", "tensor_kernel"):
+            assert counts[name] == sum(name in k for k in names), name
+        assert sum(counts.values()) == len(names)
