@@ -580,3 +580,45 @@ def test_the_second_stream_changes_no_result(name, knobs):
     finally:
         for knob, value in {2: 0, 4: 1}.items():
             ck.ckks_tune_set(ctx, knob, value)
+
+
+@pytest.mark.parametrize("name,nl,rows,n1,n2,stride", [("ring14", 7, 28, 34, 2, 32), ("ring14", 7, 28, 34, 1, 32), ("ring13_mixed", 5, 66, 2, 36, 16),
+                                                       ("ring13_int", 5, 74, 40, 1, 16)])
+def test_more_rotations_than_a_launch_takes_with_finished_limbs(name, nl, rows, n1, n2, stride):
+    """Enough ciphertexts for the main limbs' sums to be finished in the kernel that forms them, over two launches of rotations of which the
+    second one adds to the first one's sums."""
+    import paper_2604_03425_amd as ck
+    p, rc, ctx = contexts(name)
+    assert -(-rows // 4) * (p.N // 256) * (nl + len(p.p)) > 4096
+    s = attention_ref.Shape(p, rc, 1, 1, 1, seed=n1 + n2)
+    elements = [pow(5, i * stride, 2 * p.N) for i in range(1, n1)], [pow(5, i * n1 * stride % (p.N // 2), 2 * p.N) for i in range(1, n2)]
+    assert all(g % (p.N // 128) == 1 for e in elements for g in e)       # near rotations
+    few = [s.key() for _ in range(3)]
+    s.baby, s.giant = elements
+    s.baby_keys, s.giant_keys = ([few[i % 3] for i in range(len(e))] for e in elements)
+    dev = [to_dev(k) for k in few]
+    keys = to_dev(s.mult_key), [dev[i % 3] for i in range(n1 - 1)], [dev[i % 3] for i in range(n2 - 1)]
+    q, k, v = s.cts((rows,), nl), s.cts((rows,), nl), s.cts((rows,), nl)
+    at = [0, 1, rows // 2, rows - 1]
+    want = decoder_ref.attention(s, q[at], [k[i:i + 1] for i in at], [v[i:i + 1] for i in at], [1] * len(at), 0, 0, 3, 0)
+    out = torch.empty((rows, 2, nl - 1, p.N), dtype=torch.int64, device="cuda")
+    ws = ctx.attn_workspace(rows, rows, nl, n1, n2, 0).random_()
+    dk, dv = to_dev(k), to_dev(v)
+    ck.ckks_attn_paged(ctx, out, to_dev(q), nl, [1] * rows, [1] * rows, [x[None] for x in dk], [x[None] for x in dv], 1, nl, nl, 0, 0, 3, 0, n1, n2,
+                       stride, *keys, ws)
+    assert_same(to_host(out)[at], want, "sums")
+
+
+@pytest.mark.parametrize("name,nl", [("ring12", 4), ("ring13", 4), ("ring14", 5)])
+def test_the_norm_of_1024_components(name, nl):
+    """A hidden vector of 1024 (768 filled up with zeros): near giant steps, baby steps that leave their blocks."""
+    run_norm(name, nl, 2, 32, 32, 1, True, True)
+
+
+@pytest.mark.parametrize("nl", [6, 3, 2])
+def test_digits_of_one_limb(nl):
+    """Every digit a limb: the last one's own limb is the one that is divided away."""
+    PARAMS.setdefault("ring13_one", lambda: make_params(13, 6, 50, 1, 60, 6))
+    run_attention("ring13_one", nl, (13,), (1,), 5, 0, 0, min(1, nl - 2), 1, 1)
+    run_attention("ring13_one", nl, (3,), (2,), 2, 0, 0, min(1, nl - 2), 2, 2)
+    run_norm("ring13_one", nl, 13, 1, 2, (nl - 2) // 2, True, True)
