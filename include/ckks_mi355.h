@@ -384,7 +384,11 @@ int ckks_linattn_chunk(ckks_ctx* ctx, uint64_t* o_out, uint64_t* state_out, cons
  *   u_ts = slotsum'(q_t * k_s) + bias;   squarings times u_ts = Relin'(u_ts * u_ts);   o_t = Relin(sum_s u_ts * v_s),
  * a score function (x + bias)^(2^squarings) of the scores x (for squarings = 0 the scores and a constant). With bias = 2^squarings at the
  * scores' scale it is 2^(squarings 2^squarings) times the approximation (1 + x / 2^squarings)^(2^squarings) of exp(x). There is no
- * division by the sum of the weights: ckks_rmsnorm after it makes the result independent of their scale.
+ * division by the sum of the weights, which grows with the tokens that are seen: ckks_rmsnorm of o alone (ct_res NULL) makes the result
+ * independent of it; where o is added to a residual first, that sum decides how much of the attention enters.
+ * Every (query, token) pair that sees each other is a ciphertext of scores of its own: a relinearisation, n1 - 1 + n2 - 1 further products
+ * with keys in up to two decompositions, and a relinearisation for each squaring. Where the score may be linear in k, ckks_linattn_chunk
+ * and its state do without that.
  *   q       device [rows][2][nlimbs][N];   o_out device [rows][2][nlimbs - 1 - squarings][N], at the product of u's and v's scale
  *   bias    added to every slot as an integer
  * k_limbs >= nlimbs and v_limbs >= nlimbs - 1 - squarings >= 1; pages that no new token sees may be null. o_out may overlap neither q nor
@@ -396,6 +400,8 @@ int ckks_linattn_chunk(ckks_ctx* ctx, uint64_t* o_out, uint64_t* state_out, cons
  *   m = slotsum'(square h * h) + eps;   y = start - m;
  *   iterations times, k = 0..: u = Relin'(m * y), w = Relin'(y * y), y = Relin'(factors[k] y - u * w);
  *   ct_out = Relin(g * y),   g = h, or Rescale(gain (.) h) of h's first L + 1 limbs;   L = nlimbs - 1 - 2 iterations limbs.
+ * The mean is over the n1 * n2 components of a lane, all of them in one ciphertext, and gain is the same for the whole batch: a vector that
+ * lies in several ciphertexts is not normalised as one.
  * These are Newton's steps y (3 - m y^2) / 2 for 1 / sqrt(m) from y = start - m; eps, start and the factors are integers that every slot
  * gets and that hold the scales (paper_2604_03425_amd.rmsnorm_plan makes them).
  *   ct_x, ct_res, h_out   device [B][2][nlimbs][N];   gain device [L + 1][N] or NULL, evaluation domain;   ct_out device [B][2][L][N]
