@@ -622,3 +622,18 @@ def test_digits_of_one_limb(nl):
     run_attention("ring13_one", nl, (13,), (1,), 5, 0, 0, min(1, nl - 2), 1, 1)
     run_attention("ring13_one", nl, (3,), (2,), 2, 0, 0, min(1, nl - 2), 2, 2)
     run_norm("ring13_one", nl, 13, 1, 2, (nl - 2) // 2, True, True)
+
+
+@pytest.mark.parametrize("knob,value", [(0, 0), (1, 1), (2, 1), (2, 2), (3, 1), (4, 0), (5, 1)])
+@pytest.mark.parametrize("name", ["ring13_mixed", "ring13"])
+def test_tuning_knobs_on_many_ciphertexts(name, knob, value):
+    """13 of them: more than the relinearisations that go as sums of one rotation."""
+    import paper_2604_03425_amd as ck
+    p, rc, ctx = contexts(name)
+    default = {0: -1, 1: 0, 2: 0, 3: 2, 4: 1, 5: 0}[knob]
+    ck.ckks_tune_set(ctx, knob, value)
+    try:
+        run_attention(name, 4, (13,), (1,), 5, 0, 0, 1, 1, 2)
+        run_norm(name, 4, 13, 1, 1, 1, True, True)
+    finally:
+        ck.ckks_tune_set(ctx, knob, default)
