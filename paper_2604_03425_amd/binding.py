@@ -129,8 +129,9 @@ def _key_elems(ctx):
     return ctx.params.dnum * 2 * (ctx.nq + ctx.np_) * ctx.N
 
 
-def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+def _stream(ctx):
+    """The current stream of the context's device, which need not be the current one."""
+    return C.c_void_p(torch.cuda.current_stream(ctx.device).cuda_stream)
 
 
 def _ids(ids):
@@ -199,7 +200,7 @@ def ckks_prof_enable(ctx, on):
 def ckks_prof_copy(ctx, dst, src):
     """Plain copy of src into dst (same size), the calibration kernel for the HBM byte counters."""
     n = src.numel() * 8
-    _check(_lib.ckks_prof_copy(ctx.handle, _ptr(dst, "dst", ctx, src.numel()), _ptr(src, "src", ctx), n, _stream()))
+    _check(_lib.ckks_prof_copy(ctx.handle, _ptr(dst, "dst", ctx, src.numel()), _ptr(src, "src", ctx), n, _stream(ctx)))
 
 
 def ckks_prof_reset(ctx):
@@ -224,32 +225,32 @@ def ckks_workspace_bytes(ctx, op, batch, nlimbs, n1=0):
 
 def ckks_ntt(ctx, data, npoly, limb_ids):
     ids, n = _ids(limb_ids)
-    _check(_lib.ckks_ntt(ctx.handle, _ptr(data, "data", ctx, npoly * len(limb_ids) * ctx.N), npoly, ids, n, _stream()))
+    _check(_lib.ckks_ntt(ctx.handle, _ptr(data, "data", ctx, npoly * len(limb_ids) * ctx.N), npoly, ids, n, _stream(ctx)))
 
 
 def ckks_intt(ctx, data, npoly, limb_ids):
     ids, n = _ids(limb_ids)
-    _check(_lib.ckks_intt(ctx.handle, _ptr(data, "data", ctx, npoly * len(limb_ids) * ctx.N), npoly, ids, n, _stream()))
+    _check(_lib.ckks_intt(ctx.handle, _ptr(data, "data", ctx, npoly * len(limb_ids) * ctx.N), npoly, ids, n, _stream(ctx)))
 
 
 def ckks_automorph(ctx, out, inp, npoly, limb_ids, galois_elt, eval_domain):
     ids, n = _ids(limb_ids)
     e = npoly * len(limb_ids) * ctx.N
     _check(_lib.ckks_automorph(ctx.handle, _ptr(out, "out", ctx, e), _ptr(inp, "in", ctx, e), npoly, ids, n, galois_elt,
-                               1 if eval_domain else 0, _stream()))
+                               1 if eval_domain else 0, _stream(ctx)))
 
 
 def ckks_keyswitch(ctx, ks_out, d, B, nlimbs, evk, galois_elt, dnum, ws):
     e = B * nlimbs * ctx.N
     _check(_lib.ckks_keyswitch(ctx.handle, _ptr(ks_out, "ks_out", ctx, 2 * e), _ptr(d, "d", ctx, e), B, nlimbs,
                                _ptr(evk, "evk", ctx, _key_elems(ctx)), galois_elt, dnum, _ptr(ws, "ws", ctx),
-                               ws.numel() * 8, _stream()))
+                               ws.numel() * 8, _stream(ctx)))
 
 
 def ckks_hrot(ctx, ct_out, ct_in, B, nlimbs, galois_elt, evk_rot, ws):
     e = B * 2 * nlimbs * ctx.N
     _check(_lib.ckks_hrot(ctx.handle, _ptr(ct_out, "ct_out", ctx, e), _ptr(ct_in, "ct_in", ctx, e), B, nlimbs, galois_elt,
-                          _ptr(evk_rot, "evk_rot", ctx, _key_elems(ctx)), _ptr(ws, "ws", ctx), ws.numel() * 8, _stream()))
+                          _ptr(evk_rot, "evk_rot", ctx, _key_elems(ctx)), _ptr(ws, "ws", ctx), ws.numel() * 8, _stream(ctx)))
 
 
 def ckks_noalloc_scratch_bytes():
@@ -259,27 +260,27 @@ def ckks_noalloc_scratch_bytes():
 def ckks_hrot_noalloc(ctx, ct_out, ct_in, B, nlimbs, galois_elt, evk_rot):
     e = B * 2 * nlimbs * ctx.N
     _check(_lib.ckks_hrot_noalloc(ctx.handle, _ptr(ct_out, "ct_out", ctx, e), _ptr(ct_in, "ct_in", ctx, e), B, nlimbs,
-                                  galois_elt, _ptr(evk_rot, "evk_rot", ctx, _key_elems(ctx)), _stream()))
+                                  galois_elt, _ptr(evk_rot, "evk_rot", ctx, _key_elems(ctx)), _stream(ctx)))
 
 
 def ckks_hmult_relin(ctx, ct_out, ct_a, ct_b, B, nlimbs, evk_mult, ws):
     e = B * 2 * nlimbs * ctx.N
     _check(_lib.ckks_hmult_relin(ctx.handle, _ptr(ct_out, "ct_out", ctx, e), _ptr(ct_a, "ct_a", ctx, e),
                                  _ptr(ct_b, "ct_b", ctx, e), B, nlimbs, _ptr(evk_mult, "evk_mult", ctx, _key_elems(ctx)),
-                                 _ptr(ws, "ws", ctx), ws.numel() * 8, _stream()))
+                                 _ptr(ws, "ws", ctx), ws.numel() * 8, _stream(ctx)))
 
 
 def ckks_tensor_acc(ctx, d_out, ct_a, ct_b, d_acc, B, nlimbs):
     e = B * nlimbs * ctx.N
     _check(_lib.ckks_tensor_acc(ctx.handle, _ptr(d_out, "d_out", ctx, 3 * e), _ptr(ct_a, "ct_a", ctx, 2 * e),
                                 _ptr(ct_b, "ct_b", ctx, 2 * e),
-                                None if d_acc is None else _ptr(d_acc, "d_acc", ctx, 3 * e), B, nlimbs, _stream()))
+                                None if d_acc is None else _ptr(d_acc, "d_acc", ctx, 3 * e), B, nlimbs, _stream(ctx)))
 
 
 def ckks_relin(ctx, ct_out, d_in, B, nlimbs, evk_mult, ws):
     e = B * nlimbs * ctx.N
     _check(_lib.ckks_relin(ctx.handle, _ptr(ct_out, "ct_out", ctx, 2 * e), _ptr(d_in, "d_in", ctx, 3 * e), B, nlimbs,
-                           _ptr(evk_mult, "evk_mult", ctx, _key_elems(ctx)), _ptr(ws, "ws", ctx), ws.numel() * 8, _stream()))
+                           _ptr(evk_mult, "evk_mult", ctx, _key_elems(ctx)), _ptr(ws, "ws", ctx), ws.numel() * 8, _stream(ctx)))
 
 
 def ckks_hrot_hoisted(ctx, ct_out, ct_in, B, nlimbs, galois_elts, evks, ws):
@@ -290,7 +291,7 @@ def ckks_hrot_hoisted(ctx, ct_out, ct_in, B, nlimbs, galois_elts, evks, ws):
     keys = (C.c_void_p * max(1, R))(*[_ptr(k, "evk", ctx, _key_elems(ctx)).value for k in evks])
     e = B * 2 * nlimbs * ctx.N
     _check(_lib.ckks_hrot_hoisted(ctx.handle, _ptr(ct_out, "ct_out", ctx, R * e), _ptr(ct_in, "ct_in", ctx, e), B, nlimbs,
-                                  gs, keys, R, _ptr(ws, "ws", ctx), ws.numel() * 8, _stream()))
+                                  gs, keys, R, _ptr(ws, "ws", ctx), ws.numel() * 8, _stream(ctx)))
 
 
 def ckks_hrot_sum(ctx, ct_out, ct_in, B, nlimbs, galois_elts, evks, ws):
@@ -301,14 +302,14 @@ def ckks_hrot_sum(ctx, ct_out, ct_in, B, nlimbs, galois_elts, evks, ws):
     keys = (C.c_void_p * max(1, R))(*[_ptr(k, "evk", ctx, _key_elems(ctx)).value for k in evks])
     e = B * 2 * nlimbs * ctx.N
     _check(_lib.ckks_hrot_sum(ctx.handle, _ptr(ct_out, "ct_out", ctx, e), _ptr(ct_in, "ct_in", ctx, e), B, nlimbs, gs, keys,
-                              R, _ptr(ws, "ws", ctx), ws.numel() * 8, _stream()))
+                              R, _ptr(ws, "ws", ctx), ws.numel() * 8, _stream(ctx)))
 
 
 def ckks_hrot_add(ctx, ct_out, ct_in, ct_add, B, nlimbs, galois_elt, evk_rot, ws):
     e = B * 2 * nlimbs * ctx.N
     _check(_lib.ckks_hrot_add(ctx.handle, _ptr(ct_out, "ct_out", ctx, e), _ptr(ct_in, "ct_in", ctx, e),
                               _ptr(ct_add, "ct_add", ctx, e), B, nlimbs, galois_elt,
-                              _ptr(evk_rot, "evk_rot", ctx, _key_elems(ctx)), _ptr(ws, "ws", ctx), ws.numel() * 8, _stream()))
+                              _ptr(evk_rot, "evk_rot", ctx, _key_elems(ctx)), _ptr(ws, "ws", ctx), ws.numel() * 8, _stream(ctx)))
 
 
 def ckks_hrot_multi(ctx, ct_out, ct_in, B, nlimbs, galois_elts, evks, ws):
@@ -318,7 +319,7 @@ def ckks_hrot_multi(ctx, ct_out, ct_in, B, nlimbs, galois_elts, evks, ws):
     keys = (C.c_void_p * max(1, B))(*[_ptr(k, "evk", ctx, _key_elems(ctx)).value for k in evks])
     e = B * 2 * nlimbs * ctx.N
     _check(_lib.ckks_hrot_multi(ctx.handle, _ptr(ct_out, "ct_out", ctx, e), _ptr(ct_in, "ct_in", ctx, e), B, nlimbs, gs, keys,
-                                _ptr(ws, "ws", ctx), ws.numel() * 8, _stream()))
+                                _ptr(ws, "ws", ctx), ws.numel() * 8, _stream(ctx)))
 
 
 def ckks_pcmm_bsgs(ctx, ct_out, ct_in, B, nlimbs, pt_diag, n1, n2, stride, evk_baby, evk_giant, ws, hoisted=False):
@@ -331,25 +332,25 @@ def ckks_pcmm_bsgs(ctx, ct_out, ct_in, B, nlimbs, pt_diag, n1, n2, stride, evk_b
     pt_limbs = nlimbs + ctx.np_ if hoisted == "double" else nlimbs   # the extended-basis schedule takes extended plaintexts
     _check(fn(ctx.handle, _ptr(ct_out, "ct_out", ctx, e), _ptr(ct_in, "ct_in", ctx, e), B, nlimbs,
               _ptr(pt_diag, "pt_diag", ctx, n1 * n2 * pt_limbs * ctx.N), n1, n2, stride, baby, giant, _ptr(ws, "ws", ctx),
-              ws.numel() * 8, _stream()))
+              ws.numel() * 8, _stream(ctx)))
 
 
 def ckks_rescale(ctx, ct_out, ct_in, B, nlimbs, ws):
     _check(_lib.ckks_rescale(ctx.handle, _ptr(ct_out, "ct_out", ctx, B * 2 * (nlimbs - 1) * ctx.N),
                              _ptr(ct_in, "ct_in", ctx, B * 2 * nlimbs * ctx.N), B, nlimbs, _ptr(ws, "ws", ctx),
-                             ws.numel() * 8, _stream()))
+                             ws.numel() * 8, _stream(ctx)))
 
 
 def ckks_pmult(ctx, ct_out, ct_in, pt, B, nlimbs):
     e = B * 2 * nlimbs * ctx.N
     _check(_lib.ckks_pmult(ctx.handle, _ptr(ct_out, "ct_out", ctx, e), _ptr(ct_in, "ct_in", ctx, e),
-                           _ptr(pt, "pt", ctx, nlimbs * ctx.N), B, nlimbs, _stream()))
+                           _ptr(pt, "pt", ctx, nlimbs * ctx.N), B, nlimbs, _stream(ctx)))
 
 
 def ckks_add(ctx, out, a, b, npoly, nlimbs):
     e = npoly * nlimbs * ctx.N
     _check(_lib.ckks_add(ctx.handle, _ptr(out, "out", ctx, e), _ptr(a, "a", ctx, e), _ptr(b, "b", ctx, e), npoly, nlimbs,
-                         _stream()))
+                         _stream(ctx)))
 
 
 def ckks_pcmm_bsgs_hoisted(ctx, ct_out, ct_in, B, nlimbs, pt_diag, n1, n2, stride, evk_baby, evk_giant, ws):
@@ -376,7 +377,7 @@ def ckks_rope(ctx, ct_out, ct_in, B, nlimbs, pt_ext, npt, galois_elts, evks, ws)
     e = B * 2 * nlimbs * ctx.N
     _check(_lib.ckks_rope(ctx.handle, _ptr(ct_out, "ct_out", ctx, e), _ptr(ct_in, "ct_in", ctx, e), B, nlimbs,
                           _ptr(pt_ext, "pt_ext", ctx, npt * (R + 1) * (nlimbs + ctx.np_) * ctx.N), npt, gs,
-                          _keys(ctx, "evk", evks), R, _ptr(ws, "ws", ctx), ws.numel() * 8, _stream()))
+                          _keys(ctx, "evk", evks), R, _ptr(ws, "ws", ctx), ws.numel() * 8, _stream(ctx)))
 
 
 def _linattn(ctx, o_out, state_out, q, k, v, state_in, decay, tokens, B, nlimbs, n1, n2, evk_mult, evk_baby, evk_giant, evk_value):
@@ -396,7 +397,7 @@ def ckks_linattn_step(ctx, o_out, state_out, q, k, v, state_in, decay, B, nlimbs
     tensors, keys = _linattn(ctx, o_out, state_out, q, k, v, state_in, decay, 1, B, nlimbs, n1, n2, evk_mult, evk_baby, evk_giant,
                              evk_value)
     _check(_lib.ckks_linattn_step(ctx.handle, *tensors, B, nlimbs, n1, n2, stride, *keys, _ptr(ws, "ws", ctx), ws.numel() * 8,
-                                  _stream()))
+                                  _stream(ctx)))
 
 
 def ckks_linattn_chunk(ctx, o_out, state_out, q, k, v, state_in, decay, tokens, B, nlimbs, n1, n2, stride, evk_mult, evk_baby,
@@ -404,7 +405,7 @@ def ckks_linattn_chunk(ctx, o_out, state_out, q, k, v, state_in, decay, tokens, 
     tensors, keys = _linattn(ctx, o_out, state_out, q, k, v, state_in, decay, tokens, B, nlimbs, n1, n2, evk_mult, evk_baby,
                              evk_giant, evk_value)
     _check(_lib.ckks_linattn_chunk(ctx.handle, *tensors, tokens, B, nlimbs, n1, n2, stride, *keys, _ptr(ws, "ws", ctx),
-                                   ws.numel() * 8, _stream()))
+                                   ws.numel() * 8, _stream(ctx)))
 
 
 def _whole(low, high, **numbers):
@@ -449,7 +450,7 @@ def ckks_kv_append(ctx, k, v, in_limbs, new_lens, lens, k_pages, v_pages, page_t
     e = sum(new_lens) * 2 * in_limbs * ctx.N
     cache = _cache(ctx, new_lens, lens, k_pages, v_pages, page_tokens, k_limbs, v_limbs)
     _check(_lib.ckks_kv_append(ctx.handle, _ptr(k, "k", ctx, e), _ptr(v, "v", ctx, e), in_limbs, *cache, page_tokens, k_limbs, v_limbs,
-                               _stream()))
+                               _stream(ctx)))
 
 
 def ckks_attn_paged(ctx, o_out, q, nlimbs, new_lens, lens, k_pages, v_pages, page_tokens, k_limbs, v_limbs, window, sinks, bias,
@@ -464,7 +465,7 @@ def ckks_attn_paged(ctx, o_out, q, nlimbs, new_lens, lens, k_pages, v_pages, pag
                                 _ptr(q, "q", ctx, rows * 2 * nlimbs * ctx.N), nlimbs, *cache, page_tokens, k_limbs, v_limbs, window,
                                 sinks, bias, squarings, n1, n2, stride, _ptr(evk_mult, "evk_mult", ctx, _key_elems(ctx)),
                                 _keys(ctx, "evk_baby", evk_baby), _keys(ctx, "evk_giant", evk_giant), _ptr(ws, "ws", ctx),
-                                ws.numel() * 8, _stream()))
+                                ws.numel() * 8, _stream(ctx)))
 
 
 def ckks_rmsnorm_workspace_bytes(ctx, batch, nlimbs, n1, n2, iterations):
@@ -483,4 +484,4 @@ def ckks_rmsnorm(ctx, ct_out, h_out, ct_x, ct_res, gain, square, eps, start, fac
     _check(_lib.ckks_rmsnorm(ctx.handle, _ptr(ct_out, "ct_out", ctx, max(0, B * 2 * L * ctx.N)), optional[0],
                              _ptr(ct_x, "ct_x", ctx, e), optional[1], optional[2], square, eps, start, numbers, len(factors), B, nlimbs,
                              n1, n2, stride, _ptr(evk_mult, "evk_mult", ctx, _key_elems(ctx)), _keys(ctx, "evk_baby", evk_baby),
-                             _keys(ctx, "evk_giant", evk_giant), _ptr(ws, "ws", ctx), ws.numel() * 8, _stream()))
+                             _keys(ctx, "evk_giant", evk_giant), _ptr(ws, "ws", ctx), ws.numel() * 8, _stream(ctx)))
